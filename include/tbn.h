@@ -315,6 +315,198 @@ const char *tbn_linear_forward_binact_kernel(const uint32_t *xbits, const void *
                                              int64_t out, int32_t k, int32_t n_alpha, uint32_t flags);
 
 /*
+ * Paged key/value cache and the attention that reads it: what stands between the QKV projection and the output
+ * projection of a transformer whose linear layers are the ones above.  (The paper states no attention formula; these
+ * are the ordinary definitions, written out below.)
+ *
+ * A cache keeps the keys of many sequences in pages of `page` keys (32, 64 or 128).  Keys lie as rows, values
+ * transposed, so that both operands of the two matrix products of attention come from memory in 16-byte pieces, in the
+ * order in which the matrix instructions take them:
+ *
+ *   k[page][kv_head][row][dim]      v[page][kv_head][dim][row]
+ *
+ * One tbn_kv_pool describes the pages of one layer, one tbn_kv_index the bookkeeping that all layers share: which pages
+ * hold which sequence, how long the sequences are and how many table rows hold a page.  Both structs live in host
+ * memory and are read during the call; the arrays they point to are DEVICE memory.  No call synchronises, so lengths,
+ * page numbers and tokens per sequence may be the result of work that is still running; what they say is checked on the
+ * GPU: a page number outside the pool is taken as the nearest page of it, a length beyond max_pages * page as that.
+ *
+ * Summaries (optional; tbn_block_select needs them): for each page and kv head the largest and the smallest key per
+ * channel over the rows the page holds, rounded outwards to whole numbers of a power-of-two step:
+ *
+ *   a = max |k|,  x = the exponent with 2^(x-1) <= a < 2^x, at least -100 (also for a = 0),  step = 2^(x-6)
+ *   summary[page][kv_head][0][d] = ceil(max_row k[row][d] / step),  summary[..][1][d] = floor(min_row k[row][d] / step)
+ *
+ * A page that holds an infinity or not-a-number has codes 0 and step = infinity.
+ */
+typedef struct {
+    void *k;            /* DEVICE, n_pages x kv_heads x page x dim elements of type dt, 16-byte aligned */
+    void *v;            /* DEVICE, n_pages x kv_heads x dim x page, 16-byte aligned */
+    int8_t *summary;    /* DEVICE, n_pages x kv_heads x 2 x dim, 16-byte aligned, or NULL */
+    float *step;        /* DEVICE, n_pages x kv_heads, NULL exactly if summary is NULL */
+    int64_t n_pages;    /* at most 2^31 - 1 */
+    int32_t kv_heads;   /* 1 .. 1024 */
+    int32_t dim;        /* a multiple of 8, 8 .. 256 */
+    int32_t page;       /* 32, 64 or 128 */
+    int32_t dt;         /* tbn_dtype */
+} tbn_kv_pool;
+
+typedef struct {
+    int32_t *table;     /* DEVICE, n_seqs x max_pages: page of slot i of a sequence; slots beyond its length hold anything */
+    int32_t *lens;      /* DEVICE, n_seqs: keys of a sequence */
+    int32_t *refs;      /* DEVICE, n_pages: table rows that hold a page; 0 = free */
+    int32_t *status;    /* DEVICE, 1: 0, or one of TBN_KV_* below */
+    int64_t n_pages;
+    int32_t n_seqs;     /* 1 .. 8192 */
+    int32_t max_pages;  /* slots of a table row; max_pages * page at most 2^30 */
+    int32_t page;
+} tbn_kv_index;
+
+/* What *status says.  A call that cannot do its work changes nothing but *status (tbn_kv_fork: the pairs that can be
+ * done are done).  While *status is not 0 tbn_kv_reserve, tbn_kv_append and tbn_kv_keep do nothing, so that a program that
+ * looks at it now and then loses no cached key; it keeps the first failure until the caller clears it. */
+#define TBN_KV_FULL 1      /* not enough free pages */
+#define TBN_KV_INVALID 2   /* a negative number of tokens, a table row too short, a pair that cannot be forked */
+
+/* Bytes of device workspace for tbn_kv_reserve and tbn_kv_compact (0 on invalid sizes). */
+size_t tbn_kv_workspace_bytes(int64_t n_pages, int32_t n_seqs);
+
+/*
+ * Room for new keys: sequence s grows by n_new[s] >= 0 (its new keys' rows hold nothing yet; tbn_kv_append fills them).
+ * Fresh pages are the lowest free page numbers, in ascending order of (sequence, slot).  A last page that is not full
+ * and that other table rows hold too must not be written by two owners: in the order of sequences, each one that grows
+ * takes a fresh page in its place while more than one owner is left.  copy_src[s] and copy_dst[s] name that pair of pages
+ * (-1, -1 where there is none): hand them to tbn_kv_copy_pages for every layer before tbn_kv_append.
+ *
+ *   n_new, copy_src, copy_dst : DEVICE, n_seqs;  workspace : DEVICE, 4-byte aligned
+ * All or nothing: TBN_KV_FULL or TBN_KV_INVALID in *status otherwise (pairs are then -1).
+ */
+tbn_status tbn_kv_reserve(const tbn_kv_index *index, const int32_t *n_new, int32_t *copy_src, int32_t *copy_dst,
+                          void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Forking: sequence children[i] becomes a copy of parents[i] that shares its pages, the last one too (tbn_kv_reserve
+ * separates them when one grows).  No key is copied.  A child must be empty (length 0), must not be named twice and must
+ * not be a parent in the same call; such a pair is left out and *status set to TBN_KV_INVALID.
+ *   parents, children : DEVICE, n each (n <= n_seqs)
+ */
+tbn_status tbn_kv_fork(const tbn_kv_index *index, const int32_t *parents, const int32_t *children, int32_t n, void *stream);
+
+/*
+ * Freeing: sequence s keeps its first min(length, max(keep[s], 0)) keys and gives back the pages behind them (0: all of
+ * them); freed slots become -1.  A page is free once no table row holds it.
+ *   keep : DEVICE, n_seqs
+ */
+tbn_status tbn_kv_release(const tbn_kv_index *index, const int32_t *keep, void *stream);
+
+/*
+ * Compacting: with L pages in use, the i-th used page >= L moves to the i-th free page < L (both in ascending order), so
+ * that the pool's pages from L on are free.  Table rows and refs are rewritten; the pages themselves move when the pairs
+ * are handed to tbn_kv_copy_pages, for every layer and before anything else reads them (sources and targets are disjoint).
+ *   src, dst : DEVICE, n_pages / 2 entries each, the first *count are written;  count : DEVICE, 1
+ */
+tbn_status tbn_kv_compact(const tbn_kv_index *index, int32_t *src, int32_t *dst, int32_t *count, void *workspace,
+                          size_t workspace_bytes, void *stream);
+
+/*
+ * Copies page src[i] to page dst[i] with its summary, i < n (and i < *count where count is not NULL).  Pairs with a
+ * number outside the pool (-1) are left out.  No target may be another pair's source or target.
+ *   src, dst : DEVICE, n;  count : DEVICE, 1, or NULL
+ */
+tbn_status tbn_kv_copy_pages(const tbn_kv_pool *pool, const int32_t *src, const int32_t *dst, int64_t n,
+                             const int32_t *count, void *stream);
+
+/*
+ * New keys and values enter the cache: sequence s has n = cu_new[s + 1] - cu_new[s] of them, tokens cu_new[s] onwards of
+ * k_new and v_new; they are the last n of its lens[s] keys (tbn_kv_reserve has made the room).  The summaries of the
+ * pages they lie in are made again.
+ *
+ *   k_new, v_new : DEVICE, total tokens of kv_heads x dim elements of the pool's type, tokens k_stride / v_stride elements
+ *                  apart (at least kv_heads * dim: the parts of a fused projection's output need no copy)
+ *   cu_new       : DEVICE, n_seqs + 1, ascending from 0 to total;  max_new : at least the largest n
+ */
+tbn_status tbn_kv_append(const tbn_kv_pool *pool, const tbn_kv_index *index, const void *k_new, int64_t k_stride,
+                         const void *v_new, int64_t v_stride, const int32_t *cu_new, int64_t total, int32_t max_new,
+                         void *stream);
+
+/*
+ * Of the last keys of a sequence some stay (the accepted path of a tree of drafted tokens): key base[s] + picks[s][j]
+ * moves to base[s] + j, j < counts[s], with its value; picks ascend in each row.  Lengths and pages do not change
+ * (tbn_kv_release with base + counts follows); the summaries of the pages that hold the kept keys are made again over
+ * keys before base + counts.  Picks below j or at or beyond the sequence's length are left out.
+ *   base, counts : DEVICE, n_seqs;  picks : DEVICE, n_seqs x width
+ */
+tbn_status tbn_kv_keep(const tbn_kv_pool *pool, const tbn_kv_index *index, const int32_t *base, const int32_t *picks,
+                       int32_t width, const int32_t *counts, void *stream);
+
+/*
+ * Attention of the last keys' tokens over the cache.  Sequence s has T = cu_q[s + 1] - cu_q[s] queries, which belong to
+ * the last T of its keys (cached before the call).  Query i sees every key before those T and, among them, key j where
+ * bit j % 32 of word j / 32 of its mask row is set; without a mask, j <= i.  So one token per sequence is decoding, a
+ * mask of ancestors (a token's own bit included) is a tree of drafted tokens, no mask is a chunk of a prompt.
+ *
+ *   a_j = scale * sum_d q[i, h, d] * k[j, h / G, d]       (h / G: the query head's kv head, G = heads / kv_heads)
+ *   out[i, h, :] = sum_j e^(a_j - m) v[j, h / G, :] / sum_j e^(a_j - m)   over the keys j that query i sees, m their maximum
+ *   lse[i, h] = log sum_j e^(a_j)
+ *
+ * A query that sees no key gives out = 0 and lse = -infinity.  A key that a query does not see has no part in its result,
+ * whatever it and its value hold.  Sums are binary32; for bfloat16 the factors e^(a_j - m) are rounded to bfloat16 for the
+ * product with v (not for their sum), and out once, to nearest even.  The sum over keys may be split (by sizes, never by
+ * chance): results are the same from run to run.
+ *
+ *   q        : DEVICE, total_q tokens of heads x dim elements of the pool's type, q_stride elements apart
+ *   out      : DEVICE, total_q x heads x dim, dense;  lse : DEVICE, total_q x heads, or NULL
+ *   cu_q     : DEVICE, n_seqs + 1, ascending from 0 to total_q;  max_q : at least the largest T
+ *   mask     : DEVICE, total_q x mask_words words (mask_words >= max_q / 32 rounded up), or NULL
+ *   max_len  : at least the longest sequence (keys beyond it are not read), 0 for max_pages * page; only speed depends
+ *              on how near it is
+ *   workspace: DEVICE, 16-byte aligned, the bytes of the query for the same sizes (may be 0)
+ */
+size_t tbn_tree_attention_workspace_bytes(const tbn_kv_pool *pool, const tbn_kv_index *index, int64_t total_q, int32_t max_q,
+                                          int32_t heads, int64_t max_len);
+tbn_status tbn_tree_attention(const void *q, int64_t q_stride, void *out, float *lse, const tbn_kv_pool *pool,
+                              const tbn_kv_index *index, const int32_t *cu_q, int64_t total_q, int32_t max_q, int32_t heads,
+                              const uint32_t *mask, int32_t mask_words, int64_t max_len, float scale, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/*
+ * Which pages of its sequence a query attends to.  Queries, sequences and positions as for tbn_tree_attention without a
+ * mask; blocks are a sequence's table slots, a query's own block is the one its key lies in.  Per query and kv head:
+ * all blocks up to the own one if they are at most n_select; else the first n_sink, the last n_recent up to the own one,
+ * and of the others those with the highest scores, ties to the lower block.
+ *
+ *   c[g, d]  = rint(q[g, d] * 2^(6 - x)), x the exponent of max |q| over the G heads of the group (as for summaries)
+ *   score(b) = step_b * sum_g sum_d max(c[g, d] * summary[b][0][d], c[g, d] * summary[b][1][d])
+ *
+ * an upper bound on the group's summed logits on the block, up to the rounding of q and a factor that all blocks share;
+ * a page with an infinite step has score infinity, an infinity or not-a-number in q counts as 0.  The sums are whole
+ * numbers (exact while G * dim <= 4096), so the choice does not depend on how they are split.
+ *
+ *   picks    : DEVICE, total_q x kv_heads x n_select, ascending, -1 behind the last one
+ *   n_select : 1 .. 4096, n_sink >= 0, n_recent >= 1, n_sink + n_recent <= n_select;  heads / kv_heads at most 128
+ *   max_len  : as above, at most 2^20 pages
+ */
+size_t tbn_block_select_workspace_bytes(const tbn_kv_pool *pool, const tbn_kv_index *index, int64_t total_q, int32_t max_q,
+                                        int32_t heads, int64_t max_len);
+tbn_status tbn_block_select(const void *q, int64_t q_stride, int32_t *picks, const tbn_kv_pool *pool, const tbn_kv_index *index,
+                            const int32_t *cu_q, int64_t total_q, int32_t max_q, int32_t heads, int32_t n_select,
+                            int32_t n_sink, int32_t n_recent, int64_t max_len, void *workspace, size_t workspace_bytes,
+                            void *stream);
+
+/*
+ * Attention over picked blocks: as tbn_tree_attention without a mask, over the keys of the blocks picks[i][h / G][..] up
+ * to the query's own key.  Entries below 0 or behind the query's own block are passed over (an entry named twice counts
+ * twice).
+ *   picks : DEVICE, total_q x kv_heads x n_select (1 .. 4096)
+ */
+size_t tbn_block_attention_workspace_bytes(const tbn_kv_pool *pool, const tbn_kv_index *index, int64_t total_q, int32_t max_q,
+                                           int32_t heads, int32_t n_select);
+tbn_status tbn_block_attention(const void *q, int64_t q_stride, void *out, float *lse, const tbn_kv_pool *pool,
+                               const tbn_kv_index *index, const int32_t *cu_q, int64_t total_q, int32_t max_q, int32_t heads,
+                               const int32_t *picks, int32_t n_select, float scale, void *workspace, size_t workspace_bytes,
+                               void *stream);
+
+/*
  * Measurement aids.  No part of the method (the paper reports no kernel timings; its Section "GPU Inference Kernel"
  * measures memory only): they give the benchmark its denominators, measured the same way as the layer kernels.
  *

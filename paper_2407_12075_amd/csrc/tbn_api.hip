@@ -20,7 +20,7 @@ void set_error(const char *fmt, ...) {
 
 // An error left behind by an earlier HIP call of the process (outside this library) must not be reported as the
 // failure of the launch that follows: the entry points drop it before they enqueue anything.
-static void drop_stale_error() { (void)hipGetLastError(); }
+void drop_stale_error() { (void)hipGetLastError(); }
 
 tbn_status check_launch(const char *what) {
     hipError_t e = hipGetLastError();

@@ -14,6 +14,7 @@ constexpr int kWave = 64;
 
 // ---- host side -----------------------------------------------------------------------------
 void set_error(const char *fmt, ...);
+void drop_stale_error();
 tbn_status check_launch(const char *what);
 
 struct LinearArgs {

@@ -108,6 +108,29 @@ def lib() -> ctypes.CDLL:
         L.tbn_linear_forward_binact_kernel.argtypes = [_c_vp, _c_vp, ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_i32, _c_i32, _c_u32]
         L.tbn_conv2d_forward_kernel.restype = ctypes.c_char_p
         L.tbn_conv2d_forward_kernel.argtypes = [_c_vp, _c_vp, ctypes.c_int, *[_c_i64] * 5, *[_c_i32] * 8, _c_u32]
+        L.tbn_kv_workspace_bytes.restype = _c_sz
+        L.tbn_kv_workspace_bytes.argtypes = [_c_i64, _c_i32]
+        L.tbn_kv_reserve.argtypes = [_c_vp, _c_vp, _c_vp, _c_vp, _c_vp, _c_sz, _c_vp]
+        L.tbn_kv_fork.argtypes = [_c_vp, _c_vp, _c_vp, _c_i32, _c_vp]
+        L.tbn_kv_release.argtypes = [_c_vp, _c_vp, _c_vp]
+        L.tbn_kv_compact.argtypes = [_c_vp, _c_vp, _c_vp, _c_vp, _c_vp, _c_sz, _c_vp]
+        L.tbn_kv_copy_pages.argtypes = [_c_vp, _c_vp, _c_vp, _c_i64, _c_vp, _c_vp]
+        L.tbn_kv_append.argtypes = [_c_vp, _c_vp, _c_vp, _c_i64, _c_vp, _c_i64, _c_vp, _c_i64, _c_i32, _c_vp]
+        L.tbn_kv_keep.argtypes = [_c_vp, _c_vp, _c_vp, _c_vp, _c_i32, _c_vp, _c_vp]
+        L.tbn_tree_attention_workspace_bytes.argtypes = [_c_vp, _c_vp, _c_i64, _c_i32, _c_i32, _c_i64]
+        L.tbn_tree_attention.argtypes = [_c_vp, _c_i64, _c_vp, _c_vp, _c_vp, _c_vp, _c_vp, _c_i64, _c_i32, _c_i32, _c_vp, _c_i32, _c_i64,
+                                         ctypes.c_float, _c_vp, _c_sz, _c_vp]
+        L.tbn_block_select_workspace_bytes.argtypes = [_c_vp, _c_vp, _c_i64, _c_i32, _c_i32, _c_i64]
+        L.tbn_block_select.argtypes = [_c_vp, _c_i64, _c_vp, _c_vp, _c_vp, _c_vp, _c_i64, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32, _c_i64,
+                                       _c_vp, _c_sz, _c_vp]
+        L.tbn_block_attention_workspace_bytes.argtypes = [_c_vp, _c_vp, _c_i64, _c_i32, _c_i32, _c_i32]
+        L.tbn_block_attention.argtypes = [_c_vp, _c_i64, _c_vp, _c_vp, _c_vp, _c_vp, _c_vp, _c_i64, _c_i32, _c_i32, _c_vp, _c_i32,
+                                          ctypes.c_float, _c_vp, _c_sz, _c_vp]
+        for name in ("tree_attention", "block_select", "block_attention"):
+            getattr(L, f"tbn_{name}").restype = ctypes.c_int
+            getattr(L, f"tbn_{name}_workspace_bytes").restype = _c_sz
+        for name in ("reserve", "fork", "release", "compact", "copy_pages", "append", "keep"):
+            getattr(L, f"tbn_kv_{name}").restype = ctypes.c_int
         global _host
         try:
             from . import _tbn_host
