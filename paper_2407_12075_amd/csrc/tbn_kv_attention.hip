@@ -22,148 +22,27 @@
 // A key that a row does not see: its logit is replaced, not added to.  Its value is still multiplied by a weight of 0, so
 // in steps that hold such keys values behind the last visible key are replaced by 0, and if another value of the step is
 // infinite or not a number it is replaced by 0 too and a third product counts, for each row, the ones that it sees.
-#include "tbn_kv.h"
+#include "tbn_kv_attention.h"
 
 namespace tbn {
 
 namespace {
 
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-typedef float f32x4_t __attribute__((ext_vector_type(4)));
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-
-constexpr int kWaves = 4;
-constexpr int kThreads = kWaves * kWave;
-constexpr int kListed = 1024;   // pages of a workgroup's stretch of keys, at most
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-
-struct AttentionArgs {
-    tbn_kv_pool p;
-    tbn_kv_index ix;
-    KvQueries q;
-    void *out;
-    float *lse;
-    const uint32_t *mask;
-    int32_t mask_words;
-    const int32_t *picks;
-    int32_t n_select;
-    float c;            // scale * log2 e
-    float *part_o;      // (chunk, token, head, dim) sums, where the keys are split
-    float2 *part_ml;    // (chunk, token, head) maximum and sum
-    int32_t chunk;      // keys, or picks, of a workgroup
-    int32_t n_chunks;
-    int32_t row_tiles;  // of 16 * RT rows
-};
-
-template <typename T> struct Elem;
-template <> struct Elem<uint16_t> {
-    static constexpr int kStep = 32, kOf = 8;   // keys of a step, of a lane
-    static constexpr int kTiles = 2;            // tiles of 16 keys of a step, which share their query operand
-    typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
-    static __device__ __forceinline__ f32x4_t mma(u32x4_t a, u32x4_t b, f32x4_t c) {
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
-    }
-    // 1.0 where the bit is set
-    static __device__ __forceinline__ u32x4_t ones(uint32_t bits) {
-        u32x4_t w;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = ((bits >> (2 * e)) & 1u ? 0x3f80u : 0u) | ((bits >> (2 * e + 1)) & 1u ? 0x3f800000u : 0u);
-        return w;
-    }
-    // values with 0 for those that are not finite, and the kinds of those (limit_of)
-    static __device__ __forceinline__ void part(u32x4_t w, u32x4_t &finite, u32x4_t &kinds) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            uint32_t fin = 0, kin = 0;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint32_t x = (w[e] >> (16 * h)) & 0xffffu;
-                if ((x & 0x7f80u) != 0x7f80u) fin |= x << (16 * h);
-                else kin |= (x & 0x7fu ? 0x4580u : x & 0x8000u ? 0x4280u : 0x3f80u) << (16 * h);
-            }
-            finite[e] = fin;
-            kinds[e] = kin;
-        }
-    }
-};
-template <> struct Elem<float> {
-    static constexpr int kStep = 16, kOf = 4, kTiles = 1;
-    typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-    static __device__ __forceinline__ f32x4_t mma(u32x4_t a, u32x4_t b, f32x4_t c) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[e]), __uint_as_float(b[e]), c, 0, 0, 0);
-        return c;
-    }
-    static __device__ __forceinline__ u32x4_t ones(uint32_t bits) {
-        u32x4_t w;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = (bits >> e) & 1u ? 0x3f800000u : 0u;
-        return w;
-    }
-    static __device__ __forceinline__ void part(u32x4_t w, u32x4_t &finite, u32x4_t &kinds) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t x = w[e];
-            const bool fin = (x & 0x7f800000u) != 0x7f800000u;
-            finite[e] = fin ? x : 0u;
-            kinds[e] = fin ? 0u : x & 0x7fffffu ? 0x45800000u : x & 0x80000000u ? 0x42800000u : 0x3f800000u;
-        }
-    }
-};
-
-// What `counts` infinite values and not-a-numbers that a row sees add to its sum (kinds: 1 for +infinity, 64 for -infinity, 4096 for
-// not a number, so that a step's up to 32 keys of each can be told apart).
-__device__ __forceinline__ float limit_of(float counts) {
-    const uint32_t c = static_cast<uint32_t>(counts);
-    const bool plus = c & 63u, minus = (c >> 6) & 63u;
-    return c >= 4096u || (plus && minus) ? NAN : plus ? INFINITY : minus ? -INFINITY : 0.f;
-}
-
-// rows of a sequence: tokens x heads of the group; where its keys end for a row tile
-struct Span {
-    int t0, T, len, prefix;   // first token of the call, tokens, keys, keys before those tokens
-};
-
-__device__ __forceinline__ Span span_of(const AttentionArgs &a, int s) {
-    Span v;
-    v.t0 = max(a.q.cu_q[s], 0);
-    const int all = min(a.q.cu_q[s + 1], static_cast<int>(a.q.total_q)) - v.t0;
-    v.T = min(all, a.q.max_q);
-    v.len = len_in(a.ix.lens[s], a.q.max_len);
-    v.prefix = max(v.len - max(all, 0), 0);
-    return v;
-}
-
-__device__ __forceinline__ int keys_end(const AttentionArgs &a, const Span &v, int last_row, int G) {
-    return a.mask ? v.len : min(v.len, v.prefix + last_row / G + 1);
-}
-
-// a word with its first n bits set, as far as it has them
-__device__ __forceinline__ uint32_t first_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
-
-// 2^x: exact to one unit in the last place; results below 2^-126 are 0
-__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
-
 // RT: row tiles of a workgroup.  DP: channels the registers hold (dim <= DP; EVEN: dim == DP).
 template <typename T, int DP, int RT, bool PICKED, bool EVEN>
-__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void kv_attention_kernel(AttentionArgs a) {
+__global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_kernel(AttentionArgs a) {
     using E = Elem<T>;
     constexpr int KS = E::kStep, OF = E::kOf, NF = DP / 16, NQ = NF / E::kTiles;
     __shared__ int2 listed[kListed];   // slot and page
-    __shared__ float sums[kWaves][16][DP + 4];
-    __shared__ float maxima[kWaves][16], totals[kWaves][16];
+    __shared__ float sums[kAttnWaves][16][DP + 4];
+    __shared__ float maxima[kAttnWaves][16], totals[kAttnWaves][16];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
-    const int head = blockIdx.y, s = blockIdx.z, H = a.q.heads, KV = a.p.kv_heads, G = H / KV, D = a.p.dim, P = a.p.page;
+    const int s = blockIdx.y, H = a.q.heads, KV = a.p.kv_heads, G = H / KV, D = EVEN ? DP : a.p.dim, P = a.p.page;
     const int shift = __ffs(P) - 1;
     const Span v = span_of(a, s);
-    int x = blockIdx.x;
-    const int chunk = x % a.n_chunks;
-    x /= a.n_chunks;
-    const int base = (x % a.row_tiles) * (16 * RT);
-    const int only = x / a.row_tiles;   // PICKED: the token
+    const Block blk = block_of(a);
+    const int head = blk.head, chunk = blk.chunk, only = blk.token, base = blk.row_tile * (16 * RT);
     const int R = PICKED ? G : v.T * G;   // rows of the sequence (PICKED: of the token)
     if (base >= R || (PICKED && only >= v.T)) return;
     const int own = v.prefix + only;   // PICKED: the query's own key
@@ -177,7 +56,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void kv_attention_kern
         const int first = chunk * a.chunk;
         entries = min(a.n_select - first, a.chunk);
         const int32_t *picks = a.picks + (int64_t(v.t0 + only) * KV + head) * a.n_select + first;
-        for (int i = tid; i < entries; i += kThreads) {
+        for (int i = tid; i < entries; i += kAttnThreads) {
             const int b = picks[i];
             const bool in = b >= 0 && b < (end + P - 1) >> shift;
             listed[i] = make_int2(in ? b : -1, in ? page_in(table[b], n_pages) : 0);
@@ -186,7 +65,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void kv_attention_kern
         const int first = chunk * a.chunk;
         if (first >= end && chunk > 0) return;
         entries = (min(end, first + a.chunk) - first + P - 1) >> shift;
-        for (int i = tid; i < entries; i += kThreads) {
+        for (int i = tid; i < entries; i += kAttnThreads) {
             const int slot = (first >> shift) + i;
             listed[i] = make_int2(slot, page_in(table[slot], n_pages));
         }
@@ -205,7 +84,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void kv_attention_kern
         for (int f = 0; f < NQ; ++f) {
             const int d = f * (4 * OF) + OF * g;
             u32x4_t w = {0, 0, 0, 0};
-            if (row < R && (EVEN || d < D)) w = *reinterpret_cast<const typename E::u32x4_any *>(src + d);
+            if (row < R && (EVEN || d < D)) w = *reinterpret_cast<const typename E::u32x4_any *>(src + d) ^ a.flip;
             q[r][f] = w;
         }
     }
@@ -226,25 +105,26 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void kv_attention_kern
     const int steps = entries << sub_shift;
     // piece f of K: bfloat16 tile f % 2, channels 32 (f / 2) + 8 g; row n of tile 0 / 1 is key 8 (n / 4) + n % 4 (+ 4)
     const int k_key = OF == 8 ? 8 * (n >> 2) + (n & 3) : n;
+    // one lane offset for all pieces of K, one for all of V; what differs between pieces is the same for all lanes
+    const uint32_t k_lane = (k_key * D + OF * g) * sizeof(T), v_lane = (n * P + OF * g) * sizeof(T);
     auto load_k = [&](u32x4_t (&k)[NF], int page, int off) {
-        const T *src = kp + int64_t(page) * (page_elems * KV);
-        const int o0 = (off + k_key) * D + (OF == 8 ? 8 * g : 4 * g);
+        const T *src = kp + int64_t(page) * (page_elems * KV) + off * D;
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
             const int d = OF == 8 ? (f / 2) * 32 : f * 16;
-            const int o1 = o0 + d + (OF == 8 ? (f & 1) * 4 * D : 0);
+            const char *at = reinterpret_cast<const char *>(src + d + (OF == 8 ? (f & 1) * 4 * D : 0));
             u32x4_t w = {0, 0, 0, 0};
-            if (EVEN || d + OF * g < D) w = *reinterpret_cast<const u32x4_t *>(src + o1);
+            if (EVEN || d + OF * g < D) w = *reinterpret_cast<const u32x4_t *>(at + k_lane);
             k[f] = w;
         }
     };
     auto load_v = [&](u32x4_t (&w)[NF], int page, int off) {
-        const T *src = vp + int64_t(page) * (page_elems * KV);
-        const int o0 = n * P + off + OF * g;
+        const T *src = vp + int64_t(page) * (page_elems * KV) + off;
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
+            const char *at = reinterpret_cast<const char *>(src + f * 16 * P);
             u32x4_t x = {0, 0, 0, 0};
-            if (EVEN || f * 16 + n < D) x = *reinterpret_cast<const u32x4_t *>(src + o0 + f * 16 * P);
+            if (EVEN || f * 16 + n < D) x = *reinterpret_cast<const u32x4_t *>(at + v_lane);
             w[f] = x;
         }
     };
@@ -260,7 +140,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void kv_attention_kern
         while (i < steps) {
             key = key_of(i, page);
             if (key >= 0) break;
-            i += kWaves;
+            i += kAttnWaves;
         }
         return i;
     };
@@ -277,7 +157,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void kv_attention_kern
     const int all_see = PICKED ? end : a.mask ? v.prefix : v.prefix + base / G + 1;
     while (i < steps) {
         int next_key = 0, next_page = 0;
-        const int next = next_step(i + kWaves, next_key, next_page);
+        const int next = next_step(i + kAttnWaves, next_key, next_page);
         float p[RT][OF];
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
@@ -294,8 +174,8 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void kv_attention_kern
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                p[r][e] = s0[e] * a.c;
-                if constexpr (OF == 8) p[r][4 + e] = s1[e] * a.c;
+                p[r][e] = s0[e];
+                if constexpr (OF == 8) p[r][4 + e] = s1[e];
             }
         }
         if (next < steps) load_k(k, next_page, next_key & (P - 1));
@@ -307,18 +187,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void kv_attention_kern
             const int k0 = key + OF * g;   // this lane's keys
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                uint32_t bits = first_bits(end - k0);
-                if (!PICKED) {
-                    const int j0 = k0 - v.prefix;   // place among the call's tokens, negative for the keys before them
-                    if (a.mask) {
-                        const uint32_t *mask = a.mask + int64_t(v.t0 + place[r]) * a.mask_words;
-                        const int at = j0 >> 5;
-                        const uint32_t lo = at < 0 ? ~0u : at < a.mask_words ? mask[at] : 0u, hi = at < -1 ? ~0u : at + 1 < a.mask_words ? mask[at + 1] : 0u;
-                        bits &= __funnelshift_r(lo, hi, j0 & 31);
-                    } else {
-                        bits &= first_bits(place[r] + 1 - j0);
-                    }
-                }
+                const uint32_t bits = seen_bits<PICKED>(a, v, k0, end, place[r]);
 #pragma unroll
                 for (int e = 0; e < OF; ++e) p[r][e] = (bits >> e) & 1u ? p[r][e] : -INFINITY;
                 seen[r] = bits;
@@ -348,11 +217,9 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void kv_attention_kern
             float top = p[r][0];
 #pragma unroll
             for (int e = 1; e < OF; ++e) top = fmaxf(top, p[r][e]);
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float next_m = fmaxf(m[r], top);
-            if (__any(next_m > m[r])) {
-                const float keep = next_m > m[r] ? exp2_of(m[r] - next_m) : 1.f;   // the first time 2^-inf = 0
+            top = max_over_32(max_over_16(top)) * a.c;
+            if (__any(top > m[r] + kSlack)) {
+                const float next_m = fmaxf(m[r], top), keep = next_m > m[r] ? exp2_of(m[r] - next_m) : 1.f;   // the first time 2^-inf = 0
                 l[r] *= keep;
 #pragma unroll
                 for (int f = 0; f < NF; ++f) o[r][f] *= keep;
@@ -361,7 +228,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void kv_attention_kern
             const float from = m[r] == -INFINITY ? 0.f : m[r];   // a row that has seen nothing yet: every weight is 0
 #pragma unroll
             for (int e = 0; e < OF; ++e) {
-                p[r][e] = exp2_of(p[r][e] - from);
+                p[r][e] = exp2_of(fmaf(p[r][e], a.c, -from));
                 l[r] += p[r][e];
             }
         }
@@ -416,47 +283,37 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void kv_attention_kern
         __syncthreads();
         float top = maxima[0][n];
 #pragma unroll
-        for (int u = 1; u < kWaves; ++u) top = fmaxf(top, maxima[u][n]);
+        for (int u = 1; u < kAttnWaves; ++u) top = fmaxf(top, maxima[u][n]);
         const float f0 = top == -INFINITY ? 0.f : exp2_of(m[r] - top);
 #pragma unroll
         for (int f = 0; f < NF; ++f) *reinterpret_cast<f32x4_t *>(&sums[wave][n][f * 16 + 4 * g]) = o[r][f] * f0;
         __syncthreads();
-        for (int j = tid; j < 16 * (DP / 4); j += kThreads) {
+        for (int j = tid; j < 16 * (DP / 4); j += kAttnThreads) {
             const int rr = j / (DP / 4), d = (j - rr * (DP / 4)) * 4, row = base + r * 16 + rr;
             if (row >= R || (!EVEN && d >= D)) continue;
             float best = maxima[0][rr];
 #pragma unroll
-            for (int u = 1; u < kWaves; ++u) best = fmaxf(best, maxima[u][rr]);
+            for (int u = 1; u < kAttnWaves; ++u) best = fmaxf(best, maxima[u][rr]);
             f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
             float total = 0.f;
 #pragma unroll
-            for (int u = 0; u < kWaves; ++u) {
+            for (int u = 0; u < kAttnWaves; ++u) {
                 sum += *reinterpret_cast<const f32x4_t *>(&sums[u][rr][d]);
                 total += best == -INFINITY ? totals[u][rr] : totals[u][rr] * exp2_of(maxima[u][rr] - best);
             }
             const int t = PICKED ? only : row / G;
             const int64_t at = int64_t(v.t0 + t) * H + head * G + (PICKED ? row : row - t * G);
-            if (a.n_chunks > 1) {
-                const int64_t pa = int64_t(chunk) * a.q.total_q * H + at;
-                *reinterpret_cast<f32x4_t *>(a.part_o + pa * D + d) = sum;
-                if (d == 0) a.part_ml[pa] = make_float2(best, total);
-            } else {
-                const float inv = total == 0.f ? 0.f : 1.f / total;
-                T *out = static_cast<T *>(a.out) + at * D + d;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) ElemIO<T>::store(out + e, sum[e] * inv);
-                if (d == 0 && a.lse) a.lse[at] = total == 0.f ? -INFINITY : (best + log2f(total)) * kLn2;
-            }
+            store_sums<T>(a, chunk, at, d, sum, best, total);
         }
     }
 }
 
 // Joins the parts of one row: a workgroup per token and head, a wave per part, lanes on channels.
 template <typename T, bool PICKED>
-__global__ __launch_bounds__(kThreads) void kv_join_kernel(AttentionArgs a, int tile_rows) {
-    __shared__ float sums[kWaves][kMaxDim];
-    __shared__ float maxima[kWaves], totals[kWaves];
-    const int s = blockIdx.z, H = a.q.heads, G = H / a.p.kv_heads, D = a.p.dim;
+__global__ __launch_bounds__(kAttnThreads) void kv_join_kernel(AttentionArgs a, int tile_rows) {
+    __shared__ float sums[kAttnWaves][kMaxDim];
+    __shared__ float maxima[kAttnWaves], totals[kAttnWaves];
+    const int s = blockIdx.y, H = a.q.heads, G = H / a.p.kv_heads, D = a.p.dim;
     const int t = blockIdx.x / H, h = blockIdx.x - t * H, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const Span v = span_of(a, s);
     if (t >= v.T) return;
@@ -468,7 +325,7 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(AttentionArgs a, int 
     const int64_t at = int64_t(v.t0 + t) * H + h, stride = a.q.total_q * H;
     float m = -INFINITY, l = 0.f;
     f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-    for (int c = wave; c < parts; c += kWaves) {
+    for (int c = wave; c < parts; c += kAttnWaves) {
         const float2 ml = a.part_ml[c * stride + at];
         f32x4_t x = {0.f, 0.f, 0.f, 0.f};
         if (lane * 4 < D) x = *reinterpret_cast<const f32x4_t *>(a.part_o + (c * stride + at) * D + lane * 4);
@@ -487,9 +344,9 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(AttentionArgs a, int 
     const int d = threadIdx.x;
     float best = maxima[0], total = 0.f, sum = 0.f;
 #pragma unroll
-    for (int u = 1; u < kWaves; ++u) best = fmaxf(best, maxima[u]);
+    for (int u = 1; u < kAttnWaves; ++u) best = fmaxf(best, maxima[u]);
 #pragma unroll
-    for (int u = 0; u < kWaves; ++u) {
+    for (int u = 0; u < kAttnWaves; ++u) {
         const float f = maxima[u] == best ? 1.f : exp2_of(maxima[u] - best);
         total += totals[u] * f;
         if (d < D) sum += sums[u][d] * f;
@@ -499,24 +356,33 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(AttentionArgs a, int 
 }
 
 struct Plan {
-    int rt, chunk, n_chunks, row_tiles;
+    int rows, chunk, n_chunks, row_tiles;   // rows of a workgroup: 16, 32 or 64 in this file's kernel, 64 or 128 in the one for many rows
+    bool staged;                            // the latter
 };
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 int padded_dim(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 
-// Rows of a workgroup: what the registers hold of queries and sums (RT * 2 * DP / 16 operands of four registers).
-int most_tiles(const tbn_kv_pool &p) { return padded_dim(p.dim) == 256 ? 1 : padded_dim(p.dim) == 128 ? 2 : 4; }
+// Rows of a workgroup of this file's kernel: what the registers hold of queries and sums.
+int most_rows(const tbn_kv_pool &p) { return padded_dim(p.dim) == 256 ? 16 : padded_dim(p.dim) == 128 ? 32 : 64; }
 
-Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, int64_t unit_step, int64_t unit_most) {
+Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, int64_t unit_step, int64_t unit_most, bool picked) {
     // units: keys or picks to split, unit_step: the least stretch, a multiple of which a chunk is
     Plan pl;
-    pl.rt = 1;
-    while (pl.rt * 16 < rows && pl.rt < most_tiles(p)) pl.rt *= 2;
-    pl.row_tiles = static_cast<int>(ceil_div(rows, 16 * pl.rt));
+    pl.staged = !picked && p.dt == TBN_BF16 && rows > 32;
+    if (pl.staged) {
+        pl.rows = rows <= 64 ? 64 : 128;
+    } else {
+        pl.rows = 16;
+        while (pl.rows < rows && pl.rows < most_rows(p)) pl.rows *= 2;
+    }
+    pl.row_tiles = static_cast<int>(ceil_div(rows, pl.rows));
     const int64_t blocks = groups * pl.row_tiles;
-    const int64_t want = ceil_div(2048, blocks);   // workgroups: several per CU, so that ragged ends even out
+    // Workgroups to aim at.  The staged kernel has two per CU and is bound by the matrix cores: one round (64 drafted tokens on 131000
+    // keys: 184 - 202 us, with four rounds 227).  Here many small ones even out ragged lengths (64 sequences of 4096 - 16384 keys: 465 us;
+    // with 1024 workgroups 612, as long as the longest sequences run).
+    const int64_t want = ceil_div(pl.staged ? 512 : 8192, blocks);
     int64_t chunk = ceil_div(ceil_div(units, want), unit_step) * unit_step;
     if (chunk > unit_most) chunk = unit_most;
     pl.chunk = static_cast<int>(chunk);
@@ -526,11 +392,11 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, 
 
 Plan tree_plan(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q) {
     const int64_t rows = int64_t(q.max_q) * (q.heads / p.kv_heads);
-    return plan_of(p, rows, int64_t(ix.n_seqs) * p.kv_heads, q.max_len, 256, int64_t(kListed) * p.page);
+    return plan_of(p, rows, int64_t(ix.n_seqs) * p.kv_heads, q.max_len, 256, int64_t(kListed) * p.page, false);
 }
 
 Plan picked_plan(const tbn_kv_pool &p, const KvQueries &q, int32_t n_select) {
-    return plan_of(p, q.heads / p.kv_heads, q.total_q * p.kv_heads, n_select, p.page <= 64 ? 128 / p.page : 1, kListed);
+    return plan_of(p, q.heads / p.kv_heads, q.total_q * p.kv_heads, n_select, p.page <= 64 ? 128 / p.page : 1, kListed, true);
 }
 
 size_t workspace_of(const tbn_kv_pool &p, const KvQueries &q, const Plan &pl) {
@@ -539,30 +405,36 @@ size_t workspace_of(const tbn_kv_pool &p, const KvQueries &q, const Plan &pl) {
 
 template <typename T, int DP, int RT, bool PICKED>
 void launch_even(const AttentionArgs &a, dim3 grid, hipStream_t stream) {
-    if (a.p.dim == DP) hipLaunchKernelGGL((kv_attention_kernel<T, DP, RT, PICKED, true>), grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((kv_attention_kernel<T, DP, RT, PICKED, false>), grid, dim3(kThreads), 0, stream, a);
+    if (a.p.dim == DP) hipLaunchKernelGGL((kv_attention_kernel<T, DP, RT, PICKED, true>), grid, dim3(kAttnThreads), 0, stream, a);
+    else hipLaunchKernelGGL((kv_attention_kernel<T, DP, RT, PICKED, false>), grid, dim3(kAttnThreads), 0, stream, a);
 }
 
 template <typename T, int DP, bool PICKED>
-void launch_tiles(const AttentionArgs &a, int rt, dim3 grid, hipStream_t stream) {
-    if constexpr (DP <= 64) {
-        if (rt == 4) return launch_even<T, DP, 4, PICKED>(a, grid, stream);
+void launch_rows(const AttentionArgs &a, int rows, dim3 grid, hipStream_t stream) {
+    // many rows of bfloat16 go to the other kernel, unless they are a query's on picked blocks
+    if constexpr (DP <= 64 && (PICKED || sizeof(T) == 4)) {
+        if (rows == 64) return launch_even<T, DP, 4, PICKED>(a, grid, stream);
     }
     if constexpr (DP <= 128) {
-        if (rt == 2) return launch_even<T, DP, 2, PICKED>(a, grid, stream);
+        if (rows == 32) return launch_even<T, DP, 2, PICKED>(a, grid, stream);
     }
     launch_even<T, DP, 1, PICKED>(a, grid, stream);
 }
 
 template <typename T, bool PICKED>
-void launch_dims(const AttentionArgs &a, int rt, dim3 grid, dim3 join, hipStream_t stream) {
+void launch_dims(const AttentionArgs &a, int rows, dim3 grid, hipStream_t stream) {
     switch (padded_dim(a.p.dim)) {
-        case 64: launch_tiles<T, 64, PICKED>(a, rt, grid, stream); break;
-        case 128: launch_tiles<T, 128, PICKED>(a, rt, grid, stream); break;
-        default: launch_tiles<T, 256, PICKED>(a, rt, grid, stream);
+        case 64: launch_rows<T, 64, PICKED>(a, rows, grid, stream); break;
+        case 128: launch_rows<T, 128, PICKED>(a, rows, grid, stream); break;
+        default: launch_rows<T, 256, PICKED>(a, rows, grid, stream);
     }
-    if (a.n_chunks > 1) hipLaunchKernelGGL((kv_join_kernel<T, PICKED>), join, dim3(kThreads), 0, stream, a, 16 * rt);
 }
+
+float factor_of(float scale) {
+    const float c = fabsf(scale) * kLog2e;
+    return c < 1e-37f ? 1e-37f : c;
+}
+uint32_t flip_of(const tbn_kv_pool &p, float scale) { return !(scale < 0.f) ? 0u : p.dt == TBN_F32 ? 0x80000000u : 0x80008000u; }
 
 template <bool PICKED>
 tbn_status launch(AttentionArgs &a, const Plan &pl, float *ws, const char *what, hipStream_t stream) {
@@ -572,14 +444,19 @@ tbn_status launch(AttentionArgs &a, const Plan &pl, float *ws, const char *what,
     const int64_t parts = int64_t(pl.n_chunks) * a.q.total_q * a.q.heads;
     a.part_o = ws;
     a.part_ml = reinterpret_cast<float2 *>(ws ? ws + parts * a.p.dim : nullptr);
-    const int64_t x = int64_t(pl.n_chunks) * pl.row_tiles * (PICKED ? a.q.max_q : 1), jx = int64_t(a.q.max_q) * a.q.heads;
+    const int64_t x = int64_t(pl.n_chunks) * pl.row_tiles * a.p.kv_heads * (PICKED ? a.q.max_q : 1), jx = int64_t(a.q.max_q) * a.q.heads;
     if (x > 0x7fffffffLL || jx > 0x7fffffffLL) {
-        set_error("%s: %lld workgroups per kv head and sequence are beyond one launch", what, (long long)(x > jx ? x : jx));
+        set_error("%s: %lld workgroups per sequence are beyond one launch", what, (long long)(x > jx ? x : jx));
         return TBN_ERR_UNSUPPORTED;
     }
-    const dim3 grid(static_cast<unsigned>(x), a.p.kv_heads, a.ix.n_seqs), join(static_cast<unsigned>(jx), 1, a.ix.n_seqs);
-    if (a.p.dt == TBN_F32) launch_dims<float, PICKED>(a, pl.rt, grid, join, stream);
-    else launch_dims<uint16_t, PICKED>(a, pl.rt, grid, join, stream);
+    const dim3 grid(static_cast<unsigned>(x), a.ix.n_seqs), join(static_cast<unsigned>(jx), a.ix.n_seqs);
+    if (pl.staged) launch_kv_rows(a, pl.rows / 32, grid, stream);
+    else if (a.p.dt == TBN_F32) launch_dims<float, PICKED>(a, pl.rows, grid, stream);
+    else launch_dims<uint16_t, PICKED>(a, pl.rows, grid, stream);
+    if (a.n_chunks > 1) {
+        if (a.p.dt == TBN_F32) hipLaunchKernelGGL((kv_join_kernel<float, PICKED>), join, dim3(kAttnThreads), 0, stream, a, pl.rows);
+        else hipLaunchKernelGGL((kv_join_kernel<uint16_t, PICKED>), join, dim3(kAttnThreads), 0, stream, a, pl.rows);
+    }
     return check_launch(what);
 }
 
@@ -589,7 +466,7 @@ size_t tree_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, co
 
 tbn_status launch_tree_attention(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, void *out, float *lse, const uint32_t *mask,
                                  int32_t mask_words, float scale, float *ws, hipStream_t stream) {
-    AttentionArgs a{p, ix, q, out, lse, mask, mask_words, nullptr, 0, scale * kLog2e};
+    AttentionArgs a{p, ix, q, out, lse, mask, mask_words, nullptr, 0, factor_of(scale), flip_of(p, scale)};
     return launch<false>(a, tree_plan(p, ix, q), ws, "tbn_tree_attention", stream);
 }
 
@@ -599,7 +476,7 @@ size_t block_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &, con
 
 tbn_status launch_block_attention(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, void *out, float *lse, const int32_t *picks,
                                   int32_t n_select, float scale, float *ws, hipStream_t stream) {
-    AttentionArgs a{p, ix, q, out, lse, nullptr, 0, picks, n_select, scale * kLog2e};
+    AttentionArgs a{p, ix, q, out, lse, nullptr, 0, picks, n_select, factor_of(scale), flip_of(p, scale)};
     return launch<true>(a, picked_plan(p, q, n_select), ws, "tbn_block_attention", stream);
 }
 
