@@ -450,8 +450,8 @@ tbn_status tbn_kv_keep(const tbn_kv_pool *pool, const tbn_kv_index *index, const
  *   lse[i, h] = log sum_j e^(a_j)
  *
  * A query that sees no key gives out = 0 and lse = -infinity.  A key that a query does not see has no part in its result,
- * whatever it and its value hold.  Sums are binary32; for bfloat16 the factors e^(a_j - m) are rounded to bfloat16 for the
- * product with v (not for their sum), and out once, to nearest even.  The sum over keys may be split (by sizes, never by
+ * whatever it and its value hold.  Sums are binary32; for bfloat16 the factors e^(a_j - m) are rounded to bfloat16 in
+ * both sums of out (not for lse), and out once, to nearest even.  The sum over keys may be split (by sizes, never by
  * chance): results are the same from run to run.
  *
  *   q        : DEVICE, total_q tokens of heads x dim elements of the pool's type, q_stride elements apart

@@ -30,6 +30,19 @@ decltype(&tbn_linear_coltiled_workspace_bytes) p_coltiled_workspace_bytes;
 decltype(&tbn_linear_coltiled_forward) p_coltiled_forward;
 decltype(&tbn_sign_pack) p_sign_pack;
 decltype(&tbn_linear_forward_binact) p_forward_binact;
+decltype(&tbn_kv_reserve) p_kv_reserve;
+decltype(&tbn_kv_workspace_bytes) p_kv_workspace_bytes;
+decltype(&tbn_kv_fork) p_kv_fork;
+decltype(&tbn_kv_release) p_kv_release;
+decltype(&tbn_kv_copy_pages) p_kv_copy_pages;
+decltype(&tbn_kv_append) p_kv_append;
+decltype(&tbn_kv_keep) p_kv_keep;
+decltype(&tbn_tree_attention_workspace_bytes) p_tree_attention_workspace_bytes;
+decltype(&tbn_tree_attention) p_tree_attention;
+decltype(&tbn_block_select_workspace_bytes) p_block_select_workspace_bytes;
+decltype(&tbn_block_select) p_block_select;
+decltype(&tbn_block_attention_workspace_bytes) p_block_attention_workspace_bytes;
+decltype(&tbn_block_attention) p_block_attention;
 
 constexpr int64_t kMaxElems = int64_t(1) << 40;
 
@@ -249,6 +262,231 @@ PyObject *pack_tile(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- the paged cache ------------------------------------------------------------------------------------------------------
+// Pools and indices come as (address of the C struct, GPU): the Python object that holds the struct checked its tensors once.
+
+struct Held {
+    const void *at;
+    int64_t gpu;
+};
+
+bool held(PyObject *address, PyObject *gpu, Held &h) {
+    if (!PyLong_CheckExact(address) || !integer(gpu, 0, 1 << 20, h.gpu)) return false;
+    h.at = PyLong_AsVoidPtr(address);
+    if (PyErr_Occurred()) PyErr_Clear();
+    return h.at != nullptr;
+}
+
+const tbn_kv_pool *pool_of(const Held &h) { return static_cast<const tbn_kv_pool *>(h.at); }
+const tbn_kv_index *index_of(const Held &h) { return static_cast<const tbn_kv_index *>(h.at); }
+
+// a dense int32 tensor of at least n entries on the GPU
+int32_t *ints(PyObject *o, int64_t n, int64_t gpu) {
+    const at::Tensor *t = plain(o);
+    if (!t || t->scalar_type() != at::kInt || t->numel() < n || t->device().index() != gpu) return nullptr;
+    return static_cast<int32_t *>(t->data_ptr());
+}
+
+// (tokens, heads, dim) of the pool's type, heads dense, tokens `stride` elements apart (heads 0: any number)
+const at::Tensor *rows(PyObject *o, const Held &pool, int64_t heads, int64_t &stride) {
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    constexpr c10::DispatchKeySet kWrapped({c10::DispatchKey::FuncTorchBatched, c10::DispatchKey::FuncTorchGradWrapper,
+                                            c10::DispatchKey::Functionalize, c10::DispatchKey::Python});
+    if (!t.defined() || !t.is_cuda() || t.layout() != at::kStrided || t.dim() != 3 || t.key_set().has_any(kWrapped)) return nullptr;
+    const tbn_kv_pool *p = pool_of(pool);
+    if (t.device().index() != pool.gpu || t.scalar_type() != (p->dt == TBN_F32 ? at::kFloat : at::kBFloat16)) return nullptr;
+    const int64_t n = t.size(0), h = t.size(1), d = t.size(2);
+    if (d != p->dim || h < 1 || h > 65536 || (heads && h != heads) || n < 1) return nullptr;
+    if (t.stride(2) != 1 || (h > 1 && t.stride(1) != d) || (n > 1 && t.stride(0) < h * d)) return nullptr;
+    stride = n > 1 ? t.stride(0) : h * d;
+    return &t;
+}
+
+PyObject *none(tbn_status st) {
+    if (st == TBN_OK) Py_RETURN_TRUE;   // done, nothing to return (None would be "not taken")
+    PyObject *r = PyObject_CallFunction(g_raise, "i", static_cast<int>(st));
+    Py_XDECREF(r);
+    return nullptr;
+}
+
+at::Tensor bytes_like(const at::Tensor &t, size_t n) { return at::empty({static_cast<int64_t>(n)}, t.options().dtype(at::kByte)); }
+
+// (index, gpu, n_new)
+PyObject *kv_reserve(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    Held ix;
+    if (n_args != 3 || !ordinary_context() || !held(args[0], args[1], ix)) Py_RETURN_NONE;
+    const int64_t n = index_of(ix)->n_seqs;
+    const int32_t *fresh = ints(args[2], n, ix.gpu);
+    if (!fresh) Py_RETURN_NONE;
+    const at::Tensor &like = THPVariable_Unpack(args[2]);
+    at::Tensor src = at::empty({n}, like.options()), dst = at::empty({n}, like.options());
+    const size_t need = p_kv_workspace_bytes(index_of(ix)->n_pages, static_cast<int32_t>(n));
+    at::Tensor ws = bytes_like(like, need);
+    const tbn_status st = p_kv_reserve(index_of(ix), fresh, static_cast<int32_t *>(src.data_ptr()), static_cast<int32_t *>(dst.data_ptr()), ws.data_ptr(), need, stream());
+    return result(st, two, src, dst);
+    END_HANDLE_TH_ERRORS
+}
+
+// (index, gpu, parents, children)
+PyObject *kv_fork(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    Held ix;
+    if (n_args != 4 || !ordinary_context() || !held(args[0], args[1], ix)) Py_RETURN_NONE;
+    const int32_t *a = ints(args[2], 0, ix.gpu), *b = ints(args[3], 0, ix.gpu);
+    if (!a || !b) Py_RETURN_NONE;
+    const int64_t n = THPVariable_Unpack(args[2]).numel();
+    if (THPVariable_Unpack(args[3]).numel() != n || n > INT32_MAX) Py_RETURN_NONE;
+    return none(p_kv_fork(index_of(ix), a, b, static_cast<int32_t>(n), stream()));
+    END_HANDLE_TH_ERRORS
+}
+
+// (index, gpu, keep)
+PyObject *kv_release(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    Held ix;
+    if (n_args != 3 || !ordinary_context() || !held(args[0], args[1], ix)) Py_RETURN_NONE;
+    const int32_t *keep = ints(args[2], index_of(ix)->n_seqs, ix.gpu);
+    if (!keep) Py_RETURN_NONE;
+    return none(p_kv_release(index_of(ix), keep, stream()));
+    END_HANDLE_TH_ERRORS
+}
+
+// (pool, gpu, src, dst, count or None)
+PyObject *kv_copy_pages(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    Held pool;
+    if (n_args != 5 || !ordinary_context() || !held(args[0], args[1], pool)) Py_RETURN_NONE;
+    const int32_t *a = ints(args[2], 0, pool.gpu), *b = ints(args[3], 0, pool.gpu), *count = args[4] == Py_None ? nullptr : ints(args[4], 1, pool.gpu);
+    if (!a || !b || (!count && args[4] != Py_None)) Py_RETURN_NONE;
+    const int64_t n = THPVariable_Unpack(args[2]).numel();
+    if (THPVariable_Unpack(args[3]).numel() != n) Py_RETURN_NONE;
+    return none(p_kv_copy_pages(pool_of(pool), a, b, n, count, stream()));
+    END_HANDLE_TH_ERRORS
+}
+
+// (pool, gpu, index, gpu, k_new, v_new, cu_new, max_new)
+PyObject *kv_append(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    Held pool, ix;
+    int64_t most, ks, vs;
+    if (n_args != 8 || !ordinary_context() || !held(args[0], args[1], pool) || !held(args[2], args[3], ix) || pool.gpu != ix.gpu) Py_RETURN_NONE;
+    const at::Tensor *k = rows(args[4], pool, pool_of(pool)->kv_heads, ks), *v = rows(args[5], pool, pool_of(pool)->kv_heads, vs);
+    const int32_t *cu = ints(args[6], int64_t(index_of(ix)->n_seqs) + 1, ix.gpu);
+    if (!k || !v || !cu || k->size(0) != v->size(0) || !integer(args[7], 0, INT32_MAX, most)) Py_RETURN_NONE;
+    return none(p_kv_append(pool_of(pool), index_of(ix), k->data_ptr(), ks, v->data_ptr(), vs, cu, k->size(0), static_cast<int32_t>(most), stream()));
+    END_HANDLE_TH_ERRORS
+}
+
+// (pool, gpu, index, gpu, base, picks, counts)
+PyObject *kv_keep(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    Held pool, ix;
+    if (n_args != 7 || !ordinary_context() || !held(args[0], args[1], pool) || !held(args[2], args[3], ix) || pool.gpu != ix.gpu) Py_RETURN_NONE;
+    const int64_t n = index_of(ix)->n_seqs;
+    const int32_t *base = ints(args[4], n, ix.gpu), *picks = ints(args[5], 0, ix.gpu), *counts = ints(args[6], n, ix.gpu);
+    if (!base || !picks || !counts) Py_RETURN_NONE;
+    const at::Tensor &t = THPVariable_Unpack(args[5]);
+    if (t.dim() != 2 || t.size(0) != n || t.size(1) > INT32_MAX) Py_RETURN_NONE;
+    return none(p_kv_keep(pool_of(pool), index_of(ix), base, picks, static_cast<int32_t>(t.size(1)), counts, stream()));
+    END_HANDLE_TH_ERRORS
+}
+
+struct QueryArgs {
+    Held pool, ix;
+    const at::Tensor *q;
+    int64_t stride, max_q, max_len;
+    const int32_t *cu;
+};
+
+// (q, pool, gpu, index, gpu, cu_q, max_q, max_len or None, ...)
+bool queries(PyObject *const *args, QueryArgs &a) {
+    if (!ordinary_context() || !held(args[1], args[2], a.pool) || !held(args[3], args[4], a.ix) || a.pool.gpu != a.ix.gpu) return false;
+    a.q = rows(args[0], a.pool, 0, a.stride);
+    if (!a.q || a.q->size(1) % pool_of(a.pool)->kv_heads) return false;
+    a.cu = ints(args[5], int64_t(index_of(a.ix)->n_seqs) + 1, a.ix.gpu);
+    a.max_len = 0;
+    return a.cu && integer(args[6], 0, INT32_MAX, a.max_q) && (args[7] == Py_None || integer(args[7], 0, kMaxElems, a.max_len));
+}
+
+bool scale_of(PyObject *o, const Held &pool, float &scale) {
+    if (o == Py_None) scale = static_cast<float>(1.0 / std::sqrt(static_cast<double>(pool_of(pool)->dim)));
+    else if (PyFloat_CheckExact(o)) scale = static_cast<float>(PyFloat_AS_DOUBLE(o));
+    else return false;
+    return true;
+}
+
+// (.., mask or None, scale or None)
+PyObject *tree_attention(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    QueryArgs a;
+    float scale;
+    if (n_args != 10 || !queries(args, a) || !scale_of(args[9], a.pool, scale)) Py_RETURN_NONE;
+    const int64_t n = a.q->size(0), heads = a.q->size(1);
+    const int32_t *mask = nullptr;
+    int64_t words = 0;
+    if (args[8] != Py_None) {
+        mask = ints(args[8], 0, a.ix.gpu);
+        if (!mask) Py_RETURN_NONE;
+        const at::Tensor &t = THPVariable_Unpack(args[8]);
+        if (t.dim() != 2 || t.size(0) != n || t.size(1) > INT32_MAX) Py_RETURN_NONE;
+        words = t.size(1);
+    }
+    const auto *pool = pool_of(a.pool);
+    const auto *ix = index_of(a.ix);
+    at::Tensor out = at::empty({n, heads, pool->dim}, a.q->options()), lse = at::empty({n, heads}, a.q->options().dtype(at::kFloat)), ws;
+    const size_t need = p_tree_attention_workspace_bytes(pool, ix, n, static_cast<int32_t>(a.max_q), static_cast<int32_t>(heads), a.max_len);
+    if (need) ws = bytes_like(*a.q, need);
+    const tbn_status st = p_tree_attention(a.q->data_ptr(), a.stride, out.data_ptr(), floats(lse), pool, ix, a.cu, n, static_cast<int32_t>(a.max_q),
+                                           static_cast<int32_t>(heads), reinterpret_cast<const uint32_t *>(mask), static_cast<int32_t>(words), a.max_len, scale,
+                                           need ? ws.data_ptr() : nullptr, need, stream());
+    return result(st, two, out, lse);
+    END_HANDLE_TH_ERRORS
+}
+
+// (.., n_select, n_sink, n_recent)
+PyObject *block_select(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    QueryArgs a;
+    int64_t select, sink, recent;
+    if (n_args != 11 || !queries(args, a) || !integer(args[8], 1, 4096, select) || !integer(args[9], 0, 4096, sink) || !integer(args[10], 1, 4096, recent)) Py_RETURN_NONE;
+    const int64_t n = a.q->size(0), heads = a.q->size(1);
+    const auto *pool = pool_of(a.pool);
+    const auto *ix = index_of(a.ix);
+    at::Tensor picks = at::empty({n, pool->kv_heads, select}, a.q->options().dtype(at::kInt)), ws;
+    const size_t need = p_block_select_workspace_bytes(pool, ix, n, static_cast<int32_t>(a.max_q), static_cast<int32_t>(heads), a.max_len);
+    if (need) ws = bytes_like(*a.q, need);
+    const tbn_status st = p_block_select(a.q->data_ptr(), a.stride, static_cast<int32_t *>(picks.data_ptr()), pool, ix, a.cu, n, static_cast<int32_t>(a.max_q),
+                                         static_cast<int32_t>(heads), static_cast<int32_t>(select), static_cast<int32_t>(sink), static_cast<int32_t>(recent), a.max_len,
+                                         need ? ws.data_ptr() : nullptr, need, stream());
+    return result(st, one, picks, picks);
+    END_HANDLE_TH_ERRORS
+}
+
+// (.., picks, scale or None); max_len is not looked at
+PyObject *block_attention(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    QueryArgs a;
+    float scale;
+    if (n_args != 10 || !queries(args, a) || !scale_of(args[9], a.pool, scale)) Py_RETURN_NONE;
+    const int64_t n = a.q->size(0), heads = a.q->size(1);
+    const auto *pool = pool_of(a.pool);
+    const auto *ix = index_of(a.ix);
+    const int32_t *picks = ints(args[8], 0, a.ix.gpu);
+    if (!picks) Py_RETURN_NONE;
+    const at::Tensor &t = THPVariable_Unpack(args[8]);
+    if (t.dim() != 3 || t.size(0) != n || t.size(1) != pool->kv_heads || t.size(2) < 1 || t.size(2) > 4096) Py_RETURN_NONE;
+    const int32_t select = static_cast<int32_t>(t.size(2));
+    at::Tensor out = at::empty({n, heads, pool->dim}, a.q->options()), lse = at::empty({n, heads}, a.q->options().dtype(at::kFloat)), ws;
+    const size_t need = p_block_attention_workspace_bytes(pool, ix, n, static_cast<int32_t>(a.max_q), static_cast<int32_t>(heads), select);
+    if (need) ws = bytes_like(*a.q, need);
+    const tbn_status st = p_block_attention(a.q->data_ptr(), a.stride, out.data_ptr(), floats(lse), pool, ix, a.cu, n, static_cast<int32_t>(a.max_q),
+                                            static_cast<int32_t>(heads), picks, select, scale, need ? ws.data_ptr() : nullptr, need, stream());
+    return result(st, two, out, lse);
+    END_HANDLE_TH_ERRORS
+}
+
 // (raise, {name: address})
 PyObject *init(PyObject *, PyObject *args) {
     PyObject *raise, *table;
@@ -268,6 +506,19 @@ PyObject *init(PyObject *, PyObject *args) {
     take(p_coltiled_forward, "tbn_linear_coltiled_forward");
     take(p_sign_pack, "tbn_sign_pack");
     take(p_forward_binact, "tbn_linear_forward_binact");
+    take(p_kv_workspace_bytes, "tbn_kv_workspace_bytes");
+    take(p_kv_reserve, "tbn_kv_reserve");
+    take(p_kv_fork, "tbn_kv_fork");
+    take(p_kv_release, "tbn_kv_release");
+    take(p_kv_copy_pages, "tbn_kv_copy_pages");
+    take(p_kv_append, "tbn_kv_append");
+    take(p_kv_keep, "tbn_kv_keep");
+    take(p_tree_attention_workspace_bytes, "tbn_tree_attention_workspace_bytes");
+    take(p_tree_attention, "tbn_tree_attention");
+    take(p_block_select_workspace_bytes, "tbn_block_select_workspace_bytes");
+    take(p_block_select, "tbn_block_select");
+    take(p_block_attention_workspace_bytes, "tbn_block_attention_workspace_bytes");
+    take(p_block_attention, "tbn_block_attention");
     if (!ok) {
         PyErr_SetString(PyExc_ImportError, "_tbn_host: an entry point of the library is missing");
         return nullptr;
@@ -280,7 +531,9 @@ PyObject *init(PyObject *, PyObject *args) {
 
 #define TBN_FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {TBN_FAST(linear_forward), TBN_FAST(conv2d_forward), TBN_FAST(linear_coltiled_forward), TBN_FAST(sign_pack),
-                         TBN_FAST(linear_forward_binact), TBN_FAST(pack_tile), {"init", init, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         TBN_FAST(linear_forward_binact), TBN_FAST(pack_tile),
+                         TBN_FAST(kv_reserve), TBN_FAST(kv_fork), TBN_FAST(kv_release), TBN_FAST(kv_copy_pages), TBN_FAST(kv_append), TBN_FAST(kv_keep),
+                         TBN_FAST(tree_attention), TBN_FAST(block_select), TBN_FAST(block_attention), {"init", init, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tbn_host", "plain calls of the binding on C++ tensors", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

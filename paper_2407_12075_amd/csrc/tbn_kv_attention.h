@@ -29,7 +29,7 @@ struct AttentionArgs {   // of one launch
     float c;            // |scale| log2 e, never 0 (times an infinite logit it would be no number)
     uint32_t flip;      // sign bits of the query's elements, where the scale is negative
     float *part_o;      // (chunk, token, head, dim) sums, where the keys are split
-    float2 *part_ml;    // (chunk, token, head) maximum and sum
+    float4 *part_ml;    // (chunk, token, head) reference, sum of the weights, sum of the rounded weights, -
     int32_t chunk;      // keys, or picks, of a workgroup
     int32_t n_chunks;
     int32_t row_tiles;  // tiles of a workgroup's rows
@@ -150,6 +150,15 @@ __device__ __forceinline__ float max_over_16(float x) {
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
+// A weight is rounded to 8 bits for the product with v, as the values it multiplies have.  The sum that divides the product takes the
+// rounded ones, so that a row that one key dominates is not scaled by that key's rounding; lse has a sum of its own.
+__device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{lo, hi}, bf16x2_t));
+}
+__device__ __forceinline__ float add_two_bf16(uint32_t pair, float sum) {
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pair), __builtin_bit_cast(bf16x2_t, 0x3f803f80u), sum, false);
+}
+
 // 2^x: exact to one unit in the last place; results below 2^-126 are 0
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -167,20 +176,21 @@ __device__ __forceinline__ uint32_t seen_bits(const AttentionArgs &a, const Span
     return bits & __funnelshift_r(lo, hi, j0 & 31);
 }
 
-// Four channels of a row from its sums: to the output, or to the parts of its stretch.  m in units of log2.
+// Four channels of a row from its sums: to the output, or to the parts of its stretch.  m in units of log2; l the weights' sum, z the
+// rounded weights'.
 template <typename T>
-__device__ __forceinline__ void store_sums(const AttentionArgs &a, int chunk, int64_t at, int d, f32x4_t sum, float m, float total) {
+__device__ __forceinline__ void store_sums(const AttentionArgs &a, int chunk, int64_t at, int d, f32x4_t sum, float m, float l, float z) {
     const int D = a.p.dim;
     if (a.n_chunks > 1) {
         const int64_t pa = int64_t(chunk) * a.q.total_q * a.q.heads + at;
         *reinterpret_cast<f32x4_t *>(a.part_o + pa * D + d) = sum;
-        if (d == 0) a.part_ml[pa] = make_float2(m, total);
+        if (d == 0) a.part_ml[pa] = make_float4(m, l, z, 0.f);
     } else {
-        const float inv = total == 0.f ? 0.f : 1.f / total;
+        const float inv = z == 0.f ? 0.f : 1.f / z;
         T *out = static_cast<T *>(a.out) + at * D + d;
 #pragma unroll
         for (int e = 0; e < 4; ++e) ElemIO<T>::store(out + e, sum[e] * inv);
-        if (d == 0 && a.lse) a.lse[at] = total == 0.f ? -INFINITY : (m + log2f(total)) * kLn2;
+        if (d == 0 && a.lse) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
     }
 }
 

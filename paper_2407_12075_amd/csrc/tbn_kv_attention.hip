@@ -35,7 +35,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
     constexpr int KS = E::kStep, OF = E::kOf, NF = DP / 16, NQ = NF / E::kTiles;
     __shared__ int2 listed[kListed];   // slot and page
     __shared__ float sums[kAttnWaves][16][DP + 4];
-    __shared__ float maxima[kAttnWaves][16], totals[kAttnWaves][16];
+    __shared__ float maxima[kAttnWaves][16], totals[2][kAttnWaves][16];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
     const int s = blockIdx.y, H = a.q.heads, KV = a.p.kv_heads, G = H / KV, D = EVEN ? DP : a.p.dim, P = a.p.page;
@@ -90,11 +90,11 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
     }
 
     f32x4_t o[RT][NF];
-    float m[RT], l[RT];
+    float m[RT], l[RT], z[RT];   // reference, sum of the weights, of the rounded weights (float32: the same, not kept)
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         m[r] = -INFINITY;
-        l[r] = 0.f;
+        l[r] = z[r] = 0.f;
 #pragma unroll
         for (int f = 0; f < NF; ++f) o[r][f] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
@@ -221,6 +221,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
             if (__any(top > m[r] + kSlack)) {
                 const float next_m = fmaxf(m[r], top), keep = next_m > m[r] ? exp2_of(m[r] - next_m) : 1.f;   // the first time 2^-inf = 0
                 l[r] *= keep;
+                z[r] *= keep;
 #pragma unroll
                 for (int f = 0; f < NF; ++f) o[r][f] *= keep;
                 m[r] = next_m;
@@ -238,10 +239,12 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
         for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                if constexpr (OF == 8)   // weights in [0, 1] to 8 bits, as the values they multiply
-                    pw[r][e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{p[r][2 * e], p[r][2 * e + 1]}, bf16x2_t));
-                else
+                if constexpr (OF == 8) {
+                    pw[r][e] = two_bf16(p[r][2 * e], p[r][2 * e + 1]);
+                    z[r] = add_two_bf16(pw[r][e], z[r]);
+                } else {
                     pw[r][e] = __float_as_uint(p[r][e]);
+                }
             }
         if (!odd) {
 #pragma unroll
@@ -272,13 +275,16 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
     // the waves' sums, tile by tile
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        float lr = l[r];
+        float lr = l[r], zr = OF == 8 ? z[r] : l[r];
         lr += __shfl_xor(lr, 16);
         lr += __shfl_xor(lr, 32);
+        zr += __shfl_xor(zr, 16);
+        zr += __shfl_xor(zr, 32);
         __syncthreads();   // the arrays may still be read for the tile before
         if (g == 0) {
             maxima[wave][n] = m[r];
-            totals[wave][n] = lr;
+            totals[0][wave][n] = lr;
+            totals[1][wave][n] = zr;
         }
         __syncthreads();
         float top = maxima[0][n];
@@ -295,26 +301,29 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
 #pragma unroll
             for (int u = 1; u < kAttnWaves; ++u) best = fmaxf(best, maxima[u][rr]);
             f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
-            float total = 0.f;
+            float lsum = 0.f, zsum = 0.f;
 #pragma unroll
             for (int u = 0; u < kAttnWaves; ++u) {
+                const float f = best == -INFINITY ? 1.f : exp2_of(maxima[u][rr] - best);
+                lsum += totals[0][u][rr] * f;
+                zsum += totals[1][u][rr] * f;
                 sum += *reinterpret_cast<const f32x4_t *>(&sums[u][rr][d]);
-                total += best == -INFINITY ? totals[u][rr] : totals[u][rr] * exp2_of(maxima[u][rr] - best);
             }
             const int t = PICKED ? only : row / G;
             const int64_t at = int64_t(v.t0 + t) * H + head * G + (PICKED ? row : row - t * G);
-            store_sums<T>(a, chunk, at, d, sum, best, total);
+            store_sums<T>(a, chunk, at, d, sum, best, lsum, zsum);
         }
     }
 }
 
-// Joins the parts of one row: a workgroup per token and head, a wave per part, lanes on channels.
+// Joins the parts of one row: a workgroup per token and head; D / 4 lanes (rounded up to a power of two) take a part at a time.
 template <typename T, bool PICKED>
 __global__ __launch_bounds__(kAttnThreads) void kv_join_kernel(AttentionArgs a, int tile_rows) {
-    __shared__ float sums[kAttnWaves][kMaxDim];
-    __shared__ float maxima[kAttnWaves], totals[kAttnWaves];
-    const int s = blockIdx.y, H = a.q.heads, G = H / a.p.kv_heads, D = a.p.dim;
-    const int t = blockIdx.x / H, h = blockIdx.x - t * H, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __shared__ f32x4_t sums[kAttnThreads];
+    __shared__ float maxima[kAttnWaves];
+    __shared__ float2 totals[kAttnThreads / 16];
+    const int s = blockIdx.y, H = a.q.heads, G = H / a.p.kv_heads, D = a.p.dim, tid = threadIdx.x;
+    const int t = blockIdx.x / H, h = blockIdx.x - t * H;
     const Span v = span_of(a, s);
     if (t >= v.T) return;
     int parts = a.n_chunks;
@@ -323,36 +332,40 @@ __global__ __launch_bounds__(kAttnThreads) void kv_join_kernel(AttentionArgs a, 
         parts = max(1, (keys_end(a, v, last, G) + a.chunk - 1) / a.chunk);
     }
     const int64_t at = int64_t(v.t0 + t) * H + h, stride = a.q.total_q * H;
-    float m = -INFINITY, l = 0.f;
-    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-    for (int c = wave; c < parts; c += kAttnWaves) {
-        const float2 ml = a.part_ml[c * stride + at];
-        f32x4_t x = {0.f, 0.f, 0.f, 0.f};
-        if (lane * 4 < D) x = *reinterpret_cast<const f32x4_t *>(a.part_o + (c * stride + at) * D + lane * 4);
-        const float top = fmaxf(m, ml.x);
-        const float f0 = m == top ? 1.f : exp2_of(m - top), f1 = ml.x == top ? 1.f : exp2_of(ml.x - top);
-        o = o * f0 + x * f1;
-        l = l * f0 + ml.y * f1;
-        m = top;
-    }
-    if (lane * 4 < D) *reinterpret_cast<f32x4_t *>(&sums[wave][lane * 4]) = o;
-    if (lane == 0) {
-        maxima[wave] = m;
-        totals[wave] = l;
-    }
+    float best = -INFINITY;
+    for (int c = tid; c < parts; c += kAttnThreads) best = fmaxf(best, a.part_ml[c * stride + at].x);
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) best = fmaxf(best, __shfl_xor(best, d));
+    if ((tid & 63) == 0) maxima[tid >> 6] = best;
     __syncthreads();
-    const int d = threadIdx.x;
-    float best = maxima[0], total = 0.f, sum = 0.f;
-#pragma unroll
-    for (int u = 1; u < kAttnWaves; ++u) best = fmaxf(best, maxima[u]);
-#pragma unroll
-    for (int u = 0; u < kAttnWaves; ++u) {
-        const float f = maxima[u] == best ? 1.f : exp2_of(maxima[u] - best);
-        total += totals[u] * f;
-        if (d < D) sum += sums[u][d] * f;
+    best = fmaxf(fmaxf(maxima[0], maxima[1]), fmaxf(maxima[2], maxima[3]));
+    const int shift = D <= 64 ? 4 : D <= 128 ? 5 : 6, group = tid >> shift, groups = kAttnThreads >> shift, d = (tid & ((1 << shift) - 1)) * 4;
+    float l = 0.f, z = 0.f;
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int c = group; c < parts; c += groups) {
+        const float4 ml = a.part_ml[c * stride + at];
+        f32x4_t x = {0.f, 0.f, 0.f, 0.f};
+        if (d < D) x = *reinterpret_cast<const f32x4_t *>(a.part_o + (c * stride + at) * D + d);
+        const float f = ml.x == best ? 1.f : exp2_of(ml.x - best);   // no part has seen a key: every sum is 0
+        o += x * f;
+        l += ml.y * f;
+        z += ml.z * f;
     }
-    if (d < D) ElemIO<T>::store(static_cast<T *>(a.out) + at * D + d, total == 0.f ? 0.f : sum / total);
-    if (d == 0 && a.lse) a.lse[at] = total == 0.f ? -INFINITY : (best + log2f(total)) * kLn2;
+    sums[tid] = o;
+    if (d == 0) totals[group] = make_float2(l, z);
+    __syncthreads();
+    if (tid >= D) return;
+    const int lane = tid >> 2, e = tid & 3;
+    float sum = 0.f;
+    l = z = 0.f;
+    for (int g = 0; g < groups; ++g) {
+        sum += sums[(g << shift) + lane][e];
+        l += totals[g].x;
+        z += totals[g].y;
+    }
+    ElemIO<T>::store(static_cast<T *>(a.out) + at * D + tid, z == 0.f ? 0.f : sum / z);
+    if (tid == 0 && a.lse) a.lse[at] = l == 0.f ? -INFINITY : (best + log2f(l)) * kLn2;
 }
 
 struct Plan {
@@ -400,7 +413,7 @@ Plan picked_plan(const tbn_kv_pool &p, const KvQueries &q, int32_t n_select) {
 }
 
 size_t workspace_of(const tbn_kv_pool &p, const KvQueries &q, const Plan &pl) {
-    return pl.n_chunks > 1 ? static_cast<size_t>(pl.n_chunks) * q.total_q * q.heads * (p.dim + 2) * 4 : 0;
+    return pl.n_chunks > 1 ? static_cast<size_t>(pl.n_chunks) * q.total_q * q.heads * (p.dim + 4) * 4 : 0;
 }
 
 template <typename T, int DP, int RT, bool PICKED>
@@ -443,7 +456,7 @@ tbn_status launch(AttentionArgs &a, const Plan &pl, float *ws, const char *what,
     a.row_tiles = pl.row_tiles;
     const int64_t parts = int64_t(pl.n_chunks) * a.q.total_q * a.q.heads;
     a.part_o = ws;
-    a.part_ml = reinterpret_cast<float2 *>(ws ? ws + parts * a.p.dim : nullptr);
+    a.part_ml = reinterpret_cast<float4 *>(ws ? ws + parts * a.p.dim : nullptr);
     const int64_t x = int64_t(pl.n_chunks) * pl.row_tiles * a.p.kv_heads * (PICKED ? a.q.max_q : 1), jx = int64_t(a.q.max_q) * a.q.heads;
     if (x > 0x7fffffffLL || jx > 0x7fffffffLL) {
         set_error("%s: %lld workgroups per sequence are beyond one launch", what, (long long)(x > jx ? x : jx));

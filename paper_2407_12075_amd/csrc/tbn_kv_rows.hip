@@ -30,10 +30,6 @@ __device__ __forceinline__ f32x16_t mma(u32x4_t a, u32x4_t b, f32x16_t c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
 
-__device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{lo, hi}, bf16x2_t));
-}
-
 // key of row r of a tile of 32: the instruction's output register 4 i + j of a lane of half h is row 8 i + 4 h + j
 __device__ __forceinline__ int key_of_row(int r) { return 16 * (r >> 4) + 8 * ((r >> 2) & 1) + 4 * ((r >> 3) & 1) + (r & 3); }
 
@@ -48,7 +44,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
     // two buffers of each, as arrays of their own: the compiler then knows that reads of one do not wait for loads into the other
     __shared__ __attribute__((aligned(16))) uint16_t k0[KEYS * PITCH], k1[KEYS * PITCH], v0[DP * KEYS], v1[DP * KEYS];
     __shared__ int listed[kListed];
-    __shared__ float2 halves[RW][32];
+    __shared__ float4 halves[RW][32];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
     const int s = blockIdx.y, H = a.q.heads, KV = a.p.kv_heads, G = H / KV, D = EVEN ? DP : a.p.dim, P = a.p.page;
@@ -125,7 +121,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
     for (int f = 0; f < ND; ++f)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[f][e] = 0.f;
-    float m = -INFINITY, l = 0.f;
+    float m = -INFINITY, l = 0.f, z = 0.f;
     const int all_see = a.mask ? v.prefix : v.prefix + base / G + 1;   // keys from here on are not seen by every row
 
     auto compute = [&](int i, const uint16_t *kt, uint16_t *vt) {
@@ -160,6 +156,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
         if (__any(top > m + kSlack)) {
             const float next_m = fmaxf(m, top), keep = next_m > m ? exp2_of(m - next_m) : 1.f;
             l *= keep;
+            z *= keep;
 #pragma unroll
             for (int f = 0; f < ND; ++f) o[f] *= keep;
             m = next_m;
@@ -224,7 +221,10 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
             for (int u = 0; u < 2; ++u) {
                 u32x4_t pw;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) pw[e] = two_bf16(p[t][8 * u + 2 * e], p[t][8 * u + 2 * e + 1]);
+                for (int e = 0; e < 4; ++e) {
+                    pw[e] = two_bf16(p[t][8 * u + 2 * e], p[t][8 * u + 2 * e + 1]);
+                    z = add_two_bf16(pw[e], z);
+                }
                 const int c = (KW > 1 ? half : t) * 4 + 2 * u + h;   // this lane's eight keys, as a piece of a row of V^T
 #pragma unroll
                 for (int f = 0; f < ND; ++f) {
@@ -253,7 +253,9 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
 
     {   // the other half of each row's keys that this wave takes lies in the lane 32 away
         const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+        const auto u = __builtin_amdgcn_permlane32_swap(__float_as_uint(z), __float_as_uint(z), false, false);
         l = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+        z = __uint_as_float(u[0]) + __uint_as_float(u[1]);
     }
     if constexpr (KW > 1) {   // the second wave of a row group hands its sums to the first, lane for lane
         static_assert(KEYS * PITCH * 2 >= 32 * DP * 4, "a tile of K holds a wave's sums");
@@ -263,14 +265,15 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
             for (int f = 0; f < ND; ++f)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) box[(f * 4 + i) * kWave + lane] = f32x4_t{o[f][4 * i], o[f][4 * i + 1], o[f][4 * i + 2], o[f][4 * i + 3]};
-            if (h == 0) halves[group][n] = make_float2(m, l);
+            if (h == 0) halves[group][n] = make_float4(m, l, z, 0.f);
         }
         __syncthreads();
         if (half == 1) return;
-        const float2 other = halves[group][n];
+        const float4 other = halves[group][n];
         const float top = fmaxf(m, other.x), f0 = m == top ? 1.f : exp2_of(m - top), f1 = other.x == top ? 1.f : exp2_of(other.x - top);
         m = top;
         l = l * f0 + other.y * f1;
+        z = z * f0 + other.z * f1;
 #pragma unroll
         for (int f = 0; f < ND; ++f)
 #pragma unroll
@@ -286,7 +289,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int d = f * 32 + 8 * i + 4 * h;
-            if (EVEN || d < D) store_sums<uint16_t>(a, blk.chunk, at, d, f32x4_t{o[f][4 * i], o[f][4 * i + 1], o[f][4 * i + 2], o[f][4 * i + 3]}, m, l);
+            if (EVEN || d < D) store_sums<uint16_t>(a, blk.chunk, at, d, f32x4_t{o[f][4 * i], o[f][4 * i + 1], o[f][4 * i + 2], o[f][4 * i + 3]}, m, l, z);
         }
 }
 

@@ -12,7 +12,7 @@
 // above it and the first of those equal to it, in ascending order.
 //
 // One workgroup per query and kv head does all of it while there are enough of those to fill the GPU or few blocks;
-// otherwise the scores are made by workgroups of 512 blocks and pass through the workspace.
+// otherwise the scores are made by workgroups of 64 blocks and pass through the workspace.
 #include "tbn_kv.h"
 
 namespace tbn {
@@ -24,7 +24,7 @@ typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 constexpr int kThreads = 256;
 constexpr int kWavesOf = kThreads / kWave;
 constexpr int kInLds = 16384;     // scores of one query and kv head that are kept in LDS
-constexpr int kSliced = 512;      // blocks of a workgroup that only scores
+constexpr int kSliced = 64;       // blocks of a workgroup that only scores
 
 struct SelectArgs {
     tbn_kv_pool p;
@@ -169,6 +169,7 @@ struct SelectLds {
     uint32_t least[kWavesOf], most[kWavesOf];
     uint32_t part[2][kWavesOf];
     uint32_t bin, above;
+    bool all;
 };
 
 // inclusive prefix over the workgroup's threads; ends with the totals of the waves read by everyone
@@ -260,11 +261,16 @@ __global__ __launch_bounds__(kThreads) void kv_select_kernel(SelectArgs a) {
         if (upto >= k && upto - here < k) {   // exactly one thread
             l.bin = kThreads - 1 - tid;
             l.above = upto - here;
+            l.all = upto == k;
         }
         __syncthreads();
         above = l.above;
         least += l.bin << cut;
         most = most - least < (1u << cut) ? most : least + ((1u << cut) - 1u);
+        if (l.all) {   // the whole bin is taken: everything beyond the word in front of it (scores' words are above 0)
+            most = --least;
+            above = k;
+        }
         __syncthreads();
     }
     // `least` is the k-th largest word; k - above of those equal to it are taken, the lowest blocks first
@@ -288,7 +294,7 @@ __global__ __launch_bounds__(kThreads) void kv_select_kernel(SelectArgs a) {
 // The scores pass through the workspace where the queries and heads alone leave CUs idle and there is enough to share out, or
 // where they do not fit into LDS.
 bool sliced(const tbn_kv_pool &p, const KvQueries &q, int64_t blocks) {
-    return blocks > kInLds || (q.total_q * p.kv_heads < 128 && blocks > kSliced);
+    return blocks > kInLds || (q.total_q * p.kv_heads < 128 && blocks > 512);
 }
 
 int64_t blocks_of(const tbn_kv_pool &p, const KvQueries &q) { return (q.max_len + p.page - 1) / p.page; }

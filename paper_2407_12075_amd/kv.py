@@ -58,7 +58,7 @@ class KVPool:
         self.n_pages, self.kv_heads, self.page, self.dim, self.dtype, self.device = n, h, p, d, k.dtype, k.device
         self._c = _Pool(_dev(k, "k"), _dev(v, "v"), None if summary is None else _dev(summary, "summary", torch.int8),
                         None if step is None else _dev(step, "step", torch.float32), n, h, d, p, _dt(k))
-        self._at = ctypes.addressof(self._c)
+        self._at, self._gpu = ctypes.addressof(self._c), k.device.index
 
 
 class KVIndex:
@@ -72,7 +72,7 @@ class KVIndex:
         self.n_seqs, self.max_pages, self.n_pages, self.page, self.device = table.shape[0], table.shape[1], refs.numel(), page, table.device
         self._c = _Index(*(_dev(t, n, torch.int32) for t, n in ((table, "table"), (lens, "lens"), (refs, "refs"), (status, "status"))),
                          self.n_pages, self.n_seqs, self.max_pages, page)
-        self._at = ctypes.addressof(self._c)
+        self._at, self._gpu = ctypes.addressof(self._c), table.device.index
         self._ws = int(lib().tbn_kv_workspace_bytes(self.n_pages, self.n_seqs))
 
 
@@ -130,6 +130,11 @@ def _workspace(need: int, workspace: Optional[torch.Tensor], device: torch.devic
     return _dev(workspace, "workspace"), workspace.numel() * workspace.element_size()
 
 
+def _plain(*defaults) -> bool:
+    """Whether a call has the plain form that the extension module takes: nothing given that it allocates itself, the current stream."""
+    return tbn._host is not None and tbn._recording is None and all(d is None for d in defaults)
+
+
 def _done(st: int):
     if st != TBN_OK:
         _raise(st)
@@ -137,6 +142,10 @@ def _done(st: int):
 
 def tbn_kv_reserve(index: KVIndex, n_new: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Room for n_new[s] more keys of each sequence; returns the pairs of pages (-1: none) for tbn_kv_copy_pages."""
+    if _plain(workspace, stream):
+        r = tbn._host.kv_reserve(index._at, index._gpu, n_new)
+        if r is not None:
+            return r
     pairs = torch.empty((2, index.n_seqs), dtype=torch.int32, device=index.device)
     ws, size = _workspace(index._ws, workspace, index.device)
     at = pairs.data_ptr()
@@ -146,6 +155,8 @@ def tbn_kv_reserve(index: KVIndex, n_new: torch.Tensor, workspace: Optional[torc
 
 def tbn_kv_fork(index: KVIndex, parents: torch.Tensor, children: torch.Tensor, stream=None) -> None:
     """Sequence children[i], which is empty, shares the pages of parents[i]."""
+    if _plain(stream) and tbn._host.kv_fork(index._at, index._gpu, parents, children):
+        return
     n = parents.numel()
     if children.numel() != n:
         raise ValueError("parents and children must have the same length")
@@ -154,6 +165,8 @@ def tbn_kv_fork(index: KVIndex, parents: torch.Tensor, children: torch.Tensor, s
 
 def tbn_kv_release(index: KVIndex, keep: torch.Tensor, stream=None) -> None:
     """Sequence s keeps its first keep[s] keys at most and gives back the pages behind them."""
+    if _plain(stream) and tbn._host.kv_release(index._at, index._gpu, keep):
+        return
     _done(_call("tbn_kv_release", index._at, _ints(keep, "keep", index.n_seqs, index.device), _stream(stream)))
 
 
@@ -169,6 +182,8 @@ def tbn_kv_compact(index: KVIndex, workspace: Optional[torch.Tensor] = None, str
 
 def tbn_kv_copy_pages(pool: KVPool, src: torch.Tensor, dst: torch.Tensor, count: Optional[torch.Tensor] = None, stream=None) -> None:
     """Copies page src[i] to page dst[i], of the first count pairs if count is given; pairs with -1 are left out."""
+    if _plain(stream) and tbn._host.kv_copy_pages(pool._at, pool._gpu, src, dst, count):
+        return
     n = src.numel()
     if dst.numel() != n:
         raise ValueError("src and dst must have the same length")
@@ -178,6 +193,8 @@ def tbn_kv_copy_pages(pool: KVPool, src: torch.Tensor, dst: torch.Tensor, count:
 
 def tbn_kv_append(pool: KVPool, index: KVIndex, k_new: torch.Tensor, v_new: torch.Tensor, cu_new: torch.Tensor, max_new: int, stream=None) -> None:
     """Keys and values (tokens, kv_heads, dim) become the last cu_new[s + 1] - cu_new[s] <= max_new of each sequence."""
+    if _plain(stream) and tbn._host.kv_append(pool._at, pool._gpu, index._at, index._gpu, k_new, v_new, cu_new, max_new):
+        return
     _agree(pool, index)
     k, ks = _rows(k_new, "k_new", pool.kv_heads, pool.dim, pool)
     v, vs = _rows(v_new, "v_new", pool.kv_heads, pool.dim, pool)
@@ -188,6 +205,8 @@ def tbn_kv_append(pool: KVPool, index: KVIndex, k_new: torch.Tensor, v_new: torc
 
 def tbn_kv_keep(pool: KVPool, index: KVIndex, base: torch.Tensor, picks: torch.Tensor, counts: torch.Tensor, stream=None) -> None:
     """Key base[s] + picks[s, j] moves to base[s] + j for j < counts[s] (picks ascend)."""
+    if _plain(stream) and tbn._host.kv_keep(pool._at, pool._gpu, index._at, index._gpu, base, picks, counts):
+        return
     _agree(pool, index)
     if picks.dim() != 2 or picks.shape[0] != index.n_seqs:
         raise ValueError("picks must be (n_seqs, width)")
@@ -224,6 +243,10 @@ def tbn_tree_attention(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: torc
                        lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Queries q (tokens, heads, dim) of each sequence's last keys against its cache; mask int32 (tokens, words): bit j of a row
     is set where the token sees the sequence's j-th query token (None: its own and the earlier ones).  Returns (out, lse)."""
+    if _plain(out, lse, workspace, stream):
+        r = tbn._host.tree_attention(q, pool._at, pool._gpu, index._at, index._gpu, cu_q, max_q, max_len, mask, scale)
+        if r is not None:
+            return r
     at, stride, cu = _queries(q, pool, index, cu_q)
     out, lse = _outputs(q, out, lse)
     words = 0
@@ -248,6 +271,10 @@ def tbn_block_select(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: torch.
                      max_len: Optional[int] = None, picks: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                      stream=None) -> torch.Tensor:
     """Per query and kv head n_select of its sequence's pages: int32 (tokens, kv_heads, n_select), ascending, -1 behind the last."""
+    if _plain(picks, workspace, stream):
+        r = tbn._host.block_select(q, pool._at, pool._gpu, index._at, index._gpu, cu_q, max_q, max_len, n_select, n_sink, n_recent)
+        if r is not None:
+            return r
     at, stride, cu = _queries(q, pool, index, cu_q)
     shape = (q.shape[0], pool.kv_heads, n_select)
     if picks is None:
@@ -269,6 +296,10 @@ def tbn_block_attention(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: tor
                         out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                         stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """tbn_tree_attention without a mask over the keys of the picked pages only.  Returns (out, lse)."""
+    if _plain(out, lse, workspace, stream):
+        r = tbn._host.block_attention(q, pool._at, pool._gpu, index._at, index._gpu, cu_q, max_q, None, picks, scale)
+        if r is not None:
+            return r
     at, stride, cu = _queries(q, pool, index, cu_q)
     out, lse = _outputs(q, out, lse)
     if picks.dim() != 3 or tuple(picks.shape[:2]) != (q.shape[0], pool.kv_heads):

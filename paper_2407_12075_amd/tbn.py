@@ -136,7 +136,10 @@ def lib() -> ctypes.CDLL:
             from . import _tbn_host
             _tbn_host.init(_raise, {name: ctypes.cast(getattr(L, name), _c_vp).value for name in (
                 "tbn_pack_workspace_bytes", "tbn_pack_tile", "tbn_linear_forward", "tbn_conv2d_forward", "tbn_sign_pack",
-                "tbn_linear_coltiled_workspace_bytes", "tbn_linear_coltiled_forward", "tbn_linear_forward_binact")})
+                "tbn_linear_coltiled_workspace_bytes", "tbn_linear_coltiled_forward", "tbn_linear_forward_binact", "tbn_kv_workspace_bytes",
+                "tbn_kv_reserve", "tbn_kv_fork", "tbn_kv_release", "tbn_kv_copy_pages", "tbn_kv_append", "tbn_kv_keep",
+                "tbn_tree_attention_workspace_bytes", "tbn_tree_attention", "tbn_block_select_workspace_bytes", "tbn_block_select",
+                "tbn_block_attention_workspace_bytes", "tbn_block_attention")})
             _host = _tbn_host
         except ImportError as e:   # not built, or built against another torch: the wrappers serve every call by themselves
             warnings.warn(f"_tbn_host cannot be loaded ({e}): calls take about 6 us more host time each")
