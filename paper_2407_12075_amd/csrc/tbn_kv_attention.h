@@ -50,6 +50,23 @@ template <> struct Elem<uint16_t> {
         for (int e = 0; e < 4; ++e) w[e] = ((bits >> (2 * e)) & 1u ? 0x3f80u : 0u) | ((bits >> (2 * e + 1)) & 1u ? 0x3f800000u : 0u);
         return w;
     }
+    // the first n values, 0 in place of the others
+    static __device__ __forceinline__ u32x4_t first_of(u32x4_t w, int n) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] &= n > 2 * e + 1 ? ~0u : n > 2 * e ? 0xffffu : 0u;
+        return w;
+    }
+    static __device__ __forceinline__ bool not_finite(u32x4_t w) {
+        bool is = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) is |= (w[e] & 0x7f80u) == 0x7f80u || (w[e] & 0x7f800000u) == 0x7f800000u;
+        return is;
+    }
+    static __device__ __forceinline__ u32x4_t finite_of(u32x4_t w) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] &= ((w[e] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | ((w[e] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u);
+        return w;
+    }
     // values with 0 for those that are not finite, and the kinds of those (limit_of)
     static __device__ __forceinline__ void part(u32x4_t w, u32x4_t &finite, u32x4_t &kinds) {
 #pragma unroll
@@ -78,6 +95,22 @@ template <> struct Elem<float> {
         u32x4_t w;
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] = (bits >> e) & 1u ? 0x3f800000u : 0u;
+        return w;
+    }
+    static __device__ __forceinline__ u32x4_t first_of(u32x4_t w, int n) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = n > e ? w[e] : 0u;
+        return w;
+    }
+    static __device__ __forceinline__ bool not_finite(u32x4_t w) {
+        bool is = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) is |= (w[e] & 0x7f800000u) == 0x7f800000u;
+        return is;
+    }
+    static __device__ __forceinline__ u32x4_t finite_of(u32x4_t w) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = (w[e] & 0x7f800000u) == 0x7f800000u ? 0u : w[e];
         return w;
     }
     static __device__ __forceinline__ void part(u32x4_t w, u32x4_t &finite, u32x4_t &kinds) {

@@ -34,10 +34,10 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
     using E = Elem<T>;
     constexpr int KS = E::kStep, OF = E::kOf, NF = DP / 16, NQ = NF / E::kTiles;
     __shared__ int2 listed[kListed];   // slot and page
-    __shared__ float sums[kAttnWaves][16][DP + 4];
+    __shared__ float sums[RT][kAttnWaves][16][DP + 4];
     __shared__ float maxima[kAttnWaves][16], totals[2][kAttnWaves][16];
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     const int s = blockIdx.y, H = a.q.heads, KV = a.p.kv_heads, G = H / KV, D = EVEN ? DP : a.p.dim, P = a.p.page;
     const int shift = __ffs(P) - 1;
     const Span v = span_of(a, s);
@@ -76,17 +76,19 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
     int place[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        const int row = base + r * 16 + n;
-        const int t = PICKED ? only : min(row, R - 1) / G;
+        const int row = base + r * 16 + n, in = min(row, R - 1), t = PICKED ? only : in / G;
         place[r] = t;
-        const T *src = static_cast<const T *>(a.q.q) + (v.t0 + t) * a.q.q_stride + (head * G + (PICKED ? row : row - t * G)) * D;
+        const T *src = static_cast<const T *>(a.q.q) + (v.t0 + t) * a.q.q_stride + (head * G + (PICKED ? in : in - t * G)) * D;
+        // always loaded, so that the loads do not wait for each other
 #pragma unroll
         for (int f = 0; f < NQ; ++f) {
             const int d = f * (4 * OF) + OF * g;
-            u32x4_t w = {0, 0, 0, 0};
-            if (row < R && (EVEN || d < D)) w = *reinterpret_cast<const typename E::u32x4_any *>(src + d) ^ a.flip;
-            q[r][f] = w;
+            q[r][f] = *reinterpret_cast<const typename E::u32x4_any *>(src + (EVEN ? d : min(d, D - OF)));
         }
+#pragma unroll
+        for (int f = 0; f < NQ; ++f)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) q[r][f][e] = row < R && (EVEN || f * (4 * OF) + OF * g < D) ? q[r][f][e] ^ a.flip : 0u;
     }
 
     f32x4_t o[RT][NF];
@@ -145,6 +147,14 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
         return i;
     };
 
+    bool any_odd = false;   // of this wave
+    auto clear_limits = [&] {
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll 1
+            for (int f = 0; f < NF; ++f) *reinterpret_cast<f32x4_t *>(&sums[r][wave][n][f * 16 + 4 * g]) = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    };
+
     __syncthreads();
     u32x4_t k[NF], w[NF];
     int key = 0, page = 0;
@@ -195,20 +205,10 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
             // values behind the last key count as 0; are the others finite?
             bool found = false;
 #pragma unroll
-            for (int f = 0; f < NF; ++f)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    uint32_t x = w[f][e];
-                    if constexpr (OF == 8) {
-                        if (k0 + 2 * e + 1 >= end) x &= 0xffffu;
-                        if (k0 + 2 * e >= end) x = 0;
-                        found |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
-                    } else {
-                        if (k0 + e >= end) x = 0;
-                        found |= (x & 0x7f800000u) == 0x7f800000u;
-                    }
-                    w[f][e] = x;
-                }
+            for (int f = 0; f < NF; ++f) {
+                w[f] = E::first_of(w[f], end - k0);
+                found |= E::not_finite(w[f]);
+            }
             odd = __any(found);
         }
 
@@ -246,26 +246,31 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
                     pw[r][e] = __float_as_uint(p[r][e]);
                 }
             }
-        if (!odd) {
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int f = 0; f < NF; ++f) o[r][f] = E::mma(w[f], pw[r], o[r][f]);
-        } else {
-#pragma unroll
-            for (int f = 0; f < NF; ++f) {
-                u32x4_t finite, kinds;
-                E::part(w[f], finite, kinds);
+        if (odd) {   // rare: what such values add to the rows that see them goes to LDS until the end, and 0 in their place
+            if (!any_odd) clear_limits();
+            any_odd = true;
+            const T *src = vp + int64_t(page) * (page_elems * KV) + (key & (P - 1)) + OF * g;
+#pragma unroll 1
+            for (int f = 0; f < NF; ++f) {   // loaded again: a loop that is not unrolled costs the others no registers
+                const int d = f * 16 + n;
+                u32x4_t x = {0, 0, 0, 0}, finite, kinds;
+                if (EVEN || d < D) x = E::first_of(*reinterpret_cast<const u32x4_t *>(src + d * P), end - key - OF * g);
+                E::part(x, finite, kinds);
 #pragma unroll
                 for (int r = 0; r < RT; ++r) {
                     const f32x4_t counts = E::mma(kinds, E::ones(seen[r]), f32x4_t{0.f, 0.f, 0.f, 0.f});
-                    o[r][f] = E::mma(finite, pw[r], o[r][f]);
+                    float *limit = &sums[r][wave][n][f * 16 + 4 * g];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[r][f][e] += limit_of(counts[e]);
+                    for (int e = 0; e < 4; ++e) limit[e] += limit_of(counts[e]);
                 }
-                __builtin_amdgcn_sched_barrier(0);   // rare: one piece after another, so that it costs the loop no registers
             }
+#pragma unroll
+            for (int f = 0; f < NF; ++f) w[f] = E::finite_of(w[f]);
         }
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int f = 0; f < NF; ++f) o[r][f] = E::mma(w[f], pw[r], o[r][f]);
         if (next < steps) load_v(w, next_page, next_key & (P - 1));
         i = next;
         key = next_key;
@@ -292,7 +297,11 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
         for (int u = 1; u < kAttnWaves; ++u) top = fmaxf(top, maxima[u][n]);
         const float f0 = top == -INFINITY ? 0.f : exp2_of(m[r] - top);
 #pragma unroll
-        for (int f = 0; f < NF; ++f) *reinterpret_cast<f32x4_t *>(&sums[wave][n][f * 16 + 4 * g]) = o[r][f] * f0;
+        for (int f = 0; f < NF; ++f) {
+            f32x4_t *at = reinterpret_cast<f32x4_t *>(&sums[r][wave][n][f * 16 + 4 * g]), sum = o[r][f] * f0;
+            if (any_odd) sum += *at;
+            *at = sum;
+        }
         __syncthreads();
         for (int j = tid; j < 16 * (DP / 4); j += kAttnThreads) {
             const int rr = j / (DP / 4), d = (j - rr * (DP / 4)) * 4, row = base + r * 16 + rr;
@@ -307,7 +316,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
                 const float f = best == -INFINITY ? 1.f : exp2_of(maxima[u][rr] - best);
                 lsum += totals[0][u][rr] * f;
                 zsum += totals[1][u][rr] * f;
-                sum += *reinterpret_cast<const f32x4_t *>(&sums[u][rr][d]);
+                sum += *reinterpret_cast<const f32x4_t *>(&sums[r][u][rr][d]);
             }
             const int t = PICKED ? only : row / G;
             const int64_t at = int64_t(v.t0 + t) * H + head * G + (PICKED ? row : row - t * G);
@@ -316,30 +325,34 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
     }
 }
 
-// Joins the parts of one row: a workgroup per token and head; D / 4 lanes (rounded up to a power of two) take a part at a time.
-template <typename T, bool PICKED>
+// Joins the parts of one row.  D / 4 lanes (rounded up to a power of two) take a part at a time.  WIDE: a workgroup per row, else a wave.
+template <typename T, bool PICKED, bool WIDE>
 __global__ __launch_bounds__(kAttnThreads) void kv_join_kernel(AttentionArgs a, int tile_rows) {
-    __shared__ f32x4_t sums[kAttnThreads];
+    constexpr int kTeam = WIDE ? kAttnThreads : kWave;
+    __shared__ f32x4_t sums[WIDE ? kAttnThreads : 1];
     __shared__ float maxima[kAttnWaves];
-    __shared__ float2 totals[kAttnThreads / 16];
-    const int s = blockIdx.y, H = a.q.heads, G = H / a.p.kv_heads, D = a.p.dim, tid = threadIdx.x;
-    const int t = blockIdx.x / H, h = blockIdx.x - t * H;
+    __shared__ float2 totals[WIDE ? kAttnThreads / 16 : 1];
+    const int s = blockIdx.y, H = a.q.heads, G = H / a.p.kv_heads, D = a.p.dim, tid = threadIdx.x % kTeam;
+    const int row = WIDE ? blockIdx.x : __builtin_amdgcn_readfirstlane(blockIdx.x * kAttnWaves + threadIdx.x / kWave);
+    const int t = row / H, h = row - t * H;
     const Span v = span_of(a, s);
     if (t >= v.T) return;
     int parts = a.n_chunks;
     if (!PICKED) {
-        const int row = t * G + h % G, last = min(row / tile_rows * tile_rows + tile_rows, v.T * G) - 1;
+        const int r = t * G + h % G, last = min(r / tile_rows * tile_rows + tile_rows, v.T * G) - 1;
         parts = max(1, (keys_end(a, v, last, G) + a.chunk - 1) / a.chunk);
     }
     const int64_t at = int64_t(v.t0 + t) * H + h, stride = a.q.total_q * H;
     float best = -INFINITY;
-    for (int c = tid; c < parts; c += kAttnThreads) best = fmaxf(best, a.part_ml[c * stride + at].x);
+    for (int c = tid; c < parts; c += kTeam) best = fmaxf(best, a.part_ml[c * stride + at].x);
 #pragma unroll
     for (int d = 1; d < kWave; d <<= 1) best = fmaxf(best, __shfl_xor(best, d));
-    if ((tid & 63) == 0) maxima[tid >> 6] = best;
-    __syncthreads();
-    best = fmaxf(fmaxf(maxima[0], maxima[1]), fmaxf(maxima[2], maxima[3]));
-    const int shift = D <= 64 ? 4 : D <= 128 ? 5 : 6, group = tid >> shift, groups = kAttnThreads >> shift, d = (tid & ((1 << shift) - 1)) * 4;
+    if constexpr (WIDE) {
+        if ((tid & 63) == 0) maxima[tid >> 6] = best;
+        __syncthreads();
+        best = fmaxf(fmaxf(maxima[0], maxima[1]), fmaxf(maxima[2], maxima[3]));
+    }
+    const int shift = D <= 64 ? 4 : D <= 128 ? 5 : 6, group = tid >> shift, groups = kTeam >> shift, d = (tid & ((1 << shift) - 1)) * 4;
     float l = 0.f, z = 0.f;
     f32x4_t o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
@@ -352,24 +365,44 @@ __global__ __launch_bounds__(kAttnThreads) void kv_join_kernel(AttentionArgs a, 
         l += ml.y * f;
         z += ml.z * f;
     }
-    sums[tid] = o;
-    if (d == 0) totals[group] = make_float2(l, z);
-    __syncthreads();
-    if (tid >= D) return;
-    const int lane = tid >> 2, e = tid & 3;
-    float sum = 0.f;
-    l = z = 0.f;
-    for (int g = 0; g < groups; ++g) {
-        sum += sums[(g << shift) + lane][e];
-        l += totals[g].x;
-        z += totals[g].y;
+    if constexpr (WIDE) {
+        sums[tid] = o;
+        if (d == 0) totals[group] = make_float2(l, z);
+        __syncthreads();
+        if (group > 0) return;
+        for (int g = 1; g < groups; ++g) {
+            o += sums[(g << shift) + tid];
+            l += totals[g].x;
+            z += totals[g].y;
+        }
+    } else {
+        for (int x = 1 << shift; x < kWave; x <<= 1) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], x);
+            l += __shfl_xor(l, x);
+            z += __shfl_xor(z, x);
+        }
+        if (group > 0) return;
     }
-    ElemIO<T>::store(static_cast<T *>(a.out) + at * D + tid, z == 0.f ? 0.f : sum / z);
+    if (d < D) {
+        const float inv = z == 0.f ? 0.f : 1.f / z;
+        T *out = static_cast<T *>(a.out) + at * D + d;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ElemIO<T>::store(out + e, o[e] * inv);
+    }
     if (tid == 0 && a.lse) a.lse[at] = l == 0.f ? -INFINITY : (best + log2f(l)) * kLn2;
 }
 
+template <typename T, bool PICKED>
+void launch_join(const AttentionArgs &a, int tile_rows, hipStream_t stream) {
+    const int64_t rows = int64_t(a.q.max_q) * a.q.heads;   // checked by the caller
+    // many parts of a row: a workgroup each; few: a wave each (13000 rows of at most 4 parts: 14 us with a workgroup each)
+    if (a.n_chunks > 16) hipLaunchKernelGGL((kv_join_kernel<T, PICKED, true>), dim3(static_cast<unsigned>(rows), a.ix.n_seqs), dim3(kAttnThreads), 0, stream, a, tile_rows);
+    else hipLaunchKernelGGL((kv_join_kernel<T, PICKED, false>), dim3(static_cast<unsigned>((rows + kAttnWaves - 1) / kAttnWaves), a.ix.n_seqs), dim3(kAttnThreads), 0, stream, a, tile_rows);
+}
+
 struct Plan {
-    int rows, chunk, n_chunks, row_tiles;   // rows of a workgroup: 16, 32 or 64 in this file's kernel, 64 or 128 in the one for many rows
+    int rows, chunk, n_chunks, row_tiles;   // rows of a workgroup: 16 (float32 up to 64) in this file's kernel, 64 or 128 in the one for many rows
     bool staged;                            // the latter
 };
 
@@ -377,13 +410,13 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 int padded_dim(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 
-// Rows of a workgroup of this file's kernel: what the registers hold of queries and sums.
-int most_rows(const tbn_kv_pool &p) { return padded_dim(p.dim) == 256 ? 16 : padded_dim(p.dim) == 128 ? 32 : 64; }
+// Rows of a workgroup of this file's kernel: what the registers hold of queries and sums.  (bfloat16: more rows go to the other kernel.)
+int most_rows(const tbn_kv_pool &p) { return p.dt == TBN_BF16 || padded_dim(p.dim) == 256 ? 16 : padded_dim(p.dim) == 128 ? 32 : 64; }
 
 Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, int64_t unit_step, int64_t unit_most, bool picked) {
     // units: keys or picks to split, unit_step: the least stretch, a multiple of which a chunk is
     Plan pl;
-    pl.staged = !picked && p.dt == TBN_BF16 && rows > 32;
+    pl.staged = !picked && p.dt == TBN_BF16 && rows > 16;
     if (pl.staged) {
         pl.rows = rows <= 64 ? 64 : 128;
     } else {
@@ -392,11 +425,15 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, 
     }
     pl.row_tiles = static_cast<int>(ceil_div(rows, pl.rows));
     const int64_t blocks = groups * pl.row_tiles;
-    // Workgroups to aim at.  The staged kernel has two per CU and is bound by the matrix cores: one round (64 drafted tokens on 131000
-    // keys: 184 - 202 us, with four rounds 227).  Here many small ones even out ragged lengths (64 sequences of 4096 - 16384 keys: 465 us;
-    // with 1024 workgroups 612, as long as the longest sequences run).
-    const int64_t want = ceil_div(pl.staged ? 512 : 8192, blocks);
-    int64_t chunk = ceil_div(ceil_div(units, want), unit_step) * unit_step;
+    // Stretches of keys.  The staged kernel has two workgroups per CU and is bound by the matrix cores: one round of them (64 drafted tokens
+    // on 131000 keys: 184 us, in four rounds 227).  Here many small ones even out ragged lengths (64 sequences of 4096 - 16384 keys: 465 us in
+    // 8192 stretches, 534 in 512), but not below 1024 keys while those make 2048 workgroups (16 sequences, 16 rows: 153 us, with 256 keys 167).
+    int64_t chunk = ceil_div(units, ceil_div(pl.staged ? 512 : 8192, blocks));
+    if (!picked && !pl.staged) {
+        const int64_t fill = ceil_div(units * blocks, 2048), least = fill < 1024 ? fill : 1024;
+        if (chunk < least) chunk = least;
+    }
+    chunk = ceil_div(chunk, unit_step) * unit_step;
     if (chunk > unit_most) chunk = unit_most;
     pl.chunk = static_cast<int>(chunk);
     pl.n_chunks = static_cast<int>(ceil_div(units, chunk));
@@ -424,11 +461,10 @@ void launch_even(const AttentionArgs &a, dim3 grid, hipStream_t stream) {
 
 template <typename T, int DP, bool PICKED>
 void launch_rows(const AttentionArgs &a, int rows, dim3 grid, hipStream_t stream) {
-    // many rows of bfloat16 go to the other kernel, unless they are a query's on picked blocks
-    if constexpr (DP <= 64 && (PICKED || sizeof(T) == 4)) {
+    if constexpr (sizeof(T) == 4 && DP <= 64) {
         if (rows == 64) return launch_even<T, DP, 4, PICKED>(a, grid, stream);
     }
-    if constexpr (DP <= 128) {
+    if constexpr (sizeof(T) == 4 && DP <= 128) {
         if (rows == 32) return launch_even<T, DP, 2, PICKED>(a, grid, stream);
     }
     launch_even<T, DP, 1, PICKED>(a, grid, stream);
@@ -462,13 +498,13 @@ tbn_status launch(AttentionArgs &a, const Plan &pl, float *ws, const char *what,
         set_error("%s: %lld workgroups per sequence are beyond one launch", what, (long long)(x > jx ? x : jx));
         return TBN_ERR_UNSUPPORTED;
     }
-    const dim3 grid(static_cast<unsigned>(x), a.ix.n_seqs), join(static_cast<unsigned>(jx), a.ix.n_seqs);
+    const dim3 grid(static_cast<unsigned>(x), a.ix.n_seqs);
     if (pl.staged) launch_kv_rows(a, pl.rows / 32, grid, stream);
     else if (a.p.dt == TBN_F32) launch_dims<float, PICKED>(a, pl.rows, grid, stream);
     else launch_dims<uint16_t, PICKED>(a, pl.rows, grid, stream);
     if (a.n_chunks > 1) {
-        if (a.p.dt == TBN_F32) hipLaunchKernelGGL((kv_join_kernel<float, PICKED>), join, dim3(kAttnThreads), 0, stream, a, pl.rows);
-        else hipLaunchKernelGGL((kv_join_kernel<uint16_t, PICKED>), join, dim3(kAttnThreads), 0, stream, a, pl.rows);
+        if (a.p.dt == TBN_F32) launch_join<float, PICKED>(a, pl.rows, stream);
+        else launch_join<uint16_t, PICKED>(a, pl.rows, stream);
     }
     return check_launch(what);
 }

@@ -60,17 +60,18 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
     const int32_t *table = a.ix.table + int64_t(s) * a.ix.max_pages + (first >> shift);
     for (int i = tid; i < entries; i += kAttnThreads) listed[i] = page_in(table[i], static_cast<int>(a.p.n_pages));
 
-    const int row = base + group * 32 + n, place = min(row, R - 1) / G;
-    const int64_t at = int64_t(v.t0 + place) * H + blk.head * G + (row - place * G);   // of the outputs, where row < R
+    const int row = base + group * 32 + n, in = min(row, R - 1), place = in / G;
+    const int64_t at = int64_t(v.t0 + place) * H + blk.head * G + (in - place * G);   // of the outputs, where row < R
     u32x4_t q[NQ];
     {
-        const uint16_t *src = static_cast<const uint16_t *>(a.q.q) + (v.t0 + place) * a.q.q_stride + (blk.head * G + row - place * G) * D;
+        const uint16_t *src = static_cast<const uint16_t *>(a.q.q) + (v.t0 + place) * a.q.q_stride + (blk.head * G + in - place * G) * D;
+        // always loaded, so that the loads do not wait for each other
 #pragma unroll
-        for (int f = 0; f < NQ; ++f) {
-            u32x4_t w = {0, 0, 0, 0};
-            if (row < R && (EVEN || f * 16 + 8 * h < D)) w = *reinterpret_cast<const Elem<uint16_t>::u32x4_any *>(src + f * 16 + 8 * h) ^ a.flip;
-            q[f] = w;
-        }
+        for (int f = 0; f < NQ; ++f) q[f] = *reinterpret_cast<const Elem<uint16_t>::u32x4_any *>(src + (EVEN ? f * 16 + 8 * h : min(f * 16 + 8 * h, D - 8)));
+#pragma unroll
+        for (int f = 0; f < NQ; ++f)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) q[f][e] = row < R && (EVEN || f * 16 + 8 * h < D) ? q[f][e] ^ a.flip : 0u;
     }
 
     // where this lane's pieces come from: offsets within a page in bytes, relative to the step's first key
@@ -175,15 +176,8 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
             for (int L = tid; L < DP * VP; L += kAttnThreads) {
                 const int d = L / VP, there = stop - (key + ((L % VP) ^ v_swap(d)) * 8);
                 u32x4_t *at_piece = reinterpret_cast<u32x4_t *>(vt + L * 8);
-                u32x4_t w = *at_piece;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    uint32_t x = w[e];
-                    if (2 * e + 1 >= there) x &= 0xffffu;
-                    if (2 * e >= there) x = 0;
-                    odd |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
-                    w[e] = x;
-                }
+                const u32x4_t w = Elem<uint16_t>::first_of(*at_piece, there);
+                odd |= Elem<uint16_t>::not_finite(w);
                 if (there < 8) *at_piece = w;
             }
             if (__syncthreads_or(odd)) {   // rare: what they add to the rows that see them, then 0 in their place
@@ -208,9 +202,8 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
                 __syncthreads();
 #pragma unroll 1
                 for (int L = tid; L < DP * VP; L += kAttnThreads) {
-                    u32x4_t *at_piece = reinterpret_cast<u32x4_t *>(vt + L * 8), finite, kinds;
-                    Elem<uint16_t>::part(*at_piece, finite, kinds);
-                    *at_piece = finite;
+                    u32x4_t *at_piece = reinterpret_cast<u32x4_t *>(vt + L * 8);
+                    *at_piece = Elem<uint16_t>::finite_of(*at_piece);
                 }
                 __syncthreads();
             }
