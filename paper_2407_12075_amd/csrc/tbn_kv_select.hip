@@ -8,8 +8,10 @@
 //
 // A record of 2 dim bytes is read by as many lanes as it has 16-byte pieces (rounded up to a power of two); a lane keeps
 // its piece of the pooled query in registers.  The k-th largest score is found by counting: the range of the scores is
-// cut into 256 bins, the bin that holds the k-th becomes the range, at most four times; then one pass writes the blocks
-// above it and the first of those equal to it, in ascending order.
+// cut into 256 bins, the bin that holds the k-th becomes the range, at most four times and until it holds only scores that
+// are taken; then one pass writes the blocks above it and the first of those equal to it, in ascending order.  The scores
+// stay in registers, ranks come from ballots and sums over lanes from data-parallel moves: what costs time here are the
+// barriers (one per cut).
 //
 // One workgroup per query and kv head does all of it while there are enough of those to fill the GPU or few blocks;
 // otherwise the scores are made by workgroups of 64 blocks and pass through the workspace.
@@ -23,7 +25,7 @@ typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 constexpr int kWavesOf = kThreads / kWave;
-constexpr int kInLds = 16384;     // scores of one query and kv head that are kept in LDS
+constexpr int kInLds = 16384;     // scores of one query and kv head that a workgroup keeps (64 of a thread)
 constexpr int kSliced = 64;       // blocks of a workgroup that only scores
 
 struct SelectArgs {
@@ -47,25 +49,60 @@ __device__ __forceinline__ uint32_t ordered(float f) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// Sums and maxima over the lanes of a wave by data-parallel primitives: a step costs a few cycles, an exchange through LDS a hundred.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t from_lane(uint32_t v) {   // 0 where no lane is read
+    return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ uint32_t prefix_of_lanes(uint32_t v) {   // inclusive
+    v += from_lane<0x111, 0xf>(v);   // one, two, four, eight lanes up within rows of 16
+    v += from_lane<0x112, 0xf>(v);
+    v += from_lane<0x114, 0xf>(v);
+    v += from_lane<0x118, 0xf>(v);
+    v += from_lane<0x142, 0xa>(v);   // a row's last lane to the next row, the second row's to the upper half
+    v += from_lane<0x143, 0xc>(v);
+    return v;
+}
+__device__ __forceinline__ uint32_t most_of_lanes(uint32_t v) {   // in lane 63, for all
+    v = max(v, from_lane<0x111, 0xf>(v));
+    v = max(v, from_lane<0x112, 0xf>(v));
+    v = max(v, from_lane<0x114, 0xf>(v));
+    v = max(v, from_lane<0x118, 0xf>(v));
+    v = max(v, from_lane<0x142, 0xa>(v));
+    v = max(v, from_lane<0x143, 0xc>(v));
+    return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), 63));
+}
+
 // The pooled query of token `tok` and a kv head, in LDS.  Ends with a barrier.
 template <typename T>
 __device__ void pool_query(const SelectArgs &a, int64_t tok, int head, Pooled &l) {
     const int tid = threadIdx.x, D = a.p.dim, G = a.q.heads / a.p.kv_heads;
     const T *q = static_cast<const T *>(a.q.q) + tok * a.q.q_stride + int64_t(head) * G * D + tid;
-    float most = 0.f;
-    if (tid < D)
-        for (int g = 0; g < G; ++g) {
+    constexpr int kFirst = 8;   // heads that are kept between the two passes
+    float kept[kFirst], most = 0.f;
+    if (tid < D) {
+#pragma unroll
+        for (int g = 0; g < kFirst; ++g) kept[g] = g < G ? ElemIO<T>::load(q + g * D) : 0.f;
+#pragma unroll
+        for (int g = 0; g < kFirst; ++g) most = fabsf(kept[g]) < INFINITY ? fmaxf(most, fabsf(kept[g])) : most;
+        for (int g = kFirst; g < G; ++g) {
             const float f = fabsf(ElemIO<T>::load(q + g * D));
             most = f < INFINITY ? fmaxf(most, f) : most;
         }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
-    if ((tid & 63) == 0) l.most[tid >> 6] = most;
+    }
+    const uint32_t top = most_of_lanes(__float_as_uint(most));   // magnitudes order as their bits
+    if ((tid & 63) == 0) l.most[tid >> 6] = __uint_as_float(top);
     __syncthreads();
     const float up = pow2_of(6 - exponent_of(fmaxf(fmaxf(l.most[0], l.most[1]), fmaxf(l.most[2], l.most[3]))));
     if (tid < D) {
         int pos = 0, neg = 0;
-        for (int g = 0; g < G; ++g) {
+#pragma unroll
+        for (int g = 0; g < kFirst; ++g) {
+            const int c = fabsf(kept[g]) < INFINITY ? static_cast<int>(rintf(kept[g] * up)) : 0;
+            pos += max(c, 0);
+            neg += min(c, 0);
+        }
+        for (int g = kFirst; g < G; ++g) {
             const float f = ElemIO<T>::load(q + g * D);
             const int c = fabsf(f) < INFINITY ? static_cast<int>(rintf(f * up)) : 0;
             pos += max(c, 0);
@@ -165,42 +202,18 @@ __global__ __launch_bounds__(kThreads) void kv_score_kernel(SelectArgs a) {
 }
 
 struct SelectLds {
-    uint32_t bins[kThreads];
+    uint32_t bins[3][kThreads];   // one that is filled, one that may still be read, one that is cleared for the next turn
     uint32_t least[kWavesOf], most[kWavesOf];
-    uint32_t part[2][kWavesOf];
-    uint32_t bin, above;
-    bool all;
+    uint2 counts[64 * kWavesOf];   // of a round's words in a wave: larger ones, equal ones
 };
 
-// inclusive prefix over the workgroup's threads; ends with the totals of the waves read by everyone
-__device__ __forceinline__ uint32_t prefix(uint32_t v, uint32_t *part, uint32_t &total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint32_t sum = v;
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-        const uint32_t o = __shfl_up(sum, d);
-        if (lane >= d) sum += o;
-    }
-    __syncthreads();
-    if (lane == 63) part[wave] = sum;
-    __syncthreads();
-    uint32_t before = 0;
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < kWavesOf; ++w) {
-        before += w < wave ? part[w] : 0u;
-        total += part[w];
-    }
-    return before + sum;
-}
-
-// SCORED: the scores are in a.scores; IN_LDS: they are (or come) into LDS.
-template <typename T, bool SCORED, bool IN_LDS>
+// SCORED: the scores are in a.scores.  NW: words of a thread, kept in registers; 0: any number, read again each time (SCORED only).
+template <typename T, bool SCORED, int NW>
 __global__ __launch_bounds__(kThreads) void kv_select_kernel(SelectArgs a) {
-    extern __shared__ uint32_t kept[];
+    extern __shared__ uint32_t made[];
     __shared__ Pooled pooled;
     __shared__ SelectLds l;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, head = blockIdx.y;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), head = blockIdx.y;
     const Query r = query_of(a, blockIdx.z, blockIdx.x);
     if (!r.there) return;
     const int64_t row = r.tok * a.p.kv_heads + head;
@@ -214,27 +227,37 @@ __global__ __launch_bounds__(kThreads) void kv_select_kernel(SelectArgs a) {
     for (int i = tid; i < a.n_sink; i += kThreads) picks[i] = i;
     for (int i = tid; i < a.n_recent; i += kThreads) picks[a.n_select - a.n_recent + i] = r.hi + i;
     if (k == 0) return;
-    const uint32_t *scored = SCORED ? a.scores + row * a.blocks + r.lo : nullptr;
+    l.bins[0][tid] = 0;
+    const uint32_t *words = SCORED ? a.scores + row * a.blocks + r.lo : made;
     if constexpr (!SCORED) {
         pool_query<T>(a, r.tok, head, pooled);
-        score_blocks(a, r.table, head, r.lo, r.hi, pooled, [&](int b, uint32_t word) { kept[b - r.lo] = word; });
-        __syncthreads();
-    } else if constexpr (IN_LDS) {
-        for (int i = tid; i < n; i += kThreads) kept[i] = scored[i];
+        score_blocks(a, r.table, head, r.lo, r.hi, pooled, [&](int b, uint32_t word) { made[b - r.lo] = word; });
         __syncthreads();
     }
-    const uint32_t *words = IN_LDS ? kept : scored;
+    // a thread's words are kThreads apart; 0 (less than any score's word) behind the last one
+    uint32_t kept[NW > 0 ? NW : 1];
+    if constexpr (NW > 0) {
+#pragma unroll
+        for (int j = 0; j < NW; ++j) kept[j] = j * kThreads + tid < n ? words[j * kThreads + tid] : 0u;
+    }
+    const int rounds = (n + kThreads - 1) / kThreads;
+    auto each = [&](auto use) __attribute__((always_inline)) {   // use(round, word)
+        if constexpr (NW > 0) {
+#pragma unroll
+            for (int j = 0; j < NW; ++j)
+                if (NW <= 4 || j < rounds) use(j, kept[j]);
+        } else {
+            for (int j = 0; j < rounds; ++j) use(j, j * kThreads + tid < n ? words[j * kThreads + tid] : 0u);
+        }
+    };
 
     uint32_t least = 0xffffffffu, most = 0;
-    for (int i = tid; i < n; i += kThreads) {
-        least = min(least, words[i]);
-        most = max(most, words[i]);
-    }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) {
-        least = min(least, static_cast<uint32_t>(__shfl_xor(static_cast<int>(least), d)));
-        most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), d)));
-    }
+    each([&](int, uint32_t w) {
+        least = min(least, w ? w : 0xffffffffu);
+        most = max(most, w);
+    });
+    least = ~most_of_lanes(~least);
+    most = most_of_lanes(most);
     if (lane == 0) {
         l.least[wave] = least;
         l.most[wave] = most;
@@ -245,49 +268,82 @@ __global__ __launch_bounds__(kThreads) void kv_select_kernel(SelectArgs a) {
         least = min(least, l.least[w]);
         most = max(most, l.most[w]);
     }
+    least = __builtin_amdgcn_readfirstlane(least);
+    most = __builtin_amdgcn_readfirstlane(most);
     uint32_t above = 0;   // words beyond `most`
-    while (least < most) {   // the k-th largest word is in [least, most]
+    for (int turn = 0; least < most; turn = turn == 2 ? 0 : turn + 1) {   // the k-th largest word is in [least, most]
         const int cut = max(24 - __clz(most - least), 0);   // (most - least) >> cut is below 256
-        l.bins[tid] = 0;
+        l.bins[turn == 2 ? 0 : turn + 1][tid] = 0;
+        each([&](int, uint32_t w) {
+            if (w >= least && w <= most) atomicAdd(&l.bins[turn][(w - least) >> cut], 1u);
+        });
         __syncthreads();
-        for (int i = tid; i < n; i += kThreads) {
-            const uint32_t w = words[i];
-            if (w >= least && w <= most) atomicAdd(&l.bins[(w - least) >> cut], 1u);
-        }
-        __syncthreads();
-        const uint32_t here = l.bins[kThreads - 1 - tid];   // thread 0 has the highest bin
-        uint32_t total;
-        const uint32_t upto = above + prefix(here, l.part[0], total);
-        if (upto >= k && upto - here < k) {   // exactly one thread
-            l.bin = kThreads - 1 - tid;
-            l.above = upto - here;
-            l.all = upto == k;
-        }
-        __syncthreads();
-        above = l.above;
-        least += l.bin << cut;
+        // every wave finds the bin by itself: lane 0 has the four highest ones
+        const uint4 b = *reinterpret_cast<const uint4 *>(&l.bins[turn][(kWave - 1 - lane) * 4]);
+        const uint32_t here = b.x + b.y + b.z + b.w, upto = above + prefix_of_lanes(here);
+        const int at = __ffsll(static_cast<long long>(__ballot(upto >= k))) - 1;   // the first lane that reaches k
+        uint32_t sum = __builtin_amdgcn_readlane(upto - here, at);
+        const uint32_t four[4] = {static_cast<uint32_t>(__builtin_amdgcn_readlane(b.w, at)), static_cast<uint32_t>(__builtin_amdgcn_readlane(b.z, at)),
+                                  static_cast<uint32_t>(__builtin_amdgcn_readlane(b.y, at)), static_cast<uint32_t>(__builtin_amdgcn_readlane(b.x, at))};
+        int bin = (kWave - 1 - at) * 4 + 3, inside = four[0];
+#pragma unroll
+        for (int j = 1; j < 4; ++j)
+            if (sum + inside < k) {
+                sum += inside;
+                inside = four[j];
+                --bin;
+            }
+        above = sum;
+        least += static_cast<uint32_t>(bin) << cut;
         most = most - least < (1u << cut) ? most : least + ((1u << cut) - 1u);
-        if (l.all) {   // the whole bin is taken: everything beyond the word in front of it (scores' words are above 0)
+        if (sum + inside == k) {   // the whole bin is taken: everything beyond the word in front of it (scores' words are above 0)
             most = --least;
             above = k;
         }
-        __syncthreads();
     }
     // `least` is the k-th largest word; k - above of those equal to it are taken, the lowest blocks first
-    const int per = (n + kThreads - 1) / kThreads, i0 = min(tid * per, n), i1 = min(i0 + per, n);
-    uint32_t more = 0, same = 0;
-    for (int i = i0; i < i1; ++i) {
-        more += words[i] > least;
-        same += words[i] == least;
-    }
-    uint32_t total;
-    uint32_t more_at = prefix(more, l.part[0], total) - more, same_at = prefix(same, l.part[1], total) - same;
     const uint32_t take = k - above;
-    for (int i = i0; i < i1; ++i) {
-        const uint32_t w = words[i];
-        if (w > least || (w == least && same_at < take)) picks[a.n_sink + more_at + min(same_at, take)] = r.lo + i;
-        more_at += w > least;
-        same_at += w == least;
+    auto write = [&](int j, uint32_t w, uint32_t more_before, uint32_t same_before) {
+        const uint64_t more = __ballot(w > least), same = __ballot(w == least), below = (uint64_t(1) << lane) - 1;
+        const uint32_t more_at = more_before + __popcll(more & below), same_at = same_before + __popcll(same & below);
+        if (w > least || (w == least && same_at < take)) picks[a.n_sink + more_at + min(same_at, take)] = r.lo + j * kThreads + tid;
+    };
+    if constexpr (NW > 0) {
+        each([&](int j, uint32_t w) {
+            const uint64_t more = __ballot(w > least), same = __ballot(w == least);
+            if (lane == 0) l.counts[j * kWavesOf + wave] = make_uint2(__popcll(more), __popcll(same));
+        });
+        __syncthreads();
+        uint32_t more = 0, same = 0;
+        each([&](int j, uint32_t w) {
+            uint32_t more_at = more, same_at = same;
+#pragma unroll
+            for (int u = 0; u < kWavesOf; ++u) {
+                const uint2 c = l.counts[j * kWavesOf + u];
+                if (u < wave) more_at += c.x, same_at += c.y;
+                more += c.x;
+                same += c.y;
+            }
+            write(j, w, more_at, same_at);
+        });
+    } else {
+        uint32_t more = 0, same = 0;
+        for (int j = 0; j < rounds; ++j) {
+            const uint32_t w = j * kThreads + tid < n ? words[j * kThreads + tid] : 0u;
+            const uint64_t m = __ballot(w > least), e = __ballot(w == least);
+            uint2 *counts = l.counts + (j & 1) * kWavesOf;   // the round before last has been read by everyone
+            if (lane == 0) counts[wave] = make_uint2(__popcll(m), __popcll(e));
+            __syncthreads();
+            uint32_t more_at = more, same_at = same;
+#pragma unroll
+            for (int u = 0; u < kWavesOf; ++u) {
+                const uint2 c = counts[u];
+                if (u < wave) more_at += c.x, same_at += c.y;
+                more += c.x;
+                same += c.y;
+            }
+            write(j, w, more_at, same_at);
+        }
     }
 }
 
@@ -299,29 +355,35 @@ bool sliced(const tbn_kv_pool &p, const KvQueries &q, int64_t blocks) {
 
 int64_t blocks_of(const tbn_kv_pool &p, const KvQueries &q) { return (q.max_len + p.page - 1) / p.page; }
 
+template <typename T, bool SCORED>
+void launch_select_kernel(const SelectArgs &a, hipStream_t stream) {
+    const dim3 grid(a.q.max_q, a.p.kv_heads, a.ix.n_seqs), block(kThreads);
+    const unsigned lds = SCORED ? 0u : 4u * a.blocks;
+    if (a.blocks <= 4 * kThreads) hipLaunchKernelGGL((kv_select_kernel<T, SCORED, 4>), grid, block, lds, stream, a);
+    else if (a.blocks <= 16 * kThreads) hipLaunchKernelGGL((kv_select_kernel<T, SCORED, 16>), grid, block, lds, stream, a);
+    else if (!SCORED || a.blocks <= kInLds) hipLaunchKernelGGL((kv_select_kernel<T, SCORED, 64>), grid, block, lds, stream, a);
+    else hipLaunchKernelGGL((kv_select_kernel<T, true, 0>), grid, block, lds, stream, a);
+}
+
 template <typename T>
 tbn_status launch_select_typed(const SelectArgs &a, bool split, hipStream_t stream) {
-    const dim3 grid(a.q.max_q, a.p.kv_heads, a.ix.n_seqs), block(kThreads);
-    const unsigned lds = a.blocks <= kInLds ? 4u * a.blocks : 0u;
     if (split) {
         const int64_t slices = (a.blocks + kSliced - 1) / kSliced;
         if (slices * a.q.max_q > 0x7fffffffLL) {
             set_error("tbn_block_select: %d queries of %lld slices are beyond one launch", a.q.max_q, (long long)slices);
             return TBN_ERR_UNSUPPORTED;
         }
-        hipLaunchKernelGGL((kv_score_kernel<T>), dim3(static_cast<unsigned>(slices * a.q.max_q), a.p.kv_heads, a.ix.n_seqs), block, 0, stream, a);
-        if (lds) hipLaunchKernelGGL((kv_select_kernel<T, true, true>), grid, block, lds, stream, a);
-        else hipLaunchKernelGGL((kv_select_kernel<T, true, false>), grid, block, 0, stream, a);
+        hipLaunchKernelGGL((kv_score_kernel<T>), dim3(static_cast<unsigned>(slices * a.q.max_q), a.p.kv_heads, a.ix.n_seqs), dim3(kThreads), 0, stream, a);
+        launch_select_kernel<T, true>(a, stream);
     } else {
-        hipLaunchKernelGGL((kv_select_kernel<T, false, true>), grid, block, lds, stream, a);
+        launch_select_kernel<T, false>(a, stream);
     }
     return check_launch("tbn_block_select");
 }
 
 template <typename T>
-hipError_t allow_lds() {   // 64 KiB of scores and the static arrays
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&kv_select_kernel<T, true, true>), hipFuncAttributeMaxDynamicSharedMemorySize, 4 * kInLds);
-    return e != hipSuccess ? e : hipFuncSetAttribute(reinterpret_cast<const void *>(&kv_select_kernel<T, false, true>), hipFuncAttributeMaxDynamicSharedMemorySize, 4 * kInLds);
+hipError_t allow_lds() {   // up to 64 KiB of scores beside the static arrays
+    return hipFuncSetAttribute(reinterpret_cast<const void *>(&kv_select_kernel<T, false, 64>), hipFuncAttributeMaxDynamicSharedMemorySize, 4 * kInLds);
 }
 
 }  // namespace
