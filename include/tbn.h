@@ -495,8 +495,8 @@ tbn_status tbn_block_select(const void *q, int64_t q_stride, int32_t *picks, con
 
 /*
  * Attention over picked blocks: as tbn_tree_attention without a mask, over the keys of the blocks picks[i][h / G][..] up
- * to the query's own key.  Entries below 0 or behind the query's own block are passed over (an entry named twice counts
- * twice).
+ * to the query's own key.  Entries below 0 or behind the query's own block are passed over; no block may be named twice
+ * for one query and kv head.
  *   picks : DEVICE, total_q x kv_heads x n_select (1 .. 4096)
  */
 size_t tbn_block_attention_workspace_bytes(const tbn_kv_pool *pool, const tbn_kv_index *index, int64_t total_q, int32_t max_q,

@@ -227,6 +227,9 @@ __device__ __forceinline__ void store_sums(const AttentionArgs &a, int chunk, in
     }
 }
 
+// picked blocks, bfloat16: queries that share a workgroup (0: none), 32 rows at most
+int picked_queries(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, int32_t n_select);
+void launch_kv_picked(const AttentionArgs &a, int queries, dim3 grid, hipStream_t stream);
 // many rows, bfloat16: `tiles` (2 or 4) of 32 rows per workgroup
 void launch_kv_rows(const AttentionArgs &a, int tiles, dim3 grid, hipStream_t stream);
 

@@ -519,13 +519,19 @@ tbn_status launch_tree_attention(const tbn_kv_pool &p, const tbn_kv_index &ix, c
     return launch<false>(a, tree_plan(p, ix, q), ws, "tbn_tree_attention", stream);
 }
 
-size_t block_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &, const KvQueries &q, int32_t n_select) {
-    return workspace_of(p, q, picked_plan(p, q, n_select));
+size_t block_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, int32_t n_select) {
+    return picked_queries(p, ix, q, n_select) ? 0 : workspace_of(p, q, picked_plan(p, q, n_select));
 }
 
 tbn_status launch_block_attention(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, void *out, float *lse, const int32_t *picks,
                                   int32_t n_select, float scale, float *ws, hipStream_t stream) {
     AttentionArgs a{p, ix, q, out, lse, nullptr, 0, picks, n_select, factor_of(scale), flip_of(p, scale)};
+    if (const int queries = picked_queries(p, ix, q, n_select)) {
+        a.n_chunks = 1;
+        a.row_tiles = static_cast<int>(ceil_div(q.max_q, queries));
+        launch_kv_picked(a, queries, dim3(static_cast<unsigned>(a.row_tiles * p.kv_heads), ix.n_seqs), stream);   // at most 2^30 / 2 * 1024 / 32
+        return check_launch("tbn_block_attention");
+    }
     return launch<true>(a, picked_plan(p, q, n_select), ws, "tbn_block_attention", stream);
 }
 

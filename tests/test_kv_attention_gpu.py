@@ -381,6 +381,59 @@ def test_many_queries_of_a_prompt(kv, dt):
     compare(out, lse, *block_reference(qs, keys, values, [100, 37], want, P, 0.125), tolerance(dt, values))
 
 
+@pytest.mark.parametrize("H,KV,D,P,seqs,n", [
+    (32, 8, 128, 64, [(900, 40), (64, 3), (0, 70), (1, 0)], 5), (8, 8, 64, 128, [(1500, 33), (127, 130)], 4), (20, 4, 80, 64, [(700, 100), (63, 2)], 6),
+    (6, 3, 96, 64, [(640, 130)], 3), (64, 4, 128, 64, [(500, 40)], 4), (8, 2, 256, 64, [(800, 300)], 5), (4, 1, 128, 128, [(5000, 300)], 120)])
+def test_queries_that_share_a_workgroup(kv, H, KV, D, P, seqs, n):
+    """Neighbouring queries go through the union of their picks: any picks, some of them outside, none at all."""
+    rng = np.random.RandomState(n + D)
+    counts = [c for _, c in seqs]
+    pool, index, keys, values = make_cache(kv, "bf16", KV, D, P, [p + c for p, c in seqs], seed=D, extra_pages=4)
+    q, cu, qs = make_queries("bf16", counts, H, D, stride=H * D + 8)
+    picks = np.full((sum(counts), KV, n), -1, np.int32)
+    at = 0
+    for p, c in seqs:
+        for t in range(c):
+            blocks = (p + t) // P + 1
+            for h in range(KV):
+                m = rng.randint(0, min(n, blocks + 2) + 1)
+                picks[at, h, :m] = np.sort(rng.permutation(blocks + 2)[:m])   # the last two lie behind the query's own
+                if rng.rand() < 0.8 and m:
+                    picks[at, h, m - 1] = blocks - 1 if blocks - 1 not in picks[at, h, :m] else picks[at, h, m - 1]
+            at += 1
+    out, lse = kv.tbn_block_attention(q, pool, index, cu, max(counts), torch.from_numpy(picks).cuda())
+    ref = block_reference(qs, keys, values, counts, picks, P, 1 / math.sqrt(D))
+    compare(out, lse, *ref, tolerance("bf16", values))
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_queries_that_share_a_workgroup_keep_odd_values_apart(kv, bad):
+    """A page with such values is seen by the queries that picked it and by no other of the same workgroup."""
+    H, KV, D, P, prefix, n = 32, 8, 128, 64, 400, 70
+    pool, index, keys, values = make_cache(kv, "bf16", KV, D, P, [prefix + n], seed=2)
+    table = index.table.cpu().numpy()[0]
+    for key, d in ((70, 3), (200, 127), (prefix + 20, 64), (prefix + 69, 0)):
+        values[0][key, :, d] = bad
+        pool.v[int(table[key // P]), :, d, key % P] = bad
+    for key, d in ((140, 9),):   # a key of a page that few pick
+        keys[0][key, :, d] = bad
+        pool.k[int(table[key // P]), :, key % P, d] = bad
+    q, cu, qs = make_queries("bf16", [n], H, D)
+    if math.isinf(bad):
+        qs[:, :, 9] = -np.sign(bad) * (np.abs(qs[:, :, 9]) + 0.01)   # -infinity: a weight of 0
+        qs = torch.from_numpy(qs).to(q.dtype).double().numpy()
+        q.copy_(torch.from_numpy(qs))
+    rng = np.random.RandomState(4)
+    picks = np.full((n, KV, 4), -1, np.int32)
+    for t in range(n):
+        for h in range(KV):
+            m = rng.randint(1, 5)
+            picks[t, h, :m] = np.sort(rng.permutation((prefix + t) // P + 1)[:m])
+    ref = block_reference(qs, keys, values, [n], picks, P, 1 / math.sqrt(D))
+    assert not np.isfinite(ref[0]).all() and np.isfinite(ref[0]).any()
+    compare(*kv.tbn_block_attention(q, pool, index, cu, n, torch.from_numpy(picks).cuda()), *ref, tolerance("bf16", values))
+
+
 def test_streams_workspaces_and_graphs(kv):
     """The caller's stream, the caller's workspace, the calls of a step in a graph that is replayed with other queries."""
     H, KV, D, P = 8, 2, 64, 32
