@@ -73,6 +73,20 @@ __device__ __forceinline__ uint32_t most_of_lanes(uint32_t v) {   // in lane 63,
     return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), 63));
 }
 
+// sum over neighbouring LANES lanes, in all of them
+template <int LANES>
+__device__ __forceinline__ int sum_of_lanes(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0xb1, 0xf, 0xf, false);    // one lane on within pairs, two within fours,
+    v += __builtin_amdgcn_update_dpp(0, v, 0x4e, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x141, 0xf, 0xf, false);   // mirrored within eight, within sixteen
+    if (LANES > 8) v += __builtin_amdgcn_update_dpp(0, v, 0x140, 0xf, 0xf, false);
+    if (LANES > 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        v = static_cast<int>(r[0] + r[1]);
+    }
+    return v;
+}
+
 // The pooled query of token `tok` and a kv head, in LDS.  Ends with a barrier.
 template <typename T>
 __device__ void pool_query(const SelectArgs &a, int64_t tok, int head, Pooled &l) {
@@ -116,10 +130,10 @@ __device__ void pool_query(const SelectArgs &a, int64_t tok, int head, Pooled &l
     __syncthreads();
 }
 
-// Scores of blocks [from, to): put(block, word).  LANES: lanes per record.
-template <int LANES, typename Put>
-__device__ __forceinline__ void score_blocks(const SelectArgs &a, const int32_t *table, int head, int from, int to, const Pooled &l, Put put) {
-    constexpr int kAt = kThreads / LANES, kDepth = 4;   // records at once, rounds in flight
+// Scores of blocks [from, to), whose pages are page_of(block): put(block, word).  LANES: lanes per record.
+template <int LANES, int kDepth, typename Page, typename Put>
+__device__ __forceinline__ void score_blocks(const SelectArgs &a, int head, int from, int to, const Pooled &l, Page page_of, Put put) {
+    constexpr int kAt = kThreads / LANES;   // records at once; kDepth rounds in flight
     const int piece = threadIdx.x % LANES, mine = threadIdx.x / LANES, D = a.p.dim, KV = a.p.kv_heads;
     const bool there = piece * 16 < 2 * D;
     u32x4_t lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
@@ -134,7 +148,7 @@ __device__ __forceinline__ void score_blocks(const SelectArgs &a, const int32_t 
 #pragma unroll
         for (int j = 0; j < kDepth; ++j) {
             const int b = min(b0 + j * kAt, to - 1);
-            record[j] = int64_t(page_in(table[b], static_cast<int>(a.p.n_pages))) * KV + head;
+            record[j] = int64_t(page_in(page_of(b), static_cast<int>(a.p.n_pages))) * KV + head;
         }
 #pragma unroll
         for (int j = 0; j < kDepth; ++j) {
@@ -150,20 +164,18 @@ __device__ __forceinline__ void score_blocks(const SelectArgs &a, const int32_t 
                 s0 = __builtin_amdgcn_sdot4(static_cast<int>(w[j][e]), static_cast<int>(lo[e]), s0, false);
                 s1 = __builtin_amdgcn_sdot4(static_cast<int>(w[j][e]), static_cast<int>(hi[e]), s1, false);
             }
-            int sum = s0 + 128 * s1;
-#pragma unroll
-            for (int d = LANES / 2; d; d >>= 1) sum += __shfl_xor(sum, d);
+            const int sum = sum_of_lanes<LANES>(s0 + 128 * s1);
             const int b = b0 + j * kAt;
             if (piece == 0 && b < to) put(b, ordered(step[j] < INFINITY ? static_cast<float>(sum) * step[j] : INFINITY));
         }
     }
 }
 
-template <typename Put>
-__device__ __forceinline__ void score_blocks(const SelectArgs &a, const int32_t *table, int head, int from, int to, const Pooled &l, Put put) {
-    if (a.p.dim <= 64) score_blocks<8>(a, table, head, from, to, l, put);
-    else if (a.p.dim <= 128) score_blocks<16>(a, table, head, from, to, l, put);
-    else score_blocks<32>(a, table, head, from, to, l, put);
+template <int kDepth, typename Page, typename Put>
+__device__ __forceinline__ void score_blocks(const SelectArgs &a, int head, int from, int to, const Pooled &l, Page page_of, Put put) {
+    if (a.p.dim <= 64) score_blocks<8, kDepth>(a, head, from, to, l, page_of, put);
+    else if (a.p.dim <= 128) score_blocks<16, kDepth>(a, head, from, to, l, page_of, put);
+    else score_blocks<32, kDepth>(a, head, from, to, l, page_of, put);
 }
 
 // A token's sequence, its own block and the blocks that are scored: [lo, hi).
@@ -198,7 +210,7 @@ __global__ __launch_bounds__(kThreads) void kv_score_kernel(SelectArgs a) {
     if (!r.there || from >= to) return;
     pool_query<T>(a, r.tok, head, pooled);
     uint32_t *out = a.scores + (r.tok * a.p.kv_heads + head) * a.blocks;
-    score_blocks(a, r.table, head, from, to, pooled, [&](int b, uint32_t word) { out[b] = word; });
+    score_blocks<4>(a, head, from, to, pooled, [&](int b) { return r.table[b]; }, [&](int b, uint32_t word) { out[b] = word; });
 }
 
 struct SelectLds {
@@ -230,8 +242,10 @@ __global__ __launch_bounds__(kThreads) void kv_select_kernel(SelectArgs a) {
     l.bins[0][tid] = 0;
     const uint32_t *words = SCORED ? a.scores + row * a.blocks + r.lo : made;
     if constexpr (!SCORED) {
-        pool_query<T>(a, r.tok, head, pooled);
-        score_blocks(a, r.table, head, r.lo, r.hi, pooled, [&](int b, uint32_t word) { made[b - r.lo] = word; });
+        // a block's page number lies where its score will, so that records do not wait for the table one by one
+        for (int i = tid; i < n; i += kThreads) made[i] = r.table[r.lo + i];
+        pool_query<T>(a, r.tok, head, pooled);   // ends with a barrier
+        score_blocks<8>(a, head, r.lo, r.hi, pooled, [&](int b) { return static_cast<int32_t>(made[b - r.lo]); }, [&](int b, uint32_t word) { made[b - r.lo] = word; });
         __syncthreads();
     }
     // a thread's words are kThreads apart; 0 (less than any score's word) behind the last one
