@@ -349,8 +349,10 @@ int picked_queries(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries
     if (queries > kUnions / n_select) queries = kUnions / n_select;
     if (queries > q.max_q) queries = q.max_q;
     if (queries < 2 || ix.max_pages > words) return 0;
-    const int64_t tiles = (int64_t(q.total_q) + queries - 1) / queries;
-    return tiles * p.kv_heads >= 64 ? queries : 0;
+    // fewer queries together while that leaves CUs idle (the union of 64 queries' picks, eight by eight, is 46 us of one workgroup's work)
+    auto groups = [&] { return (q.total_q + queries - 1) / queries * p.kv_heads; };
+    while (queries > 3 && groups() < 256) queries /= 2;
+    return groups() >= 64 ? queries : 0;
 }
 
 void launch_kv_picked(const AttentionArgs &a, int queries, dim3 grid, hipStream_t stream) {

@@ -361,10 +361,178 @@ __global__ __launch_bounds__(kThreads) void kv_select_kernel(SelectArgs a) {
     }
 }
 
-// The scores pass through the workspace where the queries and heads alone leave CUs idle and there is enough to share out, or
+// ---- several queries of a sequence -------------------------------------------------------------------------------------------
+//
+// Eight neighbouring queries share a workgroup and a read of each record: the scores are a matrix product of the records (rows) and
+// the pooled queries' two bytes per channel (16 columns) on v_mfma_i32_16x16x64_i8.  A wave then picks for two of the queries by itself,
+// without barriers.
+
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+
+constexpr int kQueries = 8;
+constexpr int kTileBlocks = 2048;   // blocks of a sequence, at most (32 scores of a lane)
+
+// Picks of one query by one wave: the k largest of words[0, n), block r0 + i for word i, in ascending order to picks.  NW * 64 >= n.
+template <int NW>
+__device__ __forceinline__ void pick_by_wave(const uint32_t *words, int n, uint32_t k, uint32_t *bins, int r0, int32_t *picks) {
+    const int lane = threadIdx.x & 63;
+    uint32_t kept[NW], least = 0xffffffffu, most = 0;
+#pragma unroll
+    for (int j = 0; j < NW; ++j) {
+        kept[j] = j * kWave + lane < n ? words[j * kWave + lane] : 0u;
+        least = min(least, kept[j] ? kept[j] : 0xffffffffu);
+        most = max(most, kept[j]);
+    }
+    least = ~most_of_lanes(~least);
+    most = most_of_lanes(most);
+    uint32_t above = 0;
+    while (least < most) {   // as in kv_select_kernel
+        const int cut = max(24 - __clz(most - least), 0);
+        *reinterpret_cast<uint4 *>(bins + lane * 4) = make_uint4(0, 0, 0, 0);
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int j = 0; j < NW; ++j)
+            if (kept[j] >= least && kept[j] <= most) atomicAdd(&bins[(kept[j] - least) >> cut], 1u);
+        __builtin_amdgcn_wave_barrier();
+        const uint4 b = *reinterpret_cast<const uint4 *>(bins + (kWave - 1 - lane) * 4);
+        __builtin_amdgcn_wave_barrier();
+        const uint32_t here = b.x + b.y + b.z + b.w, upto = above + prefix_of_lanes(here);
+        const int at = __ffsll(static_cast<long long>(__ballot(upto >= k))) - 1;
+        uint32_t sum = __builtin_amdgcn_readlane(upto - here, at), inside = __builtin_amdgcn_readlane(b.w, at);
+        const uint32_t rest[3] = {static_cast<uint32_t>(__builtin_amdgcn_readlane(b.z, at)), static_cast<uint32_t>(__builtin_amdgcn_readlane(b.y, at)),
+                                  static_cast<uint32_t>(__builtin_amdgcn_readlane(b.x, at))};
+        int bin = (kWave - 1 - at) * 4 + 3;
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+            if (sum + inside < k) {
+                sum += inside;
+                inside = rest[j];
+                --bin;
+            }
+        above = sum;
+        least += static_cast<uint32_t>(bin) << cut;
+        most = most - least < (1u << cut) ? most : least + ((1u << cut) - 1u);
+        if (sum + inside == k) {
+            most = --least;
+            above = k;
+        }
+    }
+    const uint32_t take = k - above;
+    const uint64_t below = (uint64_t(1) << lane) - 1;
+    uint32_t more_at = 0, same_at = 0;
+#pragma unroll
+    for (int j = 0; j < NW; ++j) {
+        const uint64_t more = __ballot(kept[j] > least), same = __ballot(kept[j] == least);
+        const uint32_t m = more_at + __popcll(more & below), e = same_at + __popcll(same & below);
+        if (kept[j] > least || (kept[j] == least && e < take)) picks[m + min(e, take)] = r0 + j * kWave + lane;
+        more_at += __popcll(more);
+        same_at += __popcll(same);
+    }
+}
+
+// PRODUCTS: of 64 bytes of a record each
+template <typename T, int PRODUCTS>
+__global__ __launch_bounds__(kThreads, 4) void kv_select_tile_kernel(SelectArgs a) {
+    extern __shared__ uint32_t words[];                                 // kQueries x blocks
+    __shared__ __align__(16) int8_t pooled[2 * kQueries][2 * kMaxDim];   // columns: the low bytes of the queries, the high ones
+    __shared__ __align__(16) uint32_t bins[kWavesOf][256];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
+    const int head = blockIdx.y, t_first = blockIdx.x * kQueries, D = a.p.dim, KV = a.p.kv_heads, G = a.q.heads / KV;
+    const Query first = query_of(a, blockIdx.z, t_first);
+    if (!first.there) return;
+    int top = 0;   // blocks that some query of the tile scores: [n_sink, top)
+#pragma unroll
+    for (int t = 0; t < kQueries; ++t) {
+        const Query r = query_of(a, blockIdx.z, t_first + t);
+        if (r.there) top = max(top, r.hi);
+    }
+    const int lo = a.n_sink, count = top - lo;
+    if (count > 0) {
+        // pooled queries: a wave per query, lanes on channels
+        for (int t = wave; t < kQueries; t += kWavesOf) {
+            const Query r = query_of(a, blockIdx.z, t_first + t);
+            float most = 0.f;
+            const T *q = static_cast<const T *>(a.q.q) + (r.there ? r.tok : first.tok) * a.q.q_stride + int64_t(head) * G * D;
+#pragma unroll 4
+            for (int i = lane; i < G * D; i += kWave) {
+                const float f = fabsf(ElemIO<T>::load(q + i));
+                most = f < INFINITY ? fmaxf(most, f) : most;
+            }
+            const float up = pow2_of(6 - exponent_of(__uint_as_float(most_of_lanes(__float_as_uint(most)))));
+            for (int d = lane; d < kMaxDim; d += kWave) {
+                int pos = 0, neg = 0;
+                if (d < D)
+#pragma unroll 4
+                    for (int u = 0; u < G; ++u) {
+                        const float f = ElemIO<T>::load(q + u * D + d);
+                        const int c = fabsf(f) < INFINITY ? static_cast<int>(rintf(f * up)) : 0;
+                        pos += max(c, 0);
+                        neg += min(c, 0);
+                    }
+                if (d < D) {
+                    pooled[t][d] = static_cast<int8_t>(pos % 128);
+                    pooled[kQueries + t][d] = static_cast<int8_t>(pos / 128);
+                    pooled[t][D + d] = static_cast<int8_t>(neg % 128);
+                    pooled[kQueries + t][D + d] = static_cast<int8_t>(neg / 128);
+                }
+            }
+        }
+        __syncthreads();
+        i32x4_t column[PRODUCTS];
+#pragma unroll
+        for (int m = 0; m < PRODUCTS; ++m) {
+            column[m] = i32x4_t{0, 0, 0, 0};
+            if (64 * m + 16 * g < 2 * D) column[m] = *reinterpret_cast<const i32x4_t *>(&pooled[n][64 * m + 16 * g]);
+        }
+        for (int b0 = wave * 16; b0 < count; b0 += kWavesOf * 16) {
+            const int64_t mine = int64_t(page_in(first.table[lo + min(b0 + n, count - 1)], static_cast<int>(a.p.n_pages))) * KV + head;
+            const int8_t *record = a.p.summary + mine * (2 * D) + 16 * g;
+            const float step = a.p.step[mine];   // of record n; rows come out four to a lane
+            i32x4_t row[PRODUCTS], sum = {0, 0, 0, 0};
+#pragma unroll
+            for (int m = 0; m < PRODUCTS; ++m) {
+                row[m] = i32x4_t{0, 0, 0, 0};
+                if (64 * m + 16 * g < 2 * D) row[m] = *reinterpret_cast<const i32x4_t *>(record + 64 * m);
+            }
+#pragma unroll
+            for (int m = 0; m < PRODUCTS; ++m)
+                sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(row[m], column[m], sum, 0, 0, 0);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int high = __builtin_amdgcn_update_dpp(0, sum[j], 0x128, 0xf, 0xf, false);   // eight lanes on in the row
+                const int b = b0 + 4 * g + j;
+                const float st = __shfl(step, 4 * g + j);
+                if (n < kQueries && b < count)
+                    words[n * a.blocks + b] = ordered(st < INFINITY ? static_cast<float>(sum[j] + 128 * high) * st : INFINITY);
+            }
+        }
+        __syncthreads();
+    }
+    for (int t = wave; t < kQueries; t += kWavesOf) {
+        const Query r = query_of(a, blockIdx.z, t_first + t);
+        if (!r.there) break;
+        int32_t *picks = a.picks + (r.tok * KV + head) * a.n_select;
+        if (r.hi <= r.lo) {   // no choice
+            for (int i = lane; i < a.n_select; i += kWave) picks[i] = i <= r.last ? i : -1;
+            continue;
+        }
+        for (int i = lane; i < a.n_sink; i += kWave) picks[i] = i;
+        for (int i = lane; i < a.n_recent; i += kWave) picks[a.n_select - a.n_recent + i] = r.hi + i;
+        const uint32_t k = a.n_select - a.n_sink - a.n_recent, *mine = words + t * a.blocks;
+        const int m = r.hi - r.lo;
+        if (k == 0) continue;
+        if (m <= 4 * kWave) pick_by_wave<4>(mine, m, k, bins[wave], r.lo, picks + a.n_sink);
+        else if (m <= 12 * kWave) pick_by_wave<12>(mine, m, k, bins[wave], r.lo, picks + a.n_sink);
+        else pick_by_wave<32>(mine, m, k, bins[wave], r.lo, picks + a.n_sink);
+    }
+}
+
+bool tiled(const KvQueries &q, int64_t blocks) { return q.max_q > 1 && blocks <= kTileBlocks; }
+
+// One query at a time: the scores pass through the workspace where the queries and heads alone leave CUs idle and there is enough to share out, or
 // where they do not fit into LDS.
 bool sliced(const tbn_kv_pool &p, const KvQueries &q, int64_t blocks) {
-    return blocks > kInLds || (q.total_q * p.kv_heads < 128 && blocks > 512);
+    return !tiled(q, blocks) && (blocks > kInLds || (q.total_q * p.kv_heads < 128 && blocks > 512));
 }
 
 int64_t blocks_of(const tbn_kv_pool &p, const KvQueries &q) { return (q.max_len + p.page - 1) / p.page; }
@@ -381,7 +549,13 @@ void launch_select_kernel(const SelectArgs &a, hipStream_t stream) {
 
 template <typename T>
 tbn_status launch_select_typed(const SelectArgs &a, bool split, hipStream_t stream) {
-    if (split) {
+    if (tiled(a.q, a.blocks)) {
+        const dim3 grid((a.q.max_q + kQueries - 1) / kQueries, a.p.kv_heads, a.ix.n_seqs);
+        const unsigned lds = 4u * kQueries * a.blocks;
+        if (a.p.dim <= 64) hipLaunchKernelGGL((kv_select_tile_kernel<T, 2>), grid, dim3(kThreads), lds, stream, a);
+        else if (a.p.dim <= 128) hipLaunchKernelGGL((kv_select_tile_kernel<T, 4>), grid, dim3(kThreads), lds, stream, a);
+        else hipLaunchKernelGGL((kv_select_tile_kernel<T, 8>), grid, dim3(kThreads), lds, stream, a);
+    } else if (split) {
         const int64_t slices = (a.blocks + kSliced - 1) / kSliced;
         if (slices * a.q.max_q > 0x7fffffffLL) {
             set_error("tbn_block_select: %d queries of %lld slices are beyond one launch", a.q.max_q, (long long)slices);
@@ -397,7 +571,12 @@ tbn_status launch_select_typed(const SelectArgs &a, bool split, hipStream_t stre
 
 template <typename T>
 hipError_t allow_lds() {   // up to 64 KiB of scores beside the static arrays
-    return hipFuncSetAttribute(reinterpret_cast<const void *>(&kv_select_kernel<T, false, 64>), hipFuncAttributeMaxDynamicSharedMemorySize, 4 * kInLds);
+    const void *kernels[] = {reinterpret_cast<const void *>(&kv_select_kernel<T, false, 64>), reinterpret_cast<const void *>(&kv_select_tile_kernel<T, 2>),
+                             reinterpret_cast<const void *>(&kv_select_tile_kernel<T, 4>), reinterpret_cast<const void *>(&kv_select_tile_kernel<T, 8>)};
+    static_assert(kQueries * kTileBlocks == kInLds, "one limit");
+    for (const void *k : kernels)
+        if (const hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, 4 * kInLds); e != hipSuccess) return e;
+    return hipSuccess;
 }
 
 }  // namespace

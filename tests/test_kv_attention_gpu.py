@@ -367,6 +367,36 @@ def test_select_of_many_blocks(kv, blocks, P, dt):
                 assert got[t, h].tolist() == want + [-1] * (n - len(want))
 
 
+@pytest.mark.parametrize("blocks,P,D,G", [(300, 32, 8, 3), (600, 32, 64, 1), (1500, 64, 128, 4), (3000, 32, 16, 8), (5000, 32, 8, 2), (17000, 32, 8, 3), (400, 128, 256, 12)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens", [1, 11])
+def test_select_by_one_and_by_several(kv, blocks, P, D, G, dt, tokens):
+    """One token of each of many blocks, and neighbouring ones that share the records; scores of every sign, ties among them."""
+    KV = 2
+    rng = np.random.RandomState(blocks + D)
+    L = blocks * P - 5
+    pool = kv.kv_pool(blocks, KV, D, P, torch.float32 if dt == "f32" else torch.bfloat16, summary=True)
+    index = kv.kv_index(1, blocks, blocks, P)
+    order = rng.permutation(blocks)
+    index.table.copy_(torch.from_numpy(order.astype(np.int32)[None]))
+    index.lens.fill_(L)
+    hi = rng.randint(-64, 65, (blocks, KV, D))
+    codes = np.stack([hi, np.maximum(hi - rng.randint(0, 60, hi.shape), -64)], 2)
+    codes[rng.randint(0, blocks, blocks // 8)] = codes[0]
+    steps = 2.0 ** rng.randint(-3, 2, (blocks, KV))
+    steps[rng.randint(0, blocks, 3)] = math.inf
+    pool.summary.copy_(torch.from_numpy(codes.astype(np.int8)))
+    pool.step.copy_(torch.from_numpy(steps.astype(np.float32)))
+    q, cu, qs = make_queries(dt, [tokens], KV * G, D, stride=KV * G * D + 8)
+    for n, sink, recent in ((20, 1, 2), (min(250, blocks - 30), 0, 1), (3, 1, 1), (4, 0, 1)):
+        got = kv.tbn_block_select(q, pool, index, cu, tokens, n, n_sink=sink, n_recent=recent).cpu().numpy()
+        for t in range(tokens):
+            for h in range(KV):
+                own = (L - tokens + t) // P
+                want = orc.picks(qs[t, h * G:(h + 1) * G], codes[order, h], steps[order, h], own, n, sink, recent)
+                assert got[t, h].tolist() == want + [-1] * (n - len(want))
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_many_queries_of_a_prompt(kv, dt):
     """More queries than the rule for shared scoring takes, each with blocks of its own."""
