@@ -426,12 +426,16 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, 
     pl.row_tiles = static_cast<int>(ceil_div(rows, pl.rows));
     const int64_t blocks = groups * pl.row_tiles;
     // Stretches of keys.  The staged kernel has two workgroups per CU and is bound by the matrix cores: one round of them (64 drafted tokens
-    // on 131000 keys: 184 us, in four rounds 227).  Here many small ones even out ragged lengths (64 sequences of 4096 - 16384 keys: 465 us in
-    // 8192 stretches, 534 in 512), but not below 1024 keys while those make 2048 workgroups (16 sequences, 16 rows: 153 us, with 256 keys 167).
+    // on 131000 keys: 188 us, in four rounds 227).  Here many small ones even out ragged lengths (64 sequences of 4096 - 16384 keys: 465 us in
+    // 8192 stretches, 534 in 512), but not below 1024 keys while those make 512 workgroups (16 sequences, 16 rows: 153 us, with 256 keys 167),
+    // and down to one step of each wave where even they do not (one token on 513 keys: 10.5 us, with 256 keys 11.9; on 16000: 20.4, with 128
+    // keys 23.4).
     int64_t chunk = ceil_div(units, ceil_div(pl.staged ? 512 : 8192, blocks));
     if (!picked && !pl.staged) {
-        const int64_t fill = ceil_div(units * blocks, 2048), least = fill < 1024 ? fill : 1024;
+        const int64_t fill = ceil_div(units * blocks, 512), least = fill < 1024 ? fill : 1024;
         if (chunk < least) chunk = least;
+        // short sequences that fill the CUs: not split, the join would take longer (40 sequences of 600 keys, 8 kv heads: 20 us, 24 in parts)
+        if (units <= 1024 && blocks >= 256) chunk = units;
     }
     chunk = ceil_div(chunk, unit_step) * unit_step;
     if (chunk > unit_most) chunk = unit_most;
@@ -442,7 +446,7 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, 
 
 Plan tree_plan(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q) {
     const int64_t rows = int64_t(q.max_q) * (q.heads / p.kv_heads);
-    return plan_of(p, rows, int64_t(ix.n_seqs) * p.kv_heads, q.max_len, 256, int64_t(kListed) * p.page, false);
+    return plan_of(p, rows, int64_t(ix.n_seqs) * p.kv_heads, q.max_len, 128, int64_t(kListed) * p.page, false);
 }
 
 Plan picked_plan(const tbn_kv_pool &p, const KvQueries &q, int32_t n_select) {
