@@ -18,15 +18,11 @@ constexpr int kOneWaves = kOne / kWave;
 constexpr int kPer = 16;                 // pages per lane and round
 constexpr int kRound = kOne * kPer;
 
-// exclusive prefix of v over the workgroup's threads, and the total; `part` has kOneWaves words of LDS
-__device__ __forceinline__ int64_t block_prefix(int64_t v, int64_t *part, int64_t &total) {
+// exclusive prefix of v (below 2^26) over the workgroup's threads, and the total; `part` has kOneWaves words of LDS
+__device__ __forceinline__ int64_t block_prefix(uint32_t v, int64_t *part, int64_t &total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int64_t sum = v;
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-        const int64_t o = __shfl_up(sum, d);
-        if (lane >= d) sum += o;
-    }
+    const uint32_t low = prefix_of_lanes(v & 0xffffu), high = prefix_of_lanes(v >> 16);
+    const int64_t sum = int64_t(low) + (int64_t(high) << 16);
     __syncthreads();   // part may still be read from the call before
     if (lane == 63) part[wave] = sum;
     __syncthreads();
@@ -41,26 +37,27 @@ __device__ __forceinline__ int64_t block_prefix(int64_t v, int64_t *part, int64_
     return before + sum - v;
 }
 
-// Walks pages [begin, end) in rounds of kRound.  take(ref, page) says which pages count; the r-th of them (r from `rank`) goes to
-// out(r, page).  Ends once `want` have been found.  Returns the number found.
+// A round's pages: lane l of wave w has page at + 1024 w + 64 j + l in r[j], -1 beyond `end`.
+__device__ __forceinline__ void load_round(const int32_t *refs, int64_t at, int end, int (&r)[kPer]) {
+    const int64_t mine = at + (threadIdx.x >> 6) * (kWave * kPer) + (threadIdx.x & 63);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) r[j] = mine + j * kWave < end ? refs[mine + j * kWave] : -1;
+}
+
+// Ranks the pages [begin, end) that take(ref) picks: the i-th of them goes to out(i, page), i < want; ends once they are found.  r holds
+// the first round already.  Returns the number found, at most want.
 template <typename Take, typename Out>
-__device__ int rank_pages(const int32_t *refs, int begin, int end, int want, int64_t *part, Take take, Out out) {
+__device__ int rank_pages(const int32_t *refs, int begin, int end, int want, int64_t *part, int (&r)[kPer], Take take, Out out) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int found = 0;
     for (int64_t at = begin; at < end && found < want; at += kRound) {
-        const int64_t mine = at + wave * (kWave * kPer);
-        int r[kPer];
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            const int64_t i = mine + j * kWave + lane;
-            r[j] = i < end ? refs[i] : -1;
-        }
+        const int64_t mine = at + wave * (kWave * kPer) + lane;
+        if (at > begin) load_round(refs, at, end, r);
         uint64_t hit[kPer];
         int n = 0;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
-            const int64_t i = mine + j * kWave + lane;
-            hit[j] = __ballot(i < end && take(r[j]));
+            hit[j] = __ballot(mine + j * kWave < end && take(r[j]));
             n += __popcll(hit[j]);
         }
         __syncthreads();
@@ -77,7 +74,7 @@ __device__ int rank_pages(const int32_t *refs, int begin, int end, int want, int
         for (int j = 0; j < kPer; ++j) {
             if ((hit[j] >> lane) & 1) {
                 const int rank = before + __popcll(hit[j] & ((uint64_t(1) << lane) - 1));
-                if (rank < want) out(rank, static_cast<int>(mine + j * kWave + lane));
+                if (rank < want) out(rank, static_cast<int>(mine + j * kWave));
             }
             before += __popcll(hit[j]);
         }
@@ -86,21 +83,24 @@ __device__ int rank_pages(const int32_t *refs, int begin, int end, int want, int
     return min(found, want);
 }
 
+constexpr int kNear = 2048;   // of a list of pages, the part that stays in LDS
+
 // Three words of LDS per sequence: the last page it would write to (-1: none that is shared), its first fresh slot, the rank of its
-// first fresh page.
+// first fresh page.  What nothing has to wait for (the first round of refs, status, the first 1024 sequences) is requested first.
 __global__ __launch_bounds__(kOne) void kv_reserve_kernel(tbn_kv_index ix, const int32_t *__restrict__ n_new, int32_t *__restrict__ copy_src,
-                                                          int32_t *__restrict__ copy_dst, int32_t *__restrict__ fresh) {
+                                                          int32_t *__restrict__ copy_dst, int32_t *__restrict__ far) {
     extern __shared__ int lds[];
     __shared__ int64_t part[kOneWaves];
-    __shared__ int bad;
+    __shared__ int near[kNear];
     const int n = ix.n_seqs, tid = threadIdx.x, shift = __ffs(ix.page) - 1, n_pages = static_cast<int>(ix.n_pages);
     const int64_t most = int64_t(ix.max_pages) << shift;
     int *tail = lds, *first = lds + n, *rank = lds + 2 * n;
-    if (tid == 0) bad = *ix.status;
-    __syncthreads();
-    int invalid = 0;
+    int r[kPer];
+    load_round(ix.refs, 0, n_pages, r);
+    const int before = *ix.status, len0 = tid < n ? ix.lens[tid] : 0, add0 = tid < n ? n_new[tid] : 0;
+    bool invalid = false;
     for (int s = tid; s < n; s += kOne) {
-        const int len = ix.lens[s], add = n_new[s];
+        const int len = s == tid ? len0 : ix.lens[s], add = s == tid ? add0 : n_new[s];
         const bool ok = len >= 0 && add >= 0 && int64_t(len) + add <= most;
         invalid |= !ok;
         int t = -1;
@@ -112,56 +112,59 @@ __global__ __launch_bounds__(kOne) void kv_reserve_kernel(tbn_kv_index ix, const
         copy_src[s] = -1;
         copy_dst[s] = -1;
     }
-    if (invalid) atomicCAS(&bad, 0, TBN_KV_INVALID);
-    __syncthreads();
-    if (bad) {
-        if (tid == 0) *ix.status = bad;
+    const bool any_invalid = __syncthreads_or(invalid);
+    if (before || any_invalid) {
+        if (tid == 0 && !before) *ix.status = TBN_KV_INVALID;
         return;
     }
     int64_t total = 0;
     for (int s0 = 0; s0 < n; s0 += kOne) {
         const int s = s0 + tid;
-        int64_t need = 0;
+        uint32_t need = 0;   // at most max_pages, 2^25
         if (s < n) {
-            const int len = ix.lens[s], add = n_new[s], t = tail[s];
+            const int len = s0 == 0 ? len0 : ix.lens[s], add = s0 == 0 ? add0 : n_new[s], t = tail[s];
             int have = (len + ix.page - 1) >> shift;
             if (t >= 0) {   // shared: replaced while more than one owner is left
                 int earlier = 0;
+#pragma unroll 8
                 for (int e = 0; e < s; ++e) earlier += tail[e] == t;
                 if (ix.refs[t] - earlier > 1) --have;
             }
             first[s] = have;
-            need = add > 0 ? ((int64_t(len) + add + ix.page - 1) >> shift) - have : 0;
+            need = add > 0 ? static_cast<uint32_t>(((int64_t(len) + add + ix.page - 1) >> shift) - have) : 0;
         }
         int64_t all;
-        const int64_t before = block_prefix(need, part, all);
-        if (s < n) rank[s] = static_cast<int>(total + before);   // within the pool, or the call fails
+        const int64_t mine = block_prefix(need, part, all);
+        if (s < n) rank[s] = static_cast<int>(total + mine);   // within the pool, or the call fails
         total += all;
         if (total > n_pages) break;
     }
     const int want = static_cast<int>(min(total, int64_t(n_pages)));
-    const int found = total > n_pages ? 0 : rank_pages(ix.refs, 0, n_pages, want, part, [](int r) { return r == 0; },
-                                                       [&](int r, int page) { fresh[r] = page; });
+    const int found = total > n_pages ? 0 : rank_pages(ix.refs, 0, n_pages, want, part, r, [](int x) { return x == 0; }, [&](int i, int page) {
+        if (i < kNear) near[i] = page;
+        else far[i] = page;
+    });
     if (found < total) {
         if (tid == 0) *ix.status = TBN_KV_FULL;
         return;
     }
     __syncthreads();
-    for (int i = tid; i < total; i += kOne) {
+    auto fresh = [&](int i) { return i < kNear ? near[i] : far[i]; };
+    for (int i = tid; i < want; i += kOne) {
         int lo = 0, hi = n - 1;   // the last sequence whose rank is at most i and that needs a page
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
             if (rank[mid] <= i) lo = mid; else hi = mid - 1;
         }
-        const int page = fresh[i];
+        const int page = fresh(i);
         ix.table[int64_t(lo) * ix.max_pages + first[lo] + (i - rank[lo])] = page;
         ix.refs[page] = 1;
     }
     for (int s = tid; s < n; s += kOne) {
-        const int len = ix.lens[s], add = n_new[s], t = tail[s];
+        const int len = s == tid ? len0 : ix.lens[s], add = s == tid ? add0 : n_new[s], t = tail[s];
         if (t >= 0 && first[s] < (len + ix.page - 1) >> shift) {
             copy_src[s] = t;
-            copy_dst[s] = fresh[rank[s]];
+            copy_dst[s] = fresh(rank[s]);
             atomicSub(&ix.refs[t], 1);
         }
         if (add > 0) ix.lens[s] = len + add;
@@ -210,24 +213,41 @@ __global__ __launch_bounds__(256) void kv_release_kernel(tbn_kv_index ix, const 
 __global__ __launch_bounds__(kOne) void kv_compact_kernel(tbn_kv_index ix, int32_t *__restrict__ src, int32_t *__restrict__ dst, int32_t *__restrict__ count,
                                                           int32_t *__restrict__ ws) {
     __shared__ int64_t part[kOneWaves];
+    __shared__ int near[2][kNear];   // the first sources and targets
     const int tid = threadIdx.x, n_pages = static_cast<int>(ix.n_pages);
-    int mine = 0;
-    for (int64_t at = tid; at < n_pages; at += kRound) {
-        int r[kPer];
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) r[j] = at + j * kOne < n_pages ? ix.refs[at + j * kOne] : 0;
+    int r[kPer];
+    uint32_t mine = 0;
+    for (int64_t at = 0; at < n_pages; at += kRound) {
+        load_round(ix.refs, at, n_pages, r);
 #pragma unroll
         for (int j = 0; j < kPer; ++j) mine += r[j] > 0;
     }
     int64_t in_use;
     (void)block_prefix(mine, part, in_use);
-    const int used = static_cast<int>(in_use);
-    const int most = static_cast<int>(n_pages / 2);
-    const int n = rank_pages(ix.refs, used, n_pages, most, part, [](int r) { return r > 0; }, [&](int i, int page) { src[i] = page; });
-    rank_pages(ix.refs, 0, used, n, part, [](int r) { return r <= 0; }, [&](int i, int page) { dst[i] = page; });
+    const int used = static_cast<int>(in_use), most = static_cast<int>(n_pages / 2);
+    // a pool of one round is in r already: pages before `used` are left out by their numbers
+    const bool one = n_pages <= kRound;
+    int n;
+    {
+        const int begin = one ? 0 : used;
+        const int64_t lane_at = (tid >> 6) * (kWave * kPer) + (tid & 63);
+        int x[kPer];
+        if (!one) load_round(ix.refs, begin, n_pages, x);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) x[j] = one ? (lane_at + j * kWave >= used ? r[j] : 0) : x[j];
+        n = rank_pages(ix.refs, begin, n_pages, most, part, x, [](int v) { return v > 0; }, [&](int i, int page) {
+            src[i] = page;
+            if (i < kNear) near[0][i] = page;
+        });
+        if (!one) load_round(ix.refs, 0, used, r);
+        rank_pages(ix.refs, 0, used, n, part, r, [](int v) { return v <= 0; }, [&](int i, int page) {
+            dst[i] = page;
+            if (i < kNear) near[1][i] = page;
+        });
+    }
     __syncthreads();
     for (int i = tid; i < n; i += kOne) {
-        const int a = src[i], b = dst[i];
+        const int a = i < kNear ? near[0][i] : src[i], b = i < kNear ? near[1][i] : dst[i];
         ws[1 + a] = b;
         ix.refs[b] = ix.refs[a];
         ix.refs[a] = 0;
@@ -317,20 +337,21 @@ struct SummaryLds {
 
 // Summary of one page and kv head over its first `rows` rows (>= 1).  Lanes own 16 bytes of channels and every
 // (256 / groups)-th row; partial extremes meet in LDS.  Every thread of the workgroup calls it.
-template <typename T>
-__device__ void summarize(const tbn_kv_pool &p, int64_t page, int head, int rows, SummaryLds &l) {
+// row_at(r): where row r is.
+template <typename T, typename Row>
+__device__ void summarize(const tbn_kv_pool &p, int64_t page, int head, int rows, SummaryLds &l, Row row_at) {
     constexpr int V = Pack<T>::kVec;
     const int tid = threadIdx.x, groups = p.dim / V, lanes = kThreads / groups;
     const int g = tid % groups, r0 = tid / groups;
-    const T *k = static_cast<const T *>(p.k) + (page * p.kv_heads + head) * (int64_t(p.page) * p.dim);
     float hi[V], lo[V];
     bool bad = false;
 #pragma unroll
     for (int i = 0; i < V; ++i) hi[i] = -INFINITY, lo[i] = INFINITY;
     if (r0 < lanes)
+#pragma unroll 4
         for (int r = r0; r < rows; r += lanes) {
             float f[V];
-            Pack<T>::unpack(*reinterpret_cast<const u32x4_t *>(k + int64_t(r) * p.dim + g * V), f);
+            Pack<T>::unpack(*reinterpret_cast<const u32x4_t *>(row_at(r) + g * V), f);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 hi[i] = fmaxf(hi[i], f[i]);
@@ -373,9 +394,10 @@ __device__ void summarize(const tbn_kv_pool &p, int64_t page, int head, int rows
 
 constexpr int kCols = 64;   // channels of V that a workgroup turns at a time
 
+// + 8 bytes: rows stay aligned for 8-byte reads, and lanes that write one channel of eight begin on different banks
 template <typename T>
 struct AppendLds {
-    T tile[kCols][128 + 16 / sizeof(T)];   // + 16 bytes: rows stay aligned for 16-byte reads and start on different banks
+    T tile[kCols][128 + 8 / sizeof(T)];
 };
 
 // Rows [r0, r1) of a page come from tokens tok .. of the call.  ALIGNED: 16-byte loads from k_new and v_new.
@@ -386,10 +408,9 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(tbn_kv_pool p, tbn_
     constexpr int V = Pack<T>::kVec;
     __shared__ union { AppendLds<T> v; SummaryLds s; } lds;
     const int tid = threadIdx.x, s = blockIdx.z, head = blockIdx.y, shift = __ffs(p.page) - 1;
-    if (*ix.status != 0) return;
-    const int t0 = max(cu_new[s], 0), n = min(cu_new[s + 1], total) - t0;
+    const int failed = *ix.status, t0 = max(cu_new[s], 0), n = min(cu_new[s + 1], total) - t0;
     const int len = len_in(ix.lens[s], int64_t(ix.max_pages) << shift);
-    if (n <= 0 || n > len) return;
+    if (failed || n <= 0 || n > len) return;
     const int slot = ((len - n) >> shift) + blockIdx.x, base = slot << shift;
     if (base >= len) return;
     const int64_t page = page_in(ix.table[int64_t(s) * ix.max_pages + slot], static_cast<int>(p.n_pages));
@@ -423,13 +444,21 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(tbn_kv_pool p, tbn_
             const int cols = min(kCols, p.dim - c0);
             __syncthreads();
             if constexpr (ALIGNED) {
-                const int groups = cols / V;
-                for (int i = tid; i < rows * groups; i += kThreads) {
-                    const int r = i / groups, c = (i - r * groups) * V;
-                    union { u32x4_t w; T e[V]; } u;
-                    u.w = *reinterpret_cast<const u32x4_t *>(vs + r * v_stride + c0 + c);
+                // two rows at a time where elements are half a word: whole words go to LDS
+                constexpr int kRows = 4 / sizeof(T);
+                const int groups = cols / V, even = r0 & (kRows - 1), pairs = (rows + even + kRows - 1) / kRows;
+                for (int i = tid; i < pairs * groups; i += kThreads) {
+                    const int pr = i / groups, c = (i - pr * groups) * V, r = pr * kRows - even;   // from row r0 + r on
+                    union Piece { u32x4_t w; T e[V]; } u[kRows];
 #pragma unroll
-                    for (int e = 0; e < V; ++e) lds.v.tile[c + e][r0 + r] = u.e[e];
+                    for (int x = 0; x < kRows; ++x) u[x].w = *reinterpret_cast<const u32x4_t *>(vs + min(max(r + x, 0), rows - 1) * v_stride + c0 + c);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        if constexpr (kRows == 2)   // rows before r0 and behind r1 get something that nobody reads
+                            *reinterpret_cast<uint32_t *>(&lds.v.tile[c + e][r0 + r]) = u[0].e[e] | static_cast<uint32_t>(u[1].e[e]) << 16;
+                        else
+                            lds.v.tile[c + e][r0 + r] = u[0].e[e];
+                    }
                 }
             } else {
                 for (int i = tid; i < rows * cols; i += kThreads) {
@@ -441,7 +470,10 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(tbn_kv_pool p, tbn_
             const int groups = max(a1 - a0, 0) / V;
             for (int i = tid; i < cols * groups; i += kThreads) {
                 const int c = i / groups, r = a0 + (i - c * groups) * V;
-                *reinterpret_cast<u32x4_t *>(vp + (c0 + c) * p.page + r) = *reinterpret_cast<const u32x4_t *>(&lds.v.tile[c][r]);
+                union { u32x4_t w; uint2 h[2]; } u;
+                u.h[0] = *reinterpret_cast<const uint2 *>(&lds.v.tile[c][r]);
+                u.h[1] = *reinterpret_cast<const uint2 *>(&lds.v.tile[c][r + V / 2]);
+                *reinterpret_cast<u32x4_t *>(vp + (c0 + c) * p.page + r) = u.w;
             }
             const int head_rows = min(a0, r1) - r0, odd = head_rows + max(r1 - max(a1, a0), 0);
             for (int i = tid; i < cols * odd; i += kThreads) {
@@ -451,27 +483,28 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(tbn_kv_pool p, tbn_
         }
     }
     if (p.summary) {
-        __syncthreads();   // the keys written above are read again, the tile's LDS is used again
-        summarize<T>(p, page, head, r1, lds.s);
+        __syncthreads();   // the tile's LDS is used again, and (not ALIGNED) the keys written above are read again
+        summarize<T>(p, page, head, r1, lds.s, [&](int r) { return ALIGNED && r >= r0 ? ks + (r - r0) * k_stride : kp + r * p.dim; });
     }
 }
 
-constexpr int kKeepRows = 32;   // rows in registers and LDS between their loads and their stores
+constexpr int kKeepRows = 32;    // rows of keys and of values between their loads and their stores
+constexpr int kKeepPages = 64;   // pages from the base's on whose numbers are at hand
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void kv_keep_kernel(tbn_kv_pool p, tbn_kv_index ix, const int32_t *__restrict__ base, const int32_t *__restrict__ picks,
                                                            int width, const int32_t *__restrict__ counts) {
-    __shared__ T tile[kKeepRows][kMaxDim];
-    __shared__ SummaryLds sum;
-    __shared__ int32_t from[kKeepRows];
+    __shared__ union { T tile[2][kKeepRows][kMaxDim]; SummaryLds sum; } lds;
+    __shared__ int32_t from[kKeepRows], pages[kKeepPages];
     const int tid = threadIdx.x, s = blockIdx.y, head = blockIdx.x, shift = __ffs(p.page) - 1, inside = p.page - 1;
-    if (*ix.status != 0) return;
-    const int len = len_in(ix.lens[s], int64_t(ix.max_pages) << shift), b = base[s];
+    const int failed = *ix.status, len = len_in(ix.lens[s], int64_t(ix.max_pages) << shift), b = base[s];
     const int n = b < 0 || b > len ? 0 : min(min(counts[s], width), len - b);
-    if (n <= 0) return;
+    if (failed || n <= 0) return;
     const int32_t *row = ix.table + int64_t(s) * ix.max_pages;
-    const int n_pages = static_cast<int>(p.n_pages);
-    auto page_of = [&](int key) { return (int64_t(page_in(row[key >> shift], n_pages)) * p.kv_heads + head) * (int64_t(p.page) * p.dim); };
+    const int n_pages = static_cast<int>(p.n_pages), slot0 = b >> shift, slots = ((len + inside) >> shift) - slot0;
+    for (int i = tid; i < min(slots, kKeepPages); i += kThreads) pages[i] = page_in(row[slot0 + i], n_pages);
+    auto page_at = [&](int slot) { return slot - slot0 < kKeepPages ? pages[slot - slot0] : page_in(row[slot], n_pages); };
+    auto page_of = [&](int key) { return (int64_t(page_at(key >> shift)) * p.kv_heads + head) * (int64_t(p.page) * p.dim); };
     T *k = static_cast<T *>(p.k), *v = static_cast<T *>(p.v);
     // Picks ascend and are at or above their places, so a chunk's sources lie behind every target of the chunks before it.
     for (int j0 = 0; j0 < n; j0 += kKeepRows) {
@@ -482,30 +515,35 @@ __global__ __launch_bounds__(kThreads) void kv_keep_kernel(tbn_kv_pool p, tbn_kv
             from[tid] = pick > j0 + tid && pick < len - b ? b + pick : -1;   // -1: stays where it is, or is not there
         }
         __syncthreads();
+#pragma unroll 4
         for (int i = tid; i < m * p.dim; i += kThreads) {
             const int r = i / p.dim, c = i - r * p.dim, f = from[r];
-            if (f >= 0) tile[r][c] = k[page_of(f) + (f & inside) * p.dim + c];
+            if (f >= 0) lds.tile[0][r][c] = k[page_of(f) + (f & inside) * p.dim + c];
         }
-        __syncthreads();
-        for (int i = tid; i < m * p.dim; i += kThreads) {
-            const int r = i / p.dim, c = i - r * p.dim, t = b + j0 + r;
-            if (from[r] >= 0) k[page_of(t) + (t & inside) * p.dim + c] = tile[r][c];
-        }
-        __syncthreads();
+#pragma unroll 4
         for (int i = tid; i < m * p.dim; i += kThreads) {   // neighbouring lanes on neighbouring keys of a channel
             const int c = i / m, r = i - c * m, f = from[r];
-            if (f >= 0) tile[r][c] = v[page_of(f) + c * p.page + (f & inside)];
+            if (f >= 0) lds.tile[1][r][c] = v[page_of(f) + c * p.page + (f & inside)];
         }
         __syncthreads();
+#pragma unroll 4
+        for (int i = tid; i < m * p.dim; i += kThreads) {
+            const int r = i / p.dim, c = i - r * p.dim, t = b + j0 + r;
+            if (from[r] >= 0) k[page_of(t) + (t & inside) * p.dim + c] = lds.tile[0][r][c];
+        }
+#pragma unroll 4
         for (int i = tid; i < m * p.dim; i += kThreads) {
             const int c = i / m, r = i - c * m, t = b + j0 + r;
-            if (from[r] >= 0) v[page_of(t) + c * p.page + (t & inside)] = tile[r][c];
+            if (from[r] >= 0) v[page_of(t) + c * p.page + (t & inside)] = lds.tile[1][r][c];
         }
     }
     if (p.summary) {
         __syncthreads();
-        for (int slot = b >> shift; (slot << shift) < b + n; ++slot)
-            summarize<T>(p, page_in(row[slot], n_pages), head, min(b + n - (slot << shift), p.page), sum);
+        for (int slot = b >> shift; (slot << shift) < b + n; ++slot) {
+            const int64_t page = page_at(slot);
+            const T *rows = k + (page * p.kv_heads + head) * (int64_t(p.page) * p.dim);
+            summarize<T>(p, page, head, min(b + n - (slot << shift), p.page), lds.sum, [&](int r) { return rows + r * p.dim; });
+        }
     }
 }
 

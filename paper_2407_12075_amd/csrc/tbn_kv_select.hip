@@ -49,20 +49,7 @@ __device__ __forceinline__ uint32_t ordered(float f) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Sums and maxima over the lanes of a wave by data-parallel primitives: a step costs a few cycles, an exchange through LDS a hundred.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ uint32_t from_lane(uint32_t v) {   // 0 where no lane is read
-    return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, ROWS, 0xf, false));
-}
-__device__ __forceinline__ uint32_t prefix_of_lanes(uint32_t v) {   // inclusive
-    v += from_lane<0x111, 0xf>(v);   // one, two, four, eight lanes up within rows of 16
-    v += from_lane<0x112, 0xf>(v);
-    v += from_lane<0x114, 0xf>(v);
-    v += from_lane<0x118, 0xf>(v);
-    v += from_lane<0x142, 0xa>(v);   // a row's last lane to the next row, the second row's to the upper half
-    v += from_lane<0x143, 0xc>(v);
-    return v;
-}
+// The largest over the lanes of a wave, in the same way as prefix_of_lanes.
 __device__ __forceinline__ uint32_t most_of_lanes(uint32_t v) {   // in lane 63, for all
     v = max(v, from_lane<0x111, 0xf>(v));
     v = max(v, from_lane<0x112, 0xf>(v));
