@@ -1,4 +1,4 @@
-// Attention over picked blocks for many queries at a time (prompt chunks; bfloat16, pages of 64 or 128 keys).  Mathematics and
+// Attention over picked blocks for many queries at a time (prompt chunks; bfloat16).  Mathematics and
 // parts as in tbn_kv_attention.hip.
 //
 // Queries one by one read every page they pick for themselves.  That traffic comes from L2 and is bound by the L1: operands loaded
@@ -7,7 +7,7 @@
 //     keys enter a row's sums only if its query picked the page;
 //   - keys and values come in whole lines into LDS and from there into registers (piece index xor row, as in tbn_kv_rows.hip).
 //
-// The four waves of a workgroup take units of 64 keys in turn and do not wait for each other: each has two buffers of its own, which
+// The four waves of a workgroup take units of 64 keys (of one page, or two pages of 32) in turn and do not wait for each other: each has two buffers of its own, which
 // hold in turn the two halves of a unit's keys (32 keys each) and the two halves of its values (half of the channels each).  A
 // buffer's next contents are requested as soon as it has been read: S of one half of the keys, the other half, softmax, both halves
 // of the channels.  The waves' sums meet in LDS at the end.
@@ -46,8 +46,8 @@ __device__ __forceinline__ void send(uint32_t to, const void *from) {
 }
 #pragma clang diagnostic pop
 
-// DP: channels (dim <= DP; EVEN: equal).  a.row_tiles tiles of `queries` queries.
-template <int DP, bool EVEN>
+// DP: channels (dim <= DP; EVEN: equal).  PAIRS: pages of 32 keys.  a.row_tiles tiles of `queries` queries.
+template <int DP, bool EVEN, bool PAIRS>
 __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_picked_kernel(AttentionArgs a, int queries) {
     constexpr int BUF = 32 * DP;                 // elements: 32 keys of DP channels, or DP / 2 channels of 64 keys
     constexpr int KP = DP / 8, NP = BUF / 8 / kWave;   // pieces of a row of K; pieces of a lane
@@ -59,7 +59,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_picked_ker
     __shared__ int counts[kAttnWaves];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
-    const int s = blockIdx.y, H = a.q.heads, KV = a.p.kv_heads, G = H / KV, D = EVEN ? DP : a.p.dim, P = a.p.page, shift = __ffs(P) - 1;
+    const int s = blockIdx.y, H = a.q.heads, KV = a.p.kv_heads, G = H / KV, D = EVEN ? DP : a.p.dim, P = PAIRS ? 32 : a.p.page, shift = __ffs(P) - 1;
     const Span v = span_of(a, s);
     const Block blk = block_of(a);
     const int t_first = blk.row_tile * queries;
@@ -110,44 +110,63 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_picked_ker
             for (int e = 0; e < 4; ++e) q[f][e] = n < R && (EVEN || f * 16 + 8 * h < D) ? q[f][e] ^ a.flip : 0u;
     }
 
+    struct Unit {   // its halves of 32 keys: where keys and values are, the first key, who picked it
+        const uint16_t *k[2], *v[2];
+        int key[2];
+        uint32_t who[2];
+    };
     const int64_t page_elems = int64_t(P) * D;
     const uint16_t *kp = static_cast<const uint16_t *>(a.p.k) + blk.head * page_elems, *vp = static_cast<const uint16_t *>(a.p.v) + blk.head * page_elems;
     // Piece j of this lane in a buffer of keys is row U + lane / KP, U = 64 j / KP, and there piece (lane % KP) xor (row & 7).  Both parts of
     // the row have bits of their own, so the key of the row is the sum of theirs and the piece c0 xor (U & 7): what differs between
     // pieces is the same for all lanes, but for the few values of U & 7.
     const int c0 = (lane % KP) ^ ((lane / KP) & 7);
-    const uint32_t k_lane = key_of_row(lane / KP) * D * 2, v_lane = ((lane / 8) * P + ((lane % 8) ^ (lane / 8)) * 8) * 2;
-    auto request_k = [&](uint32_t to, const uint16_t *k, int half) {   // keys 32 * half on of a unit whose rows begin at k
+    const int v_piece = (lane % 8) ^ (lane / 8);   // of a channel's 64 keys; PAIRS: the first four are the first page's
+    const uint32_t k_lane = key_of_row(lane / KP) * D * 2, v_lane = ((lane / 8) * P + (PAIRS ? v_piece & 3 : v_piece) * 8) * 2;
+    auto request_k = [&](uint32_t to, const uint16_t *k) {   // 32 keys from k on
 #pragma unroll
         for (int j = 0; j < NP; ++j) {
             constexpr int kStep = kWave / KP;
             const int c = c0 ^ ((j * kStep) & 7);
-            const uint16_t *row = k + (half * 32 + key_of_row(j * kStep)) * D;
+            const uint16_t *row = k + key_of_row(j * kStep) * D;
             if (EVEN) send(to + j * (kWave * 16), row, k_lane + c * 16);
             else send(to + j * (kWave * 16), c * 8 < D ? reinterpret_cast<const char *>(row) + (k_lane + c * 16) : reinterpret_cast<const char *>(kNothing));
         }
     };
-    auto request_v = [&](uint32_t to, const uint16_t *vv, int half) {   // channels DP / 2 * half on of its 64 keys
+    auto request_v = [&](uint32_t to, const Unit &u, int half) {   // channels DP / 2 * half on of its 64 keys
+        const char *mine = PAIRS ? reinterpret_cast<const char *>(v_piece < 4 ? u.v[0] : u.v[1]) + v_lane : nullptr;
 #pragma unroll
         for (int j = 0; j < NP; ++j) {
             const int d = half * (DP / 2) + 8 * j;   // channels beyond the head's: any, their sums are dropped
-            send(to + j * (kWave * 16), vv + (EVEN ? d : min(d, D - 8)) * P, v_lane);
+            const int at = (EVEN ? d : min(d, D - 8)) * P;
+            if (PAIRS) send(to + j * (kWave * 16), mine + at * 2);
+            else send(to + j * (kWave * 16), u.v[0] + at, v_lane);
         }
     };
 
     uint16_t *const w0 = b0[wave], *const w1 = b1[wave];
     typedef __attribute__((address_space(3))) void *lds_ptr;
     const uint32_t to0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr)w0)), to1 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr)w1));
-    const int per_shift = shift - 6, units = entries << per_shift;
-    // unit i: where its keys and values are, its first key, who picked it
-    auto unit_of = [&](int i, const uint16_t *&k, const uint16_t *&vv, int &key, uint32_t &who) {
-        const int2 e = listed[i >> per_shift];
-        const int block = __builtin_amdgcn_readfirstlane(e.x), off = (i & ((1 << per_shift) - 1)) * 64;
-        who = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(e.y));
-        const int64_t page = int64_t(__builtin_amdgcn_readfirstlane(pages[i >> per_shift])) * (page_elems * KV);
-        k = kp + page + off * D;
-        vv = vp + page + off;
-        key = (block << shift) + off;
+    const int units = PAIRS ? (entries + 1) >> 1 : entries << (shift - 6);
+    auto unit_of = [&](int i, Unit &u) {
+#pragma unroll
+        for (int t = 0; t < (PAIRS ? 2 : 1); ++t) {
+            const int entry = PAIRS ? 2 * i + t : i >> (shift - 6), off = PAIRS ? 0 : (i & ((1 << (shift - 6)) - 1)) * 64;
+            const int use = PAIRS ? min(entry, entries - 1) : entry;   // behind the last page: it again, picked by nobody
+            const int2 e = listed[use];
+            const int block = __builtin_amdgcn_readfirstlane(e.x);
+            const int64_t page = int64_t(__builtin_amdgcn_readfirstlane(pages[use])) * (page_elems * KV);
+            u.who[t] = use == entry ? static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(e.y)) : 0u;
+            u.k[t] = kp + page + off * D;
+            u.v[t] = vp + page + off;
+            u.key[t] = (block << shift) + off;
+        }
+        if (!PAIRS) {
+            u.who[1] = u.who[0];
+            u.k[1] = u.k[0] + 32 * D;
+            u.v[1] = u.v[0];
+            u.key[1] = u.key[0] + 32;
+        }
     };
 
     f32x16_t o[ND];
@@ -160,20 +179,16 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_picked_ker
         m = -INFINITY;
         l = z = 0.f;
         __syncthreads();   // the list is complete, the buffers are free
-        const uint16_t *k = kp, *vv = vp;
-        int key = 0;
-        uint32_t who = 0;
+        Unit now = {{kp, kp}, {vp, vp}, {0, 0}, {0, 0}};
         int i = wave;
         if (i < units) {
-            unit_of(i, k, vv, key, who);
-            request_k(to0, k, 0);
-            request_k(to1, k, 1);
+            unit_of(i, now);
+            request_k(to0, now.k[0]);
+            request_k(to1, now.k[1]);
         }
         for (; i < units; i += kAttnWaves) {
-            const uint16_t *next_k = k, *next_v = vv;
-            int next_key = 0;
-            uint32_t next_who = 0;
-            if (i + kAttnWaves < units) unit_of(i + kAttnWaves, next_k, next_v, next_key, next_who);   // (behind the last one: this one again)
+            Unit next = now;
+            if (i + kAttnWaves < units) unit_of(i + kAttnWaves, next);   // (behind the last one: this one again)
             f32x16_t p[2];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
@@ -187,25 +202,26 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_picked_ker
 #pragma unroll
                 for (int f = 0; f < NQ; ++f) p[t] = mma(x[f], q[f], p[t]);
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // the buffer has been read
-                request_v(t ? to1 : to0, vv, t);
+                request_v(t ? to1 : to0, now, t);
             }
-            const bool member = (who >> mine) & 1u;
-            if (__any(key + 64 > end)) {   // some row's keys end in this unit
+            const bool member[2] = {static_cast<bool>((now.who[0] >> mine) & 1u), static_cast<bool>((now.who[1] >> mine) & 1u)};
+            float top = -INFINITY;
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < 2; ++t) {
+                if (__any(now.key[t] + 32 > end)) {   // some row's keys end in this half
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
-                        const uint32_t bits = first_bits(end - (key + 32 * t + 16 * u + 8 * h));
+                        const uint32_t bits = first_bits(end - (now.key[t] + 16 * u + 8 * h));
 #pragma unroll
                         for (int e = 0; e < 8; ++e) p[t][8 * u + e] = (bits >> e) & 1u ? p[t][8 * u + e] : -INFINITY;
                     }
+                }
+                float most = p[t][0];
+#pragma unroll
+                for (int e = 1; e < 16; ++e) most = fmaxf(most, p[t][e]);
+                top = member[t] ? fmaxf(top, most) : top;
             }
-            float top = p[0][0];
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) top = fmaxf(top, p[t][e]);
-            top = member ? max_over_32(top) * a.c : -INFINITY;
+            top = max_over_32(top) * a.c;
             if (__any(top > m + kSlack)) {
                 const float next_m = fmaxf(m, top), keep = next_m > m ? exp2_of(m - next_m) : 1.f;
                 l *= keep;
@@ -215,11 +231,11 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_picked_ker
                 m = next_m;
             }
             const float from = m == -INFINITY ? 0.f : m;
-            const uint32_t only = member ? ~0u : 0u;
-            float sum = 0.f;
             u32x4_t pw[4];
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < 2; ++t) {
+                const uint32_t only = member[t] ? ~0u : 0u;
+                float sum = 0.f;
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -229,7 +245,8 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_picked_ker
                         pw[2 * t + u][e] = two_bf16(x, y) & only;
                         z = add_two_bf16(pw[2 * t + u][e], z);
                     }
-            l += member ? sum : 0.f;
+                l += member[t] ? sum : 0.f;
+            }
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 uint16_t *buf = t ? w1 : w0;
@@ -237,7 +254,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_picked_ker
                 if (careful) {
 #pragma unroll 1
                     for (int u = 0; u < 4; ++u) {
-                        const uint32_t seen = member ? first_bits(end - (key + 16 * u + 8 * h)) : 0u;
+                        const uint32_t seen = (u < 2 ? member[0] : member[1]) ? first_bits(end - ((u < 2 ? now.key[0] : now.key[1]) + 16 * (u & 1) + 8 * h)) : 0u;
                         const u32x4_t ones = Elem<uint16_t>::ones(seen);
 #pragma unroll
                         for (int f = 0; f < ND / 2; ++f) {
@@ -268,12 +285,9 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_picked_ker
 #pragma unroll
                     for (int f = 0; f < ND / 2; ++f) o[t * (ND / 2) + f] = mma(x[f * 4 + u], pw[u], o[t * (ND / 2) + f]);
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                request_k(t ? to1 : to0, next_k, t);
+                request_k(t ? to1 : to0, next.k[t]);
             }
-            k = next_k;
-            vv = next_v;
-            key = next_key;
-            who = next_who;
+            now = next;
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing is on its way into the buffers any more
         if (careful) break;
@@ -332,18 +346,24 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_picked_ker
     }
 }
 
+template <int DP, bool PAIRS>
+void launch_page(const AttentionArgs &a, int queries, dim3 grid, hipStream_t stream) {
+    if (a.p.dim == DP) hipLaunchKernelGGL((kv_picked_kernel<DP, true, PAIRS>), grid, dim3(kAttnThreads), 0, stream, a, queries);
+    else hipLaunchKernelGGL((kv_picked_kernel<DP, false, PAIRS>), grid, dim3(kAttnThreads), 0, stream, a, queries);
+}
+
 template <int DP>
 void launch_dim(const AttentionArgs &a, int queries, dim3 grid, hipStream_t stream) {
-    if (a.p.dim == DP) hipLaunchKernelGGL((kv_picked_kernel<DP, true>), grid, dim3(kAttnThreads), 0, stream, a, queries);
-    else hipLaunchKernelGGL((kv_picked_kernel<DP, false>), grid, dim3(kAttnThreads), 0, stream, a, queries);
+    if (a.p.page == 32) launch_page<DP, true>(a, queries, grid, stream);
+    else launch_page<DP, false>(a, queries, grid, stream);
 }
 
 }  // namespace
 
-// Queries that share a workgroup, 0 where queries go one by one: float32, pages of 32 keys, heads or picks of which 32 rows or the
+// Queries that share a workgroup, 0 where queries go one by one: float32, heads or picks of which 32 rows or the
 // list hold fewer than two queries, tables longer than the buffers have words, or so few workgroups that the GPU is all but empty.
 int picked_queries(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, int32_t n_select) {
-    if (p.dt != TBN_BF16 || p.page < 64) return 0;
+    if (p.dt != TBN_BF16) return 0;
     const int G = q.heads / p.kv_heads, words = p.dim <= 64 ? 4096 : p.dim <= 128 ? 8192 : 16384;
     int queries = G <= 32 ? 32 / G : 0;
     if (queries > kUnions / n_select) queries = kUnions / n_select;

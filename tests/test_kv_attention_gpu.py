@@ -413,7 +413,9 @@ def test_many_queries_of_a_prompt(kv, dt):
 
 @pytest.mark.parametrize("H,KV,D,P,seqs,n", [
     (32, 8, 128, 64, [(900, 40), (64, 3), (0, 70), (1, 0)], 5), (8, 8, 64, 128, [(1500, 33), (127, 130)], 4), (20, 4, 80, 64, [(700, 100), (63, 2)], 6),
-    (6, 3, 96, 64, [(640, 130)], 3), (64, 4, 128, 64, [(500, 40)], 4), (8, 2, 256, 64, [(800, 300)], 5), (4, 1, 128, 128, [(5000, 300)], 120)])
+    (6, 3, 96, 64, [(640, 130)], 3), (64, 4, 128, 64, [(500, 40)], 4), (8, 2, 256, 64, [(800, 300)], 5), (4, 1, 128, 128, [(5000, 300)], 120),
+    (32, 8, 128, 32, [(450, 40), (32, 3), (0, 70), (1, 0)], 5), (8, 8, 64, 32, [(370, 33), (31, 130)], 7), (20, 4, 80, 32, [(350, 100), (31, 2)], 6),
+    (6, 3, 96, 32, [(320, 130)], 3), (4, 2, 256, 32, [(1000, 200)], 21), (8, 2, 136, 32, [(90, 140)], 4)])
 def test_queries_that_share_a_workgroup(kv, H, KV, D, P, seqs, n):
     """Neighbouring queries go through the union of their picks: any picks, some of them outside, none at all."""
     rng = np.random.RandomState(n + D)
@@ -436,10 +438,11 @@ def test_queries_that_share_a_workgroup(kv, H, KV, D, P, seqs, n):
     compare(out, lse, *ref, tolerance("bf16", values))
 
 
+@pytest.mark.parametrize("P", [64, 32])
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
-def test_queries_that_share_a_workgroup_keep_odd_values_apart(kv, bad):
+def test_queries_that_share_a_workgroup_keep_odd_values_apart(kv, bad, P):
     """A page with such values is seen by the queries that picked it and by no other of the same workgroup."""
-    H, KV, D, P, prefix, n = 32, 8, 128, 64, 400, 70
+    H, KV, D, prefix, n = 32, 8, 128, 400, 70
     pool, index, keys, values = make_cache(kv, "bf16", KV, D, P, [prefix + n], seed=2)
     table = index.table.cpu().numpy()[0]
     for key, d in ((70, 3), (200, 127), (prefix + 20, 64), (prefix + 69, 0)):
