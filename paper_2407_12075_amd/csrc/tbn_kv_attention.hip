@@ -22,6 +22,8 @@
 // A key that a row does not see: its logit is replaced, not added to.  Its value is still multiplied by a weight of 0, so
 // in steps that hold such keys values behind the last visible key are replaced by 0, and if another value of the step is
 // infinite or not a number it is replaced by 0 too and a third product counts, for each row, the ones that it sees.
+#include <cmath>
+
 #include "tbn_kv_attention.h"
 
 namespace tbn {
@@ -426,13 +428,17 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, 
     pl.row_tiles = static_cast<int>(ceil_div(rows, pl.rows));
     const int64_t blocks = groups * pl.row_tiles;
     // Stretches of keys.  The staged kernel has two workgroups per CU and is bound by the matrix cores: one round of them (64 drafted tokens
-    // on 131000 keys: 188 us, in four rounds 227).  Here many small ones even out ragged lengths (64 sequences of 4096 - 16384 keys: 465 us in
-    // 8192 stretches, 534 in 512), but not below 1024 keys while those make 512 workgroups (16 sequences, 16 rows: 153 us, with 256 keys 167),
-    // and down to one step of each wave where even they do not (one token on 513 keys: 10.5 us, with 256 keys 11.9; on 16000: 20.4, with 128
-    // keys 23.4).
+    // on 131000 keys: 188 us, in four rounds 227).  Here lengths are ragged, and many short stretches even them out (64 sequences of 4096 -
+    // 16384 keys: 465 us in 8192 stretches, 534 in 512), against the cost of starting, ending and joining each.
     int64_t chunk = ceil_div(units, ceil_div(pl.staged ? 512 : 8192, blocks));
     if (!picked && !pl.staged) {
-        const int64_t fill = ceil_div(units * blocks, 512), least = fill < 1024 ? fill : 1024;
+        // fill: the stretch that gives each place for a workgroup one.  Beyond 256 keys several stretches a place: with a cost of c keys each and
+        // about half a stretch idle at the end, the best length grows as sqrt(2 c fill); c of 32 was measured (34 sequences of up to 3698
+        // keys, float32: 72 us with 256 keys, 97 with 1024; 16 of 16000, 16 rows: 155 us with 512 - 1024, 168 with 256).  Below, the nearest
+        // multiple of a step of each wave (9 sequences of 15000 keys: 18.9 us with 256 keys, 21.7 with 384, 22.5 with 128).
+        const double fill = static_cast<double>(units) * blocks / (padded_dim(p.dim) == 256 ? 256 : 512);
+        const double want = fill <= 256 ? fill : std::fmax(256, std::fmin(1024, 8 * std::sqrt(fill)));
+        const int64_t least = static_cast<int64_t>(want / unit_step + 0.5) * unit_step;
         if (chunk < least) chunk = least;
         // short sequences that fill the CUs: not split, the join would take longer (40 sequences of 600 keys, 8 kv heads: 20 us, 24 in parts)
         if (units <= 1024 && blocks >= 256) chunk = units;
