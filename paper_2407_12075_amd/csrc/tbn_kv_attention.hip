@@ -418,7 +418,20 @@ int most_rows(const tbn_kv_pool &p) { return p.dt == TBN_BF16 || padded_dim(p.di
 Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, int64_t unit_step, int64_t unit_most, bool picked) {
     // units: keys or picks to split, unit_step: the least stretch, a multiple of which a chunk is
     Plan pl;
-    pl.staged = !picked && p.dt == TBN_BF16 && rows > 16;
+    const int64_t places = padded_dim(p.dim) == 256 ? 256 : 512;   // for workgroups at a time: the least of both kernels
+    // fill: keys that give each place for a workgroup one stretch.  Short sequences that fill the CUs are not split.
+    const double fill = static_cast<double>(units) * groups / places;
+    const bool whole = units <= 1024 && groups >= 256;
+    // one round of the staged kernel: as many stretches as fit, where they take 7/8 of the places; otherwise a few more than fit
+    const int64_t fit = places / groups;
+    const bool round = fit * groups * 8 >= places * 7;
+    // Up to 16 rows and 128 channels the staged kernel's waves read each byte of the cache for one another and its loads run further ahead: it is
+    // the faster one as soon as each place has more than 256 keys of its own and one round takes the work (16 sequences of 16000 keys,
+    // 4 - 7 rows: 130 us, 143 - 150 in the other; 8 of 3000, 22 to 26; 100 of 1500 with 16 rows, 95 to 114).  Below, and where a round ends
+    // half full, the other one's short stretches win (4 of 2000: 14.1 us to 15.0; 34 of 3698: 79 to 92; 200 of 300: 45 to 59).  With 64
+    // and 256 channels they measure alike.
+    const bool few = rows <= 16 && padded_dim(p.dim) == 128 && p.dim > 96 && fill > 256 && !whole && (groups >= places || round);
+    pl.staged = !picked && p.dt == TBN_BF16 && (rows > 16 || few);
     if (pl.staged) {
         pl.rows = rows <= 64 ? 64 : 128;
     } else {
@@ -427,20 +440,20 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, 
     }
     pl.row_tiles = static_cast<int>(ceil_div(rows, pl.rows));
     const int64_t blocks = groups * pl.row_tiles;
-    // Stretches of keys.  The staged kernel has two workgroups per CU and is bound by the matrix cores: one round of them (64 drafted tokens
-    // on 131000 keys: 188 us, in four rounds 227).  Here lengths are ragged, and many short stretches even them out (64 sequences of 4096 -
-    // 16384 keys: 465 us in 8192 stretches, 534 in 512), against the cost of starting, ending and joining each.
-    int64_t chunk = ceil_div(units, ceil_div(pl.staged ? 512 : 8192, blocks));
+    // Stretches of keys.  The staged kernel takes one round of the places (64 drafted tokens on 131000 keys: 188 us, in four rounds 227), two
+    // where a stretch would be longer than 8192 keys: lengths are ragged, and two even them out (64 sequences of 4096 - 16384 keys: 456 us, 490 in
+    // one round, 462 in the other kernel).  Here many short stretches even them out, against the cost of starting, ending and joining each.
+    const int64_t parts = (few && round ? fit : ceil_div(places, blocks)) * (few && fill > 8192 ? 2 : 1);
+    int64_t chunk = ceil_div(units, pl.staged ? parts : ceil_div(8192, blocks));
     if (!picked && !pl.staged) {
-        // fill: the stretch that gives each place for a workgroup one.  Beyond 256 keys several stretches a place: with a cost of c keys each and
-        // about half a stretch idle at the end, the best length grows as sqrt(2 c fill); c of 32 was measured (34 sequences of up to 3698
-        // keys, float32: 72 us with 256 keys, 97 with 1024; 16 of 16000, 16 rows: 155 us with 512 - 1024, 168 with 256).  Below, the nearest
-        // multiple of a step of each wave (9 sequences of 15000 keys: 18.9 us with 256 keys, 21.7 with 384, 22.5 with 128).
-        const double fill = static_cast<double>(units) * blocks / (padded_dim(p.dim) == 256 ? 256 : 512);
-        const double want = fill <= 256 ? fill : std::fmax(256, std::fmin(1024, 8 * std::sqrt(fill)));
+        // Beyond 256 keys several stretches a place: with a cost of c keys each and about half a stretch idle at the end, the best length grows
+        // as sqrt(2 c fill); c of 32 was measured (34 sequences of up to 3698 keys, float32: 72 us with 256 keys, 97 with 1024; 16 of 16000,
+        // 16 rows: 155 us with 512 - 1024, 168 with 256).  Below, the nearest multiple of a step of each wave (9 sequences of 15000 keys: 18.9 us
+        // with 256 keys, 21.7 with 384, 22.5 with 128).
+        const double want = fill * pl.row_tiles <= 256 ? fill * pl.row_tiles : std::fmax(256, std::fmin(1024, 8 * std::sqrt(fill * pl.row_tiles)));
         const int64_t least = static_cast<int64_t>(want / unit_step + 0.5) * unit_step;
         if (chunk < least) chunk = least;
-        // short sequences that fill the CUs: not split, the join would take longer (40 sequences of 600 keys, 8 kv heads: 20 us, 24 in parts)
+        // not split, the join would take longer (40 sequences of 600 keys, 8 kv heads: 20 us, 24 in parts)
         if (units <= 1024 && blocks >= 256) chunk = units;
     }
     chunk = ceil_div(chunk, unit_step) * unit_step;

@@ -117,6 +117,25 @@ def test_keys_split_over_workgroups(kv, H, KV, D, P, seqs, dt):
         assert torch.equal(out, again) and torch.equal(lse, lse2)
 
 
+@pytest.mark.parametrize("H,KV,D,P,seqs", [
+    (4, 4, 128, 64, [(33000, 1), (0, 1), (700, 1)]),                        # one row, stretches that most sequences do not reach
+    (8, 8, 104, 128, [(17100, 2)]),                                         # channels that end inside an operand
+    (10, 2, 128, 32, [(9001, 3)] * 8),                                      # 15 rows, pages of half a step
+    (64, 64, 128, 64, [(1500, 1), (1, 1), (1023, 2), (0, 0), (64, 1), (2, 2), (130, 1), (640, 1)])])   # a stretch is a sequence
+def test_few_rows_on_many_keys(kv, H, KV, D, P, seqs):
+    """bfloat16, few rows, enough keys for every CU: the kernel that stages keys in LDS."""
+    counts = [n for _, n in seqs]
+    pool, index, keys, values = make_cache(kv, "bf16", KV, D, P, [p + n for p, n in seqs], seed=8)
+    q, cu, qs = make_queries("bf16", counts, H, D)
+    see = masks("any", counts, 4)
+    mask = pack_mask(np.concatenate([np.pad(m, ((0, 0), (0, 32 - m.shape[1]))) for m in see]), 1)
+    ref = reference(qs, keys, values, counts, see, 1 / math.sqrt(D))
+    out, lse = kv.tbn_tree_attention(q, pool, index, cu, max(counts), mask=mask)
+    compare(out, lse, *ref, tolerance("bf16", values))
+    again, lse2 = kv.tbn_tree_attention(q, pool, index, cu, max(counts), mask=mask)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
 def test_what_a_query_does_not_see_has_no_part(kv, dt, bad):
