@@ -456,6 +456,9 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, 
         // not split, the join would take longer (40 sequences of 600 keys, 8 kv heads: 20 us, 24 in parts)
         if (units <= 1024 && blocks >= 256) chunk = units;
     }
+    // Nor up to 80 KB of keys: the join's launch takes longer than the steps it saves (one sequence, 8 kv heads of 128 channels, bfloat16: 200
+    // keys 8.0 us, 10.2 in parts; 300 keys 9.3 to 10.2; 513 keys 12.4 to 10.4).
+    if (!pl.staged && units * (picked ? p.page : 1) * padded_dim(p.dim) * (p.dt == TBN_F32 ? 4 : 2) <= 80 * 1024) chunk = units;
     chunk = ceil_div(chunk, unit_step) * unit_step;
     if (chunk > unit_most) chunk = unit_most;
     pl.chunk = static_cast<int>(chunk);

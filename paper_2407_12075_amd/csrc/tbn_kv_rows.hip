@@ -209,6 +209,8 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
                 __syncthreads();
             }
         }
+        // these products go before the softmax of the SIMD's other wave (64 drafted tokens on 131000 keys: 186 us, 191 without)
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int t = 0; t < TILES; ++t)
 #pragma unroll
@@ -226,6 +228,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
                     o[f] = mma(*reinterpret_cast<const u32x4_t *>(vt + d * KEYS + (c ^ v_swap(d)) * 8), pw, o[f]);
                 }
             }
+        __builtin_amdgcn_s_setprio(0);
     };
 
     __syncthreads();
