@@ -136,6 +136,18 @@ def test_few_rows_on_many_keys(kv, H, KV, D, P, seqs):
     assert torch.equal(out, again) and torch.equal(lse, lse2)
 
 
+@pytest.mark.parametrize("H,KV,D", [(4, 2, 256), (2, 1, 128), (6, 6, 64)])
+def test_float32_is_not_lost_in_long_sums(kv, H, KV, D):
+    """A logit of magnitude up to 8 is summed in chains of at most 64 products: about sqrt(64) roundings of 2^-24 of it, 8 * 8 * 2^-24 / 2 = 2e-6 at worst
+    and a fifth of that in the mean, since the partial sums are mostly smaller; it is what a weight is off by."""
+    pool, index, keys, values = make_cache(kv, "f32", KV, D, 64, [1814, 700], seed=3)
+    q, cu, qs = make_queries("f32", [1, 1], H, D)
+    out, _ = kv.tbn_tree_attention(q, pool, index, cu, 1)
+    ref, _ = reference(qs, keys, values, [1, 1], masks("chain", [1, 1], 0), 1 / math.sqrt(D))
+    err = np.linalg.norm(out.double().cpu().numpy() - ref) / np.linalg.norm(ref)
+    assert err <= 1e-6, f"{err:.2e}"
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
 def test_what_a_query_does_not_see_has_no_part(kv, dt, bad):
