@@ -25,7 +25,7 @@ namespace {
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 
-__device__ __attribute__((aligned(16))) const uint32_t kZeros[4] = {0, 0, 0, 0};   // channels beyond the head's
+__device__ __attribute__((aligned(16))) const uint32_t kZeros[4] = {0, 0, 0, 0};   // pieces beyond the head's channels
 
 __device__ __forceinline__ f32x16_t mma(u32x4_t a, u32x4_t b, f32x16_t c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
@@ -39,6 +39,7 @@ template <int DP, int RW, bool EVEN>
 __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kernel(AttentionArgs a) {
     constexpr int KW = kAttnWaves / RW, KEYS = DP == 256 && KW == 1 ? 32 : 64, TILES = KEYS / 32 / KW;
     constexpr int PITCH = DP == 96 ? 128 : DP;                     // channels of a row of K in LDS
+    constexpr bool FULL = EVEN && PITCH == DP;                     // every piece of such a row is the head's
     constexpr int KP = PITCH / 8, VP = KEYS / 8;                   // 16-byte pieces of a row of K, of V^T
     constexpr int NK = KEYS * KP / kAttnThreads, NV = DP * VP / kAttnThreads;
     constexpr int NQ = DP / 16, ND = DP / 32;
@@ -84,7 +85,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
     for (int j = 0; j < NK; ++j) {
         const int L = (j * kAttnWaves + wave) * kWave + lane, r = L / KP, c = (L % KP) ^ (r & 7);
         k_from[j] = (((r & ~31) + key_of_row(r & 31)) * D + c * 8) * 2;
-        k_there[j] = EVEN || c * 8 < D;
+        k_there[j] = FULL || c * 8 < D;
     }
     auto v_swap = [](int d) { return KEYS == 64 ? d & 7 : (d >> 1) & 3; };
 #pragma unroll
@@ -109,7 +110,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
 #pragma unroll
         for (int j = 0; j < NK; ++j) {
             const char *from = ((j * kAttnThreads) / KP >= 32 ? kb : ka) + k_from[j];
-            if (!EVEN) from = k_there[j] ? from : reinterpret_cast<const char *>(kZeros);
+            if (!FULL) from = k_there[j] ? from : reinterpret_cast<const char *>(kZeros);
             __builtin_amdgcn_global_load_lds((global_ptr)from, (lds_ptr)(kt + (j * kAttnWaves + wave) * (kWave * 8)), 16, 0, 0);
         }
         const char *vl = late ? vb : va;
