@@ -22,7 +22,7 @@ from typing import Optional, Tuple
 import torch
 
 from . import tbn
-from .tbn import _call, _dev, _dt, _own, _raise, _stream, lib, TBN_OK
+from .tbn import _call, _dev, _dt, _empty, _own, _raise, _stream, lib, TBN_OK
 
 TBN_KV_FULL = 1
 TBN_KV_INVALID = 2
@@ -120,11 +120,11 @@ def _agree(pool: KVPool, index: KVIndex):
         raise ValueError(f"pool and index must live on one device, got {pool.device} and {index.device}")
 
 
-def _workspace(need: int, workspace: Optional[torch.Tensor], device: torch.device):
+def _workspace(need: int, workspace: Optional[torch.Tensor], device: torch.device, stream):
     if workspace is None:
         if need == 0:
             return None, 0
-        workspace = _own(torch.empty(need, dtype=torch.uint8, device=device))
+        workspace = _own(_empty(need, torch.uint8, device, stream, output=False))
     else:
         _same_device(device, workspace)
     return _dev(workspace, "workspace"), workspace.numel() * workspace.element_size()
@@ -146,8 +146,8 @@ def tbn_kv_reserve(index: KVIndex, n_new: torch.Tensor, workspace: Optional[torc
         r = tbn._host.kv_reserve(index._at, index._gpu, n_new)
         if r is not None:
             return r
-    pairs = torch.empty((2, index.n_seqs), dtype=torch.int32, device=index.device)
-    ws, size = _workspace(index._ws, workspace, index.device)
+    pairs = _empty((2, index.n_seqs), torch.int32, index.device, stream)
+    ws, size = _workspace(index._ws, workspace, index.device, stream)
     at = pairs.data_ptr()
     _done(_call("tbn_kv_reserve", index._at, _ints(n_new, "n_new", index.n_seqs, index.device), at, at + 4 * index.n_seqs, ws, size, _stream(stream)))
     return pairs[0], pairs[1]
@@ -173,8 +173,8 @@ def tbn_kv_release(index: KVIndex, keep: torch.Tensor, stream=None) -> None:
 def tbn_kv_compact(index: KVIndex, workspace: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """Used pages go to the lowest numbers; returns (src, dst, count) for tbn_kv_copy_pages."""
     half = max(index.n_pages // 2, 1)
-    moves = torch.empty(2 * half + 1, dtype=torch.int32, device=index.device)
-    ws, size = _workspace(index._ws, workspace, index.device)
+    moves = _empty(2 * half + 1, torch.int32, index.device, stream)
+    ws, size = _workspace(index._ws, workspace, index.device, stream)
     at = moves.data_ptr()
     _done(_call("tbn_kv_compact", index._at, at, at + 4 * half, at + 8 * half, ws, size, _stream(stream)))
     return moves[:half], moves[half:2 * half], moves[2 * half:]
@@ -222,13 +222,13 @@ def _queries(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: torch.Tensor):
     return at, stride, _ints(cu_q, "cu_q", index.n_seqs + 1, index.device)
 
 
-def _outputs(q: torch.Tensor, out: Optional[torch.Tensor], lse: Optional[torch.Tensor]):
+def _outputs(q: torch.Tensor, out: Optional[torch.Tensor], lse: Optional[torch.Tensor], stream):
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = _empty(q.shape, q.dtype, q.device, stream)
     elif out.shape != q.shape or out.dtype != q.dtype or out.device != q.device:
         raise ValueError("out must have q's shape, dtype and device")
     if lse is None:
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        lse = _empty(q.shape[:2], torch.float32, q.device, stream)
     elif lse.shape != q.shape[:2] or lse.device != q.device:
         raise ValueError("lse must be (tokens, heads) on q's device")
     return out, lse
@@ -248,7 +248,7 @@ def tbn_tree_attention(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: torc
         if r is not None:
             return r
     at, stride, cu = _queries(q, pool, index, cu_q)
-    out, lse = _outputs(q, out, lse)
+    out, lse = _outputs(q, out, lse, stream)
     words = 0
     if mask is not None:
         if mask.dim() != 2 or mask.shape[0] != q.shape[0]:
@@ -256,7 +256,7 @@ def tbn_tree_attention(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: torc
         words = mask.shape[1]
         _same_device(q.device, mask)
     need = int(lib().tbn_tree_attention_workspace_bytes(pool._at, index._at, q.shape[0], max_q, q.shape[1], max_len or 0))
-    ws, size = _workspace(need, workspace, q.device)
+    ws, size = _workspace(need, workspace, q.device, stream)
     _done(_call("tbn_tree_attention", at, stride, _dev(out, "out"), _dev(lse, "lse", torch.float32), pool._at, index._at, cu, q.shape[0], max_q, q.shape[1],
                 None if mask is None else _dev(mask, "mask", torch.int32), words, max_len or 0, 1.0 / math.sqrt(pool.dim) if scale is None else scale, ws, size,
                 _stream(stream)))
@@ -278,11 +278,11 @@ def tbn_block_select(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: torch.
     at, stride, cu = _queries(q, pool, index, cu_q)
     shape = (q.shape[0], pool.kv_heads, n_select)
     if picks is None:
-        picks = torch.empty(shape, dtype=torch.int32, device=q.device)
+        picks = _empty(shape, torch.int32, q.device, stream)
     elif tuple(picks.shape) != shape or picks.device != q.device:
         raise ValueError(f"picks must be {shape} on {q.device}")
     need = int(lib().tbn_block_select_workspace_bytes(pool._at, index._at, q.shape[0], max_q, q.shape[1], max_len or 0))
-    ws, size = _workspace(need, workspace, q.device)
+    ws, size = _workspace(need, workspace, q.device, stream)
     _done(_call("tbn_block_select", at, stride, _dev(picks, "picks", torch.int32), pool._at, index._at, cu, q.shape[0], max_q, q.shape[1], n_select, n_sink,
                 n_recent, max_len or 0, ws, size, _stream(stream)))
     return picks
@@ -301,13 +301,13 @@ def tbn_block_attention(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: tor
         if r is not None:
             return r
     at, stride, cu = _queries(q, pool, index, cu_q)
-    out, lse = _outputs(q, out, lse)
+    out, lse = _outputs(q, out, lse, stream)
     if picks.dim() != 3 or tuple(picks.shape[:2]) != (q.shape[0], pool.kv_heads):
         raise ValueError("picks must be (tokens, kv_heads, n_select)")
     _same_device(q.device, picks)
     n = picks.shape[2]
     need = int(lib().tbn_block_attention_workspace_bytes(pool._at, index._at, q.shape[0], max_q, q.shape[1], n))
-    ws, size = _workspace(need, workspace, q.device)
+    ws, size = _workspace(need, workspace, q.device, stream)
     _done(_call("tbn_block_attention", at, stride, _dev(out, "out"), _dev(lse, "lse", torch.float32), pool._at, index._at, cu, q.shape[0], max_q, q.shape[1],
                 _dev(picks, "picks", torch.int32), n, 1.0 / math.sqrt(pool.dim) if scale is None else scale, ws, size, _stream(stream)))
     return out, lse

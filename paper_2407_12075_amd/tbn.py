@@ -204,6 +204,24 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _empty(shape, dtype: torch.dtype, device: torch.device, stream=None, output: bool = True) -> torch.Tensor:
+    """Memory that a call on `stream` (None: the current one) writes.  It comes from that stream's share of the allocator: the current
+    stream's may hand out a block that its own unfinished work still uses, or hand on a workspace that is dropped here while `stream` still
+    writes to it.  An output is the caller's, so its block waits for the current stream, too, when it is dropped."""
+    if stream is None or device.type != "cuda":
+        return torch.empty(shape, dtype=dtype, device=device)
+    here, handle = torch.cuda.current_stream(device), _stream(stream)
+    if handle == here.cuda_stream:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if output:
+        t.record_stream(here)
+    return t
+
+
 def _dev(t: torch.Tensor, name: str, dtype=None) -> int:
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
@@ -259,14 +277,14 @@ def tbn_pack_tile(w_real: torch.Tensor, k: int, n_alpha: int = 1, a_real: Option
     words = tbn_tile_words(n, k)
     dev = w_real.device
     if tile_out is None:
-        tile_out = torch.empty(max(words, 1), dtype=torch.int32, device=dev)
+        tile_out = _empty(max(words, 1), torch.int32, dev, stream)
     if alpha_out is None:
-        alpha_out = torch.empty(max(n_alpha, 1), dtype=torch.float32, device=dev)
+        alpha_out = _empty(max(n_alpha, 1), torch.float32, dev, stream)
     need = tbn_pack_workspace_bytes(n, k, n_alpha)
     if workspace is None:
         if _recording is not None:
             raise ValueError("tbn_bind(tbn_pack_tile, ...): pass the workspace (the bound call does not own one)")
-        workspace = torch.empty(max(need, 8), dtype=torch.uint8, device=dev)
+        workspace = _empty(max(need, 8), torch.uint8, dev, stream, output=False)
     if tile_out.numel() < words or alpha_out.numel() < n_alpha or any(t.device != dev for t in (tile_out, alpha_out, workspace)) \
             or (a_real is not None and (a_real.numel() != n or a_real.device != dev)):
         raise ValueError("tbn_pack_tile: tile_out, alpha_out, a_real or workspace too small or on another device")
@@ -305,7 +323,7 @@ def tbn_linear_forward(x: torch.Tensor, tile: torch.Tensor, alpha: torch.Tensor,
         raise ValueError("x must be (M, in)")
     M, cin = x.shape
     if y is None:
-        y = torch.empty((M, out_features), dtype=x.dtype, device=x.device)
+        y = _empty((M, out_features), x.dtype, x.device, stream)
     elif tuple(y.shape) != (M, out_features) or y.dtype != x.dtype:
         raise ValueError("y must be (M, out) with x's dtype")
     _check_layer_tensors("tbn_linear_forward", x, tile, alpha, cin * out_features, k, y)
@@ -338,7 +356,7 @@ def tbn_linear_forward_ws(x: torch.Tensor, tile: torch.Tensor, alpha: torch.Tens
         raise ValueError("x must be (M, in)")
     M, cin = x.shape
     if y is None:
-        y = torch.empty((M, out_features), dtype=x.dtype, device=x.device)
+        y = _empty((M, out_features), x.dtype, x.device, stream)
     elif tuple(y.shape) != (M, out_features) or y.dtype != x.dtype:
         raise ValueError("y must be (M, out) with x's dtype")
     _check_layer_tensors("tbn_linear_forward_ws", x, tile, alpha, cin * out_features, k, y, workspace)
@@ -363,11 +381,11 @@ def tbn_pack_coltile(w_real: torch.Tensor, k: int, n_alpha: int = 1, a_real: Opt
         raise ValueError("w_real must be (out, in)")
     out, cin = w_real.shape
     dev = w_real.device
-    tile_out = torch.empty(max(tbn_tile_words(out * cin, k), 1), dtype=torch.int32, device=dev)
-    alpha_out = torch.empty(max(n_alpha, 1), dtype=torch.float32, device=dev)
+    tile_out = _empty(max(tbn_tile_words(out * cin, k), 1), torch.int32, dev, stream)
+    alpha_out = _empty(max(n_alpha, 1), torch.float32, dev, stream)
     need = int(lib().tbn_pack_coltile_workspace_bytes(out, cin, k, n_alpha))
     if workspace is None:
-        workspace = _own(torch.empty(max(need, 8), dtype=torch.uint8, device=dev))
+        workspace = _own(_empty(max(need, 8), torch.uint8, dev, stream, output=False))
     st = _call("tbn_pack_coltile", _dev(w_real, "w_real", torch.float32),
                                 None if a_real is None else _dev(a_real, "a_real", torch.float32),
                                 out, cin, k, n_alpha, _dev(tile_out, "tile_out", torch.int32),
@@ -394,11 +412,11 @@ def tbn_linear_coltiled_forward(x: torch.Tensor, tile: torch.Tensor, alpha: torc
         raise ValueError("x must be (M, in)")
     M, cin = x.shape
     if y is None:
-        y = torch.empty((M, out_features), dtype=x.dtype, device=x.device)
+        y = _empty((M, out_features), x.dtype, x.device, stream)
     elif tuple(y.shape) != (M, out_features) or y.dtype != x.dtype:
         raise ValueError("y must be (M, out) with x's dtype")
     if workspace is None:
-        workspace = _own(torch.empty(max(tbn_linear_coltiled_workspace_bytes(x, k), 16), dtype=torch.uint8, device=x.device))
+        workspace = _own(_empty(max(tbn_linear_coltiled_workspace_bytes(x, k), 16), torch.uint8, x.device, stream, output=False))
     _check_layer_tensors("tbn_linear_coltiled_forward", x, tile, alpha, cin * out_features, k, y, workspace)
     st = _call("tbn_linear_coltiled_forward", _dev(x, "x"), _dev(y, "y"), _dt(x), M, cin, out_features,
                                            _dev(tile, "tile", torch.int32), k, _dev(alpha, "alpha", torch.float32),
@@ -422,7 +440,7 @@ def tbn_conv2d_forward(x: torch.Tensor, tile: torch.Tensor, alpha: torch.Tensor,
     N, C, H, W = x.shape
     Ho, Wo = conv_out_hw(H, W, kh, kw, stride, pad)
     if y is None:
-        y = torch.empty((N, out_channels, max(Ho, 0), max(Wo, 0)), dtype=x.dtype, device=x.device)
+        y = _empty((N, out_channels, max(Ho, 0), max(Wo, 0)), x.dtype, x.device, stream)
     elif tuple(y.shape) != (N, out_channels, Ho, Wo) or y.dtype != x.dtype:
         raise ValueError("y must be (N, O, Ho, Wo) with x's dtype")
     _check_layer_tensors("tbn_conv2d_forward", x, tile, alpha, out_channels * C * kh * kw, k, y)
@@ -457,7 +475,7 @@ def tbn_sign_pack(x: torch.Tensor, xbits: Optional[torch.Tensor] = None, stream=
     M, cin = x.shape
     words = tbn_sign_row_words(cin)
     if xbits is None:
-        xbits = torch.empty((M, words), dtype=torch.int32, device=x.device)
+        xbits = _empty((M, words), torch.int32, x.device, stream)
     elif tuple(xbits.shape) != (M, words) or xbits.device != x.device:
         raise ValueError(f"xbits must be ({M}, {words}) on {x.device}")
     st = _call("tbn_sign_pack", _dev(x, "x"), _dt(x), M, cin, _dev(xbits, "xbits", torch.int32), _stream(stream))
@@ -482,7 +500,7 @@ def tbn_linear_forward_binact(xbits: torch.Tensor, cin: int, tile: torch.Tensor,
     else:
         shape, ydt = (M, out_features), dtype
     if y is None:
-        y = torch.empty(shape, dtype=ydt, device=xbits.device)
+        y = _empty(shape, ydt, xbits.device, stream)
     elif tuple(y.shape) != shape or (flags & TBN_FLAG_SIGN_OUT and y.dtype != torch.int32):
         raise ValueError(f"y must be {shape}" + (" int32" if flags & TBN_FLAG_SIGN_OUT else ""))
     _check_layer_tensors("tbn_linear_forward_binact", xbits, tile, alpha, cin * out_features, k, y)
