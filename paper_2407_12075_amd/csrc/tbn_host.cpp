@@ -303,6 +303,13 @@ const at::Tensor *rows(PyObject *o, const Held &pool, int64_t heads, int64_t &st
     return &t;
 }
 
+// the library's call, without the interpreter's lock: a launch may wait for room in a queue
+template <typename Call>
+tbn_status unlocked(Call call) {
+    pybind11::gil_scoped_release no_gil;
+    return call();
+}
+
 PyObject *none(tbn_status st) {
     if (st == TBN_OK) Py_RETURN_TRUE;   // done, nothing to return (None would be "not taken")
     PyObject *r = PyObject_CallFunction(g_raise, "i", static_cast<int>(st));
@@ -324,7 +331,9 @@ PyObject *kv_reserve(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     at::Tensor src = at::empty({n}, like.options()), dst = at::empty({n}, like.options());
     const size_t need = p_kv_workspace_bytes(index_of(ix)->n_pages, static_cast<int32_t>(n));
     at::Tensor ws = bytes_like(like, need);
-    const tbn_status st = p_kv_reserve(index_of(ix), fresh, static_cast<int32_t *>(src.data_ptr()), static_cast<int32_t *>(dst.data_ptr()), ws.data_ptr(), need, stream());
+    const tbn_status st = unlocked([&] {
+        return p_kv_reserve(index_of(ix), fresh, static_cast<int32_t *>(src.data_ptr()), static_cast<int32_t *>(dst.data_ptr()), ws.data_ptr(), need, stream());
+    });
     return result(st, two, src, dst);
     END_HANDLE_TH_ERRORS
 }
@@ -338,7 +347,7 @@ PyObject *kv_fork(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     if (!a || !b) Py_RETURN_NONE;
     const int64_t n = THPVariable_Unpack(args[2]).numel();
     if (THPVariable_Unpack(args[3]).numel() != n || n > INT32_MAX) Py_RETURN_NONE;
-    return none(p_kv_fork(index_of(ix), a, b, static_cast<int32_t>(n), stream()));
+    return none(unlocked([&] { return p_kv_fork(index_of(ix), a, b, static_cast<int32_t>(n), stream()); }));
     END_HANDLE_TH_ERRORS
 }
 
@@ -349,7 +358,7 @@ PyObject *kv_release(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     if (n_args != 3 || !ordinary_context() || !held(args[0], args[1], ix)) Py_RETURN_NONE;
     const int32_t *keep = ints(args[2], index_of(ix)->n_seqs, ix.gpu);
     if (!keep) Py_RETURN_NONE;
-    return none(p_kv_release(index_of(ix), keep, stream()));
+    return none(unlocked([&] { return p_kv_release(index_of(ix), keep, stream()); }));
     END_HANDLE_TH_ERRORS
 }
 
@@ -362,7 +371,7 @@ PyObject *kv_copy_pages(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     if (!a || !b || (!count && args[4] != Py_None)) Py_RETURN_NONE;
     const int64_t n = THPVariable_Unpack(args[2]).numel();
     if (THPVariable_Unpack(args[3]).numel() != n) Py_RETURN_NONE;
-    return none(p_kv_copy_pages(pool_of(pool), a, b, n, count, stream()));
+    return none(unlocked([&] { return p_kv_copy_pages(pool_of(pool), a, b, n, count, stream()); }));
     END_HANDLE_TH_ERRORS
 }
 
@@ -375,7 +384,7 @@ PyObject *kv_append(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     const at::Tensor *k = rows(args[4], pool, pool_of(pool)->kv_heads, ks), *v = rows(args[5], pool, pool_of(pool)->kv_heads, vs);
     const int32_t *cu = ints(args[6], int64_t(index_of(ix)->n_seqs) + 1, ix.gpu);
     if (!k || !v || !cu || k->size(0) != v->size(0) || !integer(args[7], 0, INT32_MAX, most)) Py_RETURN_NONE;
-    return none(p_kv_append(pool_of(pool), index_of(ix), k->data_ptr(), ks, v->data_ptr(), vs, cu, k->size(0), static_cast<int32_t>(most), stream()));
+    return none(unlocked([&] { return p_kv_append(pool_of(pool), index_of(ix), k->data_ptr(), ks, v->data_ptr(), vs, cu, k->size(0), static_cast<int32_t>(most), stream()); }));
     END_HANDLE_TH_ERRORS
 }
 
@@ -389,7 +398,7 @@ PyObject *kv_keep(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     if (!base || !picks || !counts) Py_RETURN_NONE;
     const at::Tensor &t = THPVariable_Unpack(args[5]);
     if (t.dim() != 2 || t.size(0) != n || t.size(1) > INT32_MAX) Py_RETURN_NONE;
-    return none(p_kv_keep(pool_of(pool), index_of(ix), base, picks, static_cast<int32_t>(t.size(1)), counts, stream()));
+    return none(unlocked([&] { return p_kv_keep(pool_of(pool), index_of(ix), base, picks, static_cast<int32_t>(t.size(1)), counts, stream()); }));
     END_HANDLE_TH_ERRORS
 }
 
@@ -438,9 +447,11 @@ PyObject *tree_attention(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     at::Tensor out = at::empty({n, heads, pool->dim}, a.q->options()), lse = at::empty({n, heads}, a.q->options().dtype(at::kFloat)), ws;
     const size_t need = p_tree_attention_workspace_bytes(pool, ix, n, static_cast<int32_t>(a.max_q), static_cast<int32_t>(heads), a.max_len);
     if (need) ws = bytes_like(*a.q, need);
-    const tbn_status st = p_tree_attention(a.q->data_ptr(), a.stride, out.data_ptr(), floats(lse), pool, ix, a.cu, n, static_cast<int32_t>(a.max_q),
-                                           static_cast<int32_t>(heads), reinterpret_cast<const uint32_t *>(mask), static_cast<int32_t>(words), a.max_len, scale,
-                                           need ? ws.data_ptr() : nullptr, need, stream());
+    const tbn_status st = unlocked([&] {
+        return p_tree_attention(a.q->data_ptr(), a.stride, out.data_ptr(), floats(lse), pool, ix, a.cu, n, static_cast<int32_t>(a.max_q),
+                                static_cast<int32_t>(heads), reinterpret_cast<const uint32_t *>(mask), static_cast<int32_t>(words), a.max_len, scale,
+                                need ? ws.data_ptr() : nullptr, need, stream());
+    });
     return result(st, two, out, lse);
     END_HANDLE_TH_ERRORS
 }
@@ -457,9 +468,11 @@ PyObject *block_select(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     at::Tensor picks = at::empty({n, pool->kv_heads, select}, a.q->options().dtype(at::kInt)), ws;
     const size_t need = p_block_select_workspace_bytes(pool, ix, n, static_cast<int32_t>(a.max_q), static_cast<int32_t>(heads), a.max_len);
     if (need) ws = bytes_like(*a.q, need);
-    const tbn_status st = p_block_select(a.q->data_ptr(), a.stride, static_cast<int32_t *>(picks.data_ptr()), pool, ix, a.cu, n, static_cast<int32_t>(a.max_q),
-                                         static_cast<int32_t>(heads), static_cast<int32_t>(select), static_cast<int32_t>(sink), static_cast<int32_t>(recent), a.max_len,
-                                         need ? ws.data_ptr() : nullptr, need, stream());
+    const tbn_status st = unlocked([&] {
+        return p_block_select(a.q->data_ptr(), a.stride, static_cast<int32_t *>(picks.data_ptr()), pool, ix, a.cu, n, static_cast<int32_t>(a.max_q),
+                              static_cast<int32_t>(heads), static_cast<int32_t>(select), static_cast<int32_t>(sink), static_cast<int32_t>(recent), a.max_len,
+                              need ? ws.data_ptr() : nullptr, need, stream());
+    });
     return result(st, one, picks, picks);
     END_HANDLE_TH_ERRORS
 }
@@ -481,8 +494,10 @@ PyObject *block_attention(PyObject *, PyObject *const *args, Py_ssize_t n_args) 
     at::Tensor out = at::empty({n, heads, pool->dim}, a.q->options()), lse = at::empty({n, heads}, a.q->options().dtype(at::kFloat)), ws;
     const size_t need = p_block_attention_workspace_bytes(pool, ix, n, static_cast<int32_t>(a.max_q), static_cast<int32_t>(heads), select);
     if (need) ws = bytes_like(*a.q, need);
-    const tbn_status st = p_block_attention(a.q->data_ptr(), a.stride, out.data_ptr(), floats(lse), pool, ix, a.cu, n, static_cast<int32_t>(a.max_q),
-                                            static_cast<int32_t>(heads), picks, select, scale, need ? ws.data_ptr() : nullptr, need, stream());
+    const tbn_status st = unlocked([&] {
+        return p_block_attention(a.q->data_ptr(), a.stride, out.data_ptr(), floats(lse), pool, ix, a.cu, n, static_cast<int32_t>(a.max_q),
+                                 static_cast<int32_t>(heads), picks, select, scale, need ? ws.data_ptr() : nullptr, need, stream());
+    });
     return result(st, two, out, lse);
     END_HANDLE_TH_ERRORS
 }
