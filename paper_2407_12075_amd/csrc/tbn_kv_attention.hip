@@ -532,6 +532,13 @@ float factor_of(float scale) {
 }
 uint32_t flip_of(const tbn_kv_pool &p, float scale) { return !(scale < 0.f) ? 0u : p.dt == TBN_F32 ? 0x80000000u : 0x80008000u; }
 
+constexpr int64_t kMostBlocks = 0x7fffffff;   // workgroups of a sequence
+
+tbn_status too_many(const char *what, int64_t blocks) {
+    set_error("%s: %lld workgroups per sequence are beyond one launch", what, (long long)blocks);
+    return TBN_ERR_UNSUPPORTED;
+}
+
 template <bool PICKED>
 tbn_status launch(AttentionArgs &a, const Plan &pl, float *ws, const char *what, hipStream_t stream) {
     a.chunk = pl.chunk;
@@ -541,10 +548,7 @@ tbn_status launch(AttentionArgs &a, const Plan &pl, float *ws, const char *what,
     a.part_o = ws;
     a.part_ml = reinterpret_cast<float4 *>(ws ? ws + parts * a.p.dim : nullptr);
     const int64_t x = int64_t(pl.n_chunks) * pl.row_tiles * a.p.kv_heads * (PICKED ? a.q.max_q : 1), jx = int64_t(a.q.max_q) * a.q.heads;
-    if (x > 0x7fffffffLL || jx > 0x7fffffffLL) {
-        set_error("%s: %lld workgroups per sequence are beyond one launch", what, (long long)(x > jx ? x : jx));
-        return TBN_ERR_UNSUPPORTED;
-    }
+    if (x > kMostBlocks || jx > kMostBlocks) return too_many(what, x > jx ? x : jx);
     const dim3 grid(static_cast<unsigned>(x), a.ix.n_seqs);
     if (pl.staged) launch_kv_rows(a, pl.rows / 32, grid, stream);
     else if (a.p.dt == TBN_F32) launch_dims<float, PICKED>(a, pl.rows, grid, stream);
@@ -573,13 +577,16 @@ size_t block_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, c
 tbn_status launch_block_attention(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, void *out, float *lse, const int32_t *picks,
                                   int32_t n_select, float scale, float *ws, hipStream_t stream) {
     AttentionArgs a{p, ix, q, out, lse, nullptr, 0, picks, n_select, factor_of(scale), flip_of(p, scale)};
+    const char *what = "tbn_block_attention";
     if (const int queries = picked_queries(p, ix, q, n_select)) {
         a.n_chunks = 1;
         a.row_tiles = static_cast<int>(ceil_div(q.max_q, queries));
-        launch_kv_picked(a, queries, dim3(static_cast<unsigned>(a.row_tiles * p.kv_heads), ix.n_seqs), stream);   // at most 2^30 / 2 * 1024 / 32
-        return check_launch("tbn_block_attention");
+        const int64_t x = int64_t(a.row_tiles) * p.kv_heads;
+        if (x > kMostBlocks) return too_many(what, x);
+        launch_kv_picked(a, queries, dim3(static_cast<unsigned>(x), ix.n_seqs), stream);
+        return check_launch(what);
     }
-    return launch<true>(a, picked_plan(p, q, n_select), ws, "tbn_block_attention", stream);
+    return launch<true>(a, picked_plan(p, q, n_select), ws, what, stream);
 }
 
 }  // namespace tbn
