@@ -449,8 +449,9 @@ tbn_status tbn_kv_keep(const tbn_kv_pool *pool, const tbn_kv_index *index, const
  *   out[i, h, :] = sum_j e^(a_j - m) v[j, h / G, :] / sum_j e^(a_j - m)   over the keys j that query i sees, m their maximum
  *   lse[i, h] = log sum_j e^(a_j)
  *
- * A query that sees no key gives out = 0 and lse = -infinity.  A key that a query does not see has no part in its result,
- * whatever it and its value hold.  Sums are binary32; for bfloat16 the factors e^(a_j - m) are rounded to bfloat16 in
+ * A query that sees no key, or only keys with a_j = -infinity, gives out = 0 and lse = -infinity.  One that sees an a_j of
+ * +infinity gives lse = +infinity and, infinity less infinity, not-a-number in out; one that sees a not-a-number, that in
+ * both.  A key that a query does not see has no part in its result, whatever it and its value hold.  Sums are binary32; for bfloat16 the factors e^(a_j - m) are rounded to bfloat16 in
  * both sums of out (not for lse), and out once, to nearest even.  The sum over keys may be split (by sizes, never by
  * chance): results are the same from run to run.
  *

@@ -128,15 +128,17 @@ def summary(k):
 
 
 def attention(q, k, v, see, scale):
-    """One query row (dim) over keys (n, dim); see: which of them.  (out, lse)"""
+    """One query row (dim) over keys (n, dim); see: which of them.  (out, lse).  Logits that are all -infinity have no weights: as if no key were seen."""
     see = np.asarray(see, bool)
     if not see.any():
         return np.zeros(v.shape[1]), -math.inf
     with np.errstate(invalid="ignore", over="ignore"):
         a = scale * (k[see] @ q)
         m = a.max()
+        if m == -math.inf:
+            return np.zeros(v.shape[1]), -math.inf
         p = np.exp(a - m)
-        return (p[:, None] * v[see]).sum(0) / p.sum(), m + math.log(p.sum())
+        return (p[:, None] * v[see]).sum(0) / p.sum(), m if m == math.inf else m + math.log(p.sum())
 
 
 def picks(q, codes, steps, own, n_select, n_sink, n_recent):

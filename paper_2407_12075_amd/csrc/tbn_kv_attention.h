@@ -1,5 +1,7 @@
 // What the attention kernels share (tbn_kv_attention.hip, tbn_kv_rows.hip): arguments, operands, masks.
 #pragma once
+#include <cfloat>
+
 #include "tbn_kv.h"
 
 namespace tbn {
@@ -194,6 +196,10 @@ __device__ __forceinline__ float add_two_bf16(uint32_t pair, float sum) {
 
 // 2^x: exact to one unit in the last place; results below 2^-126 are 0
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// What a row's logits are counted from.  Finite, so that a row that has seen nothing yet gives weights of 0 (-infinity less a finite number) and
+// an infinite logit one of infinity (infinity less infinity would be no number): its sum, and so lse, is infinity then.
+__device__ __forceinline__ float reference_of(float m) { return __builtin_amdgcn_fmed3f(m, -FLT_MAX, FLT_MAX); }
 
 // Which of a lane's `n` keys from `k0` on a row sees, as bits: keys before `end` and, among the call's own tokens, those of the row's mask
 // or up to its place.

@@ -236,7 +236,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
                 for (int f = 0; f < NF; ++f) o[r][f] *= keep;
                 m[r] = next_m;
             }
-            const float from = m[r] == -INFINITY ? 0.f : m[r];   // a row that has seen nothing yet: every weight is 0
+            const float from = reference_of(m[r]);
 #pragma unroll
             for (int e = 0; e < OF; ++e) {
                 p[r][e] = exp2_of(fmaf(p[r][e], a.c, -from));
@@ -305,7 +305,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
         float top = maxima[0][n];
 #pragma unroll
         for (int u = 1; u < kAttnWaves; ++u) top = fmaxf(top, maxima[u][n]);
-        const float f0 = top == -INFINITY ? 0.f : exp2_of(m[r] - top);
+        const float f0 = m[r] == top ? 1.f : exp2_of(m[r] - top);
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
             f32x4_t *at = reinterpret_cast<f32x4_t *>(&sums[r][wave][n][f * 16 + 4 * g]), sum = o[r][f] * f0;
@@ -323,7 +323,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
             float lsum = 0.f, zsum = 0.f;
 #pragma unroll
             for (int u = 0; u < kAttnWaves; ++u) {
-                const float f = best == -INFINITY ? 1.f : exp2_of(maxima[u][rr] - best);
+                const float f = maxima[u][rr] == best ? 1.f : exp2_of(maxima[u][rr] - best);
                 lsum += totals[0][u][rr] * f;
                 zsum += totals[1][u][rr] * f;
                 sum += *reinterpret_cast<const f32x4_t *>(&sums[r][u][rr][d]);

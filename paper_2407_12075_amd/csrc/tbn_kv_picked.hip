@@ -230,7 +230,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_picked_ker
                 for (int f = 0; f < ND; ++f) o[f] *= keep;
                 m = next_m;
             }
-            const float from = m == -INFINITY ? 0.f : m;
+            const float from = reference_of(m);
             u32x4_t pw[4];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {

@@ -164,7 +164,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
             for (int f = 0; f < ND; ++f) o[f] *= keep;
             m = next_m;
         }
-        const float from = m == -INFINITY ? 0.f : m;
+        const float from = reference_of(m);
 #pragma unroll
         for (int t = 0; t < TILES; ++t)
 #pragma unroll
