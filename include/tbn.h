@@ -457,11 +457,13 @@ tbn_status tbn_kv_keep(const tbn_kv_pool *pool, const tbn_kv_index *index, const
  *
  *   q        : DEVICE, total_q tokens of heads x dim elements of the pool's type, q_stride elements apart
  *   out      : DEVICE, total_q x heads x dim, dense;  lse : DEVICE, total_q x heads, or NULL
- *   cu_q     : DEVICE, n_seqs + 1, ascending from 0 to total_q;  max_q : at least the largest T
+ *   cu_q     : DEVICE, n_seqs + 1, ascending from 0 to total_q (idle sequences have none of the tokens);  max_q : at least
+ *              the largest T; like max_len, only speed depends on how near it is
  *   mask     : DEVICE, total_q x mask_words words (mask_words >= max_q / 32 rounded up), or NULL
  *   max_len  : at least the longest sequence (keys beyond it are not read), 0 for max_pages * page; only speed depends
  *              on how near it is
- *   workspace: DEVICE, 16-byte aligned, the bytes of the query for the same sizes (may be 0)
+ *   workspace: DEVICE, 16-byte aligned, the bytes of the query for the same sizes (may be 0; fewer tokens, whose keys are
+ *              split further, can need more)
  */
 size_t tbn_tree_attention_workspace_bytes(const tbn_kv_pool *pool, const tbn_kv_index *index, int64_t total_q, int32_t max_q,
                                           int32_t heads, int64_t max_len);

@@ -35,6 +35,7 @@ struct AttentionArgs {   // of one launch
     int32_t chunk;      // keys, or picks, of a workgroup
     int32_t n_chunks;
     int32_t row_tiles;  // tiles of a workgroup's rows
+    int32_t by_token;   // blockIdx.y is a token of the call, not a sequence
 };
 
 template <typename T> struct Elem;
@@ -147,6 +148,24 @@ __device__ __forceinline__ Span span_of(const AttentionArgs &a, int s) {
     v.len = len_in(a.ix.lens[s], a.q.max_len);
     v.prefix = max(v.len - max(all, 0), 0);
     return v;
+}
+
+// The sequence of a workgroup, -1 if there is nothing to do.  An index with more sequences than the call has tokens has idle ones: there the
+// launch has a row of workgroups for each token, and that of a sequence's first token does its work.  Their sequence is the last one that begins at or
+// before the token: 64 places are looked at in each round.
+__device__ __forceinline__ int sequence_of(const AttentionArgs &a) {
+    if (!a.by_token) return blockIdx.y;
+    const int token = blockIdx.y, lane = threadIdx.x & 63;
+    int from = 0, n = a.ix.n_seqs + 1;   // it is among these entries of cu_q
+    while (n > 1) {
+        const int step = (n + kWave - 1) / kWave;
+        const uint64_t before = __ballot(lane * step < n && a.q.cu_q[from + min(lane * step, n - 1)] <= token);
+        const int skip = max(__popcll(before) - 1, 0) * step;   // below n
+        from += skip;
+        n = min(step, n - skip);
+    }
+    from = __builtin_amdgcn_readfirstlane(from);
+    return from < a.ix.n_seqs && max(a.q.cu_q[from], 0) == token ? from : -1;
 }
 
 // A workgroup's share.  Heads vary fastest: neighbouring workgroups go to different XCDs, so every XCD gets the same mix of stretches (a

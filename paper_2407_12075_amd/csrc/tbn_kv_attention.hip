@@ -22,6 +22,7 @@
 // A key that a row does not see: its logit is replaced, not added to.  Its value is still multiplied by a weight of 0, so
 // in steps that hold such keys values behind the last visible key are replaced by 0, and if another value of the step is
 // infinite or not a number it is replaced by 0 too and a third product counts, for each row, the ones that it sees.
+#include <algorithm>
 #include <cmath>
 
 #include "tbn_kv_attention.h"
@@ -40,7 +41,9 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
     __shared__ float maxima[kAttnWaves][16], totals[2][kAttnWaves][16];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
-    const int s = blockIdx.y, H = a.q.heads, KV = a.p.kv_heads, G = H / KV, D = EVEN ? DP : a.p.dim, P = a.p.page;
+    const int s = sequence_of(a);
+    if (s < 0) return;
+    const int H = a.q.heads, KV = a.p.kv_heads, G = H / KV, D = EVEN ? DP : a.p.dim, P = a.p.page;
     const int shift = __ffs(P) - 1;
     const Span v = span_of(a, s);
     const Block blk = block_of(a);
@@ -342,7 +345,9 @@ __global__ __launch_bounds__(kAttnThreads) void kv_join_kernel(AttentionArgs a, 
     __shared__ f32x4_t sums[WIDE ? kAttnThreads : 1];
     __shared__ float maxima[kAttnWaves];
     __shared__ float2 totals[WIDE ? kAttnThreads / 16 : 1];
-    const int s = blockIdx.y, H = a.q.heads, G = H / a.p.kv_heads, D = a.p.dim, tid = threadIdx.x % kTeam;
+    const int s = sequence_of(a);
+    if (s < 0) return;
+    const int H = a.q.heads, G = H / a.p.kv_heads, D = a.p.dim, tid = threadIdx.x % kTeam;
     const int row = WIDE ? blockIdx.x : __builtin_amdgcn_readfirstlane(blockIdx.x * kAttnWaves + threadIdx.x / kWave);
     const int t = row / H, h = row - t * H;
     const Span v = span_of(a, s);
@@ -416,12 +421,15 @@ __global__ __launch_bounds__(kAttnThreads) void kv_join_kernel(AttentionArgs a, 
     if (tid == 0 && a.lse) a.lse[at] = l == 0.f ? -INFINITY : (best + log2f(l)) * kLn2;
 }
 
+// rows of workgroups of a launch (sequence_of)
+unsigned sequences(const AttentionArgs &a) { return static_cast<unsigned>(a.by_token ? a.q.total_q : a.ix.n_seqs); }
+
 template <typename T, bool PICKED>
 void launch_join(const AttentionArgs &a, int tile_rows, hipStream_t stream) {
     const int64_t rows = int64_t(a.q.max_q) * a.q.heads;   // checked by the caller
     // many parts of a row: a workgroup each; few: a wave each (13000 rows of at most 4 parts: 14 us with a workgroup each)
-    if (a.n_chunks > 16) hipLaunchKernelGGL((kv_join_kernel<T, PICKED, true>), dim3(static_cast<unsigned>(rows), a.ix.n_seqs), dim3(kAttnThreads), 0, stream, a, tile_rows);
-    else hipLaunchKernelGGL((kv_join_kernel<T, PICKED, false>), dim3(static_cast<unsigned>((rows + kAttnWaves - 1) / kAttnWaves), a.ix.n_seqs), dim3(kAttnThreads), 0, stream, a, tile_rows);
+    if (a.n_chunks > 16) hipLaunchKernelGGL((kv_join_kernel<T, PICKED, true>), dim3(static_cast<unsigned>(rows), sequences(a)), dim3(kAttnThreads), 0, stream, a, tile_rows);
+    else hipLaunchKernelGGL((kv_join_kernel<T, PICKED, false>), dim3(static_cast<unsigned>((rows + kAttnWaves - 1) / kAttnWaves), sequences(a)), dim3(kAttnThreads), 0, stream, a, tile_rows);
 }
 
 struct Plan {
@@ -440,6 +448,7 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, 
     // units: keys or picks to split, unit_step: the least stretch, a multiple of which a chunk is
     Plan pl;
     const int64_t places = padded_dim(p.dim) == 256 ? 256 : 512;   // for workgroups at a time: the least of both kernels
+    // groups: sequences of the call (of picked blocks: queries) x kv heads
     // fill: keys that give each place for a workgroup one stretch.  Short sequences that fill the CUs are not split.
     const double fill = static_cast<double>(units) * groups / places;
     const bool whole = units <= 1024 && groups >= 256;
@@ -489,7 +498,11 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, 
 
 Plan tree_plan(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q) {
     const int64_t rows = int64_t(q.max_q) * (q.heads / p.kv_heads);
-    return plan_of(p, rows, int64_t(ix.n_seqs) * p.kv_heads, q.max_len, 128, int64_t(kListed) * p.page, false);
+    // Sequences of the call, not places of the index: an index has room for more than are there (one token on 131000 keys in one of 64 places: 101 us,
+    // 1070 counted by places).  max_q tokens each would be the fewest; drafts are ragged, half of max_q and more in the mean, so twice that (16 trees of up to 26
+    // tokens: 49 us, 58 with the fewest; one tree in one of 64 places: 127 us, 115 in an index of its own, 1390 counted by places).
+    const int64_t live = std::min<int64_t>({ix.n_seqs, q.total_q, 2 * ceil_div(q.total_q, q.max_q)});
+    return plan_of(p, rows, live * p.kv_heads, q.max_len, 128, int64_t(kListed) * p.page, false);
 }
 
 Plan picked_plan(const tbn_kv_pool &p, const KvQueries &q, int32_t n_select) {
@@ -549,7 +562,7 @@ tbn_status launch(AttentionArgs &a, const Plan &pl, float *ws, const char *what,
     a.part_ml = reinterpret_cast<float4 *>(ws ? ws + parts * a.p.dim : nullptr);
     const int64_t x = int64_t(pl.n_chunks) * pl.row_tiles * a.p.kv_heads * (PICKED ? a.q.max_q : 1), jx = int64_t(a.q.max_q) * a.q.heads;
     if (x > kMostBlocks || jx > kMostBlocks) return too_many(what, x > jx ? x : jx);
-    const dim3 grid(static_cast<unsigned>(x), a.ix.n_seqs);
+    const dim3 grid(static_cast<unsigned>(x), sequences(a));
     if (pl.staged) launch_kv_rows(a, pl.rows / 32, grid, stream);
     else if (a.p.dt == TBN_F32) launch_dims<float, PICKED>(a, pl.rows, grid, stream);
     else launch_dims<uint16_t, PICKED>(a, pl.rows, grid, stream);
@@ -567,6 +580,7 @@ size_t tree_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, co
 tbn_status launch_tree_attention(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, void *out, float *lse, const uint32_t *mask,
                                  int32_t mask_words, float scale, float *ws, hipStream_t stream) {
     AttentionArgs a{p, ix, q, out, lse, mask, mask_words, nullptr, 0, factor_of(scale), flip_of(p, scale)};
+    a.by_token = q.total_q < ix.n_seqs;
     return launch<false>(a, tree_plan(p, ix, q), ws, "tbn_tree_attention", stream);
 }
 
@@ -577,13 +591,14 @@ size_t block_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, c
 tbn_status launch_block_attention(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, void *out, float *lse, const int32_t *picks,
                                   int32_t n_select, float scale, float *ws, hipStream_t stream) {
     AttentionArgs a{p, ix, q, out, lse, nullptr, 0, picks, n_select, factor_of(scale), flip_of(p, scale)};
+    a.by_token = q.total_q < ix.n_seqs;
     const char *what = "tbn_block_attention";
     if (const int queries = picked_queries(p, ix, q, n_select)) {
         a.n_chunks = 1;
         a.row_tiles = static_cast<int>(ceil_div(q.max_q, queries));
         const int64_t x = int64_t(a.row_tiles) * p.kv_heads;
         if (x > kMostBlocks) return too_many(what, x);
-        launch_kv_picked(a, queries, dim3(static_cast<unsigned>(x), ix.n_seqs), stream);
+        launch_kv_picked(a, queries, dim3(static_cast<unsigned>(x), sequences(a)), stream);
         return check_launch(what);
     }
     return launch<true>(a, picked_plan(p, q, n_select), ws, what, stream);

@@ -14,3 +14,25 @@ def test_more_workgroups_than_a_launch_has(lib):  # noqa: F811
         assert lib.tbn_block_attention_workspace_bytes(*args, n, n, 4096, select) == 0   # queries share workgroups
         assert lib.tbn_block_attention(FAKE, 4096 * dim, FAKE, None, *args, FAKE, n, n, 4096, FAKE, select, 1.0, FAKE, big, None) == 3
         assert b"beyond one launch" in lib.tbn_last_error()
+
+
+def parts(lib, total, max_q, n_seqs, dt=1, max_len=131000, heads=32):  # noqa: F811
+    """Stretches that the keys of a sequence are split into, from the bytes of the workspace (0: not split)."""
+    p, i = structs(pool_kv_heads=8, pool_dim=128, pool_page=64, index_page=64, pool_dt=dt, index_n_seqs=n_seqs, index_max_pages=2048, pool_n_pages=1 << 20, index_n_pages=1 << 20)
+    need = lib.tbn_tree_attention_workspace_bytes(ctypes.addressof(p), ctypes.addressof(i), total, max_q, heads, max_len)
+    assert need % (total * heads * (128 + 4) * 4) == 0
+    return need // (total * heads * (128 + 4) * 4)
+
+
+def test_keys_are_split_by_the_sequences_that_are_there(lib):  # noqa: F811
+    """Places of the index that no token belongs to count for nothing."""
+    for dt in (0, 1):
+        for live, keys in ((1, 131000), (8, 9000), (3, 40000)):
+            alone = parts(lib, live, 1, live, dt, keys)
+            assert alone >= 4
+            assert [parts(lib, live, 1, n, dt, keys) for n in (16, 64, 512, 8192)] == [alone] * 4
+            # several tokens of each: no fewer than half of the stretches
+            alone = parts(lib, 26 * live, 26, live, dt, keys)
+            assert all(2 * parts(lib, 26 * live, 26, n, dt, keys) >= alone for n in (16, 64, 512, 8192))
+        # an index without idle places: as many as there are places, whether the drafts are of one length or ragged
+        assert parts(lib, 16 * 26, 26, 16, dt) == parts(lib, 16 * 15, 26, 16, dt) > 1
