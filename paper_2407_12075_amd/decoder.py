@@ -125,8 +125,10 @@ class Decoder:
 
     def prompt(self, tokens: torch.Tensor, copies: int) -> torch.Tensor:
         """Runs a prompt as sequence 0 and forks it into the sequences below `copies`; each begins with another of the best first
-        tokens, which are returned (int64, copies) and whose keys are not in the cache yet."""
+        tokens, which are returned (int64, copies) and whose keys are not in the cache yet.  What the cache held is given back first."""
         n = tokens.numel()
+        kv.tbn_kv_release(self.index, torch.zeros_like(self.index.lens))
+        self.index.status.zero_()
         counts = torch.zeros(self.cfg.n_seqs, dtype=torch.int32, device=self.device)
         counts[0] = n
         logits = self.forward(tokens, torch.arange(n, device=self.device), counts, n)
