@@ -470,10 +470,12 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, 
     }
     pl.row_tiles = static_cast<int>(ceil_div(rows, pl.rows));
     const int64_t blocks = groups * pl.row_tiles;
-    // Stretches of keys.  The staged kernel takes one round of the places (64 drafted tokens on 131000 keys: 188 us, in four rounds 227), two
-    // where a stretch would be longer than 8192 keys: lengths are ragged, and two even them out (64 sequences of 4096 - 16384 keys: 456 us, 490 in
-    // one round, 462 in the other kernel).  Here many short stretches even them out, against the cost of starting, ending and joining each.
-    const int64_t parts = (few && round ? fit : ceil_div(places, blocks)) * (few && fill > 8192 ? 2 : 1);
+    // Stretches of keys.  The staged kernel takes one round of the places (64 drafted tokens on 131000 keys: 188 us, in four rounds 227).  Two where
+    // whole sequences of few rows would fill the round and are long: their lengths are ragged, and halves of them even that out (64 sequences of
+    // 4096 - 16384 keys: 456 us, 490 in one round, 462 in the other kernel; up to 8192: 236 - 242, 250 in one; 4100: 133 - 139 to 135 - 142; 3200 level; 100 of
+    // 2000: 119 - 123 to 110 - 113).  Fewer sequences are cut into more stretches anyway (16 of 60000: 410 - 425 us in one round, 431 - 454 in two; 32 of
+    // 16384 level).  Here many short stretches even them out, against the cost of starting, ending and joining each.
+    const int64_t parts = (few && round ? fit : ceil_div(places, blocks)) * (few && groups >= places && units > 4096 ? 2 : 1);
     int64_t chunk = ceil_div(units, pl.staged ? parts : ceil_div(8192, blocks));
     if (!picked && !pl.staged) {
         // Beyond 256 keys several stretches a place: with a cost of c keys each and about half a stretch idle at the end, the best length grows

@@ -36,3 +36,10 @@ def test_keys_are_split_by_the_sequences_that_are_there(lib):  # noqa: F811
             assert all(2 * parts(lib, 26 * live, 26, n, dt, keys) >= alone for n in (16, 64, 512, 8192))
         # an index without idle places: as many as there are places, whether the drafts are of one length or ragged
         assert parts(lib, 16 * 26, 26, 16, dt) == parts(lib, 16 * 15, 26, 16, dt) > 1
+
+
+def test_rounds_of_the_staged_kernel(lib):  # noqa: F811
+    """Single tokens, 512 places for workgroups, 8 key heads: whole sequences that fill the places and are long are cut in two, fewer into as many as fit."""
+    assert [parts(lib, 64, 1, 64, 1, n) for n in (3200, 4096, 4200, 16384)] == [0, 0, 2, 2]
+    assert [parts(lib, 100, 1, 100, 1, n) for n in (2000, 6000)] == [0, 2]
+    assert [parts(lib, n, 1, n, 1, 60000) for n in (16, 32)] == [4, 2]
