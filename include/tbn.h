@@ -394,7 +394,9 @@ tbn_status tbn_kv_fork(const tbn_kv_index *index, const int32_t *parents, const 
 
 /*
  * Freeing: sequence s keeps its first min(length, max(keep[s], 0)) keys and gives back the pages behind them (0: all of
- * them); freed slots become -1.  A page is free once no table row holds it.
+ * them); freed slots become -1.  A page is free once no table row holds it.  Pages and their summaries stay as they are: the
+ * summary of a page that is cut short still covers the keys that are gone (an upper bound all the same, infinite if one of
+ * them was) until tbn_kv_append writes to the page.
  *   keep : DEVICE, n_seqs
  */
 tbn_status tbn_kv_release(const tbn_kv_index *index, const int32_t *keep, void *stream);
@@ -433,7 +435,8 @@ tbn_status tbn_kv_append(const tbn_kv_pool *pool, const tbn_kv_index *index, con
  * Of the last keys of a sequence some stay (the accepted path of a tree of drafted tokens): key base[s] + picks[s][j]
  * moves to base[s] + j, j < counts[s], with its value; picks ascend in each row.  Lengths and pages do not change
  * (tbn_kv_release with base + counts follows); the summaries of the pages that hold the kept keys are made again over
- * keys before base + counts.  Picks below j or at or beyond the sequence's length are left out.
+ * keys before base + counts; nothing is done for a sequence with counts of 0.  Picks below j or at or beyond the sequence's
+ * length are left out.  The pages from key base on must be held by no other sequence, as tbn_kv_reserve leaves them.
  *   base, counts : DEVICE, n_seqs;  picks : DEVICE, n_seqs x width
  */
 tbn_status tbn_kv_keep(const tbn_kv_pool *pool, const tbn_kv_index *index, const int32_t *base, const int32_t *picks,

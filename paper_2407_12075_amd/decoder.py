@@ -9,8 +9,8 @@ cache (``kv.py``), and its operators run together as a server would use them:
 
 What is emitted is what the whole model picks (its highest logit) after each prefix: drafts change the speed only.  Weights
 are synthetic; embeddings, norms, residual sums and the choice of tokens are PyTorch's, everything else is the library's.  At this
-size the host's launches set the pace (127 steps without drafts in 83 ms, 67 steps of four passes with them in 185 ms): what the
-example shows is how the calls fit together, and that drafts save steps.
+size the host's launches set the pace (127 steps without drafts in 79 - 89 ms, 66 steps of four passes with them in 194 - 197 ms): what the
+example shows is how the calls fit together, and that drafts save steps, not that they pay.
 
     python -m paper_2407_12075_amd.decoder          # tokens per second with and without drafts on cuda:0
 """
