@@ -35,7 +35,6 @@ struct AttentionArgs {   // of one launch
     int32_t chunk;      // keys, or picks, of a workgroup
     int32_t n_chunks;
     int32_t row_tiles;  // tiles of a workgroup's rows
-    int32_t by_token;   // blockIdx.y is a token of the call, not a sequence
 };
 
 template <typename T> struct Elem;
@@ -151,21 +150,23 @@ __device__ __forceinline__ Span span_of(const AttentionArgs &a, int s) {
 }
 
 // The sequence of a workgroup, -1 if there is nothing to do.  An index with more sequences than the call has tokens has idle ones: there the
-// launch has a row of workgroups for each token, and that of a sequence's first token does its work.  Their sequence is the last one that begins at or
-// before the token: 64 places are looked at in each round.
+// launch may have a row of workgroups for each token (TOKENS), and that of a sequence's first token does its work.  Their sequence is the last one that
+// begins at or before the token: 64 places are looked at in each round.  (Instances of their own: a branch would cost every launch 0.5 us.)
+template <bool TOKENS>
 __device__ __forceinline__ int sequence_of(const AttentionArgs &a) {
-    if (!a.by_token) return blockIdx.y;
-    const int token = blockIdx.y, lane = threadIdx.x & 63;
-    int from = 0, n = a.ix.n_seqs + 1;   // it is among these entries of cu_q
+    const int row = blockIdx.y;
+    if constexpr (!TOKENS) return row;
+    const int lane = threadIdx.x & 63;
+    int s = 0, n = a.ix.n_seqs + 1;   // it is among the n entries of cu_q from s on
     while (n > 1) {
         const int step = (n + kWave - 1) / kWave;
-        const uint64_t before = __ballot(lane * step < n && a.q.cu_q[from + min(lane * step, n - 1)] <= token);
-        const int skip = max(__popcll(before) - 1, 0) * step;   // below n
-        from += skip;
+        const int before = static_cast<int>(__popcll(__ballot(lane * step < n && a.q.cu_q[s + min(lane * step, n - 1)] <= row)));
+        const int skip = max(before - 1, 0) * step;   // below n
+        s += skip;
         n = min(step, n - skip);
     }
-    from = __builtin_amdgcn_readfirstlane(from);
-    return from < a.ix.n_seqs && max(a.q.cu_q[from], 0) == token ? from : -1;
+    s = __builtin_amdgcn_readfirstlane(s);
+    return s < a.ix.n_seqs && max(a.q.cu_q[s], 0) == row ? s : -1;
 }
 
 // A workgroup's share.  Heads vary fastest: neighbouring workgroups go to different XCDs, so every XCD gets the same mix of stretches (a
@@ -257,6 +258,6 @@ __device__ __forceinline__ void store_sums(const AttentionArgs &a, int chunk, in
 int picked_queries(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, int32_t n_select);
 void launch_kv_picked(const AttentionArgs &a, int queries, dim3 grid, hipStream_t stream);
 // many rows, bfloat16: `tiles` (2 or 4) of 32 rows per workgroup
-void launch_kv_rows(const AttentionArgs &a, int tiles, dim3 grid, hipStream_t stream);
+void launch_kv_rows(const AttentionArgs &a, int tiles, bool tokens, dim3 grid, hipStream_t stream);
 
 }  // namespace tbn

@@ -31,8 +31,8 @@ namespace tbn {
 
 namespace {
 
-// RT: row tiles of a workgroup.  DP: channels the registers hold (dim <= DP; EVEN: dim == DP).
-template <typename T, int DP, int RT, bool PICKED, bool EVEN>
+// RT: row tiles of a workgroup.  DP: channels the registers hold (dim <= DP; EVEN: dim == DP).  TOKENS: blockIdx.y is a token (sequence_of).
+template <typename T, int DP, int RT, bool PICKED, bool EVEN, bool TOKENS>
 __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_kernel(AttentionArgs a) {
     using E = Elem<T>;
     constexpr int KS = E::kStep, OF = E::kOf, NF = DP / 16, NQ = NF / E::kTiles;
@@ -41,8 +41,8 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
     __shared__ float maxima[kAttnWaves][16], totals[2][kAttnWaves][16];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
-    const int s = sequence_of(a);
-    if (s < 0) return;
+    const int s = sequence_of<TOKENS>(a);
+    if (TOKENS && s < 0) return;
     const int H = a.q.heads, KV = a.p.kv_heads, G = H / KV, D = EVEN ? DP : a.p.dim, P = a.p.page;
     const int shift = __ffs(P) - 1;
     const Span v = span_of(a, s);
@@ -339,14 +339,14 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
 }
 
 // Joins the parts of one row.  D / 4 lanes (rounded up to a power of two) take a part at a time.  WIDE: a workgroup per row, else a wave.
-template <typename T, bool PICKED, bool WIDE>
+template <typename T, bool PICKED, bool WIDE, bool TOKENS>
 __global__ __launch_bounds__(kAttnThreads) void kv_join_kernel(AttentionArgs a, int tile_rows) {
     constexpr int kTeam = WIDE ? kAttnThreads : kWave;
     __shared__ f32x4_t sums[WIDE ? kAttnThreads : 1];
     __shared__ float maxima[kAttnWaves];
     __shared__ float2 totals[WIDE ? kAttnThreads / 16 : 1];
-    const int s = sequence_of(a);
-    if (s < 0) return;
+    const int s = sequence_of<TOKENS>(a);
+    if (TOKENS && s < 0) return;
     const int H = a.q.heads, G = H / a.p.kv_heads, D = a.p.dim, tid = threadIdx.x % kTeam;
     const int row = WIDE ? blockIdx.x : __builtin_amdgcn_readfirstlane(blockIdx.x * kAttnWaves + threadIdx.x / kWave);
     const int t = row / H, h = row - t * H;
@@ -421,15 +421,12 @@ __global__ __launch_bounds__(kAttnThreads) void kv_join_kernel(AttentionArgs a, 
     if (tid == 0 && a.lse) a.lse[at] = l == 0.f ? -INFINITY : (best + log2f(l)) * kLn2;
 }
 
-// rows of workgroups of a launch (sequence_of)
-unsigned sequences(const AttentionArgs &a) { return static_cast<unsigned>(a.by_token ? a.q.total_q : a.ix.n_seqs); }
-
-template <typename T, bool PICKED>
-void launch_join(const AttentionArgs &a, int tile_rows, hipStream_t stream) {
+template <typename T, bool PICKED, bool TOKENS>
+void launch_join(const AttentionArgs &a, int tile_rows, unsigned groups, hipStream_t stream) {
     const int64_t rows = int64_t(a.q.max_q) * a.q.heads;   // checked by the caller
     // many parts of a row: a workgroup each; few: a wave each (13000 rows of at most 4 parts: 14 us with a workgroup each)
-    if (a.n_chunks > 16) hipLaunchKernelGGL((kv_join_kernel<T, PICKED, true>), dim3(static_cast<unsigned>(rows), sequences(a)), dim3(kAttnThreads), 0, stream, a, tile_rows);
-    else hipLaunchKernelGGL((kv_join_kernel<T, PICKED, false>), dim3(static_cast<unsigned>((rows + kAttnWaves - 1) / kAttnWaves), sequences(a)), dim3(kAttnThreads), 0, stream, a, tile_rows);
+    if (a.n_chunks > 16) hipLaunchKernelGGL((kv_join_kernel<T, PICKED, true, TOKENS>), dim3(static_cast<unsigned>(rows), groups), dim3(kAttnThreads), 0, stream, a, tile_rows);
+    else hipLaunchKernelGGL((kv_join_kernel<T, PICKED, false, TOKENS>), dim3(static_cast<unsigned>((rows + kAttnWaves - 1) / kAttnWaves), groups), dim3(kAttnThreads), 0, stream, a, tile_rows);
 }
 
 struct Plan {
@@ -498,13 +495,27 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, 
     return pl;
 }
 
+// Whether a launch has a row of workgroups per token of the call instead of per place of the index (sequence_of): where no token is without work, or
+// places are many more.
+bool by_token(const tbn_kv_index &ix, const KvQueries &q) { return q.total_q < ix.n_seqs && (q.max_q == 1 || 16 * q.total_q <= ix.n_seqs); }
+
+// An index has room for more sequences than are there, so keys are split by the sequences of the call: max_q tokens each would be the fewest; drafts are
+// ragged, half of max_q and more in the mean, so twice that (16 trees of up to 26 tokens: 49 us, 58 with the fewest).  One token on 131000 keys in one of 64
+// places: 101 us, 1070 split by places; a tree of 26: 128 and 1390.  But every place or token has its row of workgroups, 0.2 - 0.6 ns each where all but a few end
+// at once (a token's 1.4 - 6), so there are fewer stretches, as if for twice as many sequences and so on up to one for each row, beyond a number that is small
+// against the work.
+int64_t most_blocks(const KvQueries &q) { return std::min<int64_t>(150000, 16384 + 8 * q.max_len); }
+
 Plan tree_plan(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q) {
     const int64_t rows = int64_t(q.max_q) * (q.heads / p.kv_heads);
-    // Sequences of the call, not places of the index: an index has room for more than are there (one token on 131000 keys in one of 64 places: 101 us,
-    // 1070 counted by places).  max_q tokens each would be the fewest; drafts are ragged, half of max_q and more in the mean, so twice that (16 trees of up to 26
-    // tokens: 49 us, 58 with the fewest; one tree in one of 64 places: 127 us, 115 in an index of its own, 1390 counted by places).
-    const int64_t live = std::min<int64_t>({ix.n_seqs, q.total_q, 2 * ceil_div(q.total_q, q.max_q)});
-    return plan_of(p, rows, live * p.kv_heads, q.max_len, 128, int64_t(kListed) * p.page, false);
+    const bool token = by_token(ix, q);
+    const int64_t most = token ? q.total_q : ix.n_seqs, weight = most * (token && q.max_q > 1 ? 5 : 1);
+    int64_t sequences = std::min<int64_t>({ix.n_seqs, q.total_q, 2 * ceil_div(q.total_q, q.max_q)});
+    for (;; sequences = std::min(most, 2 * sequences)) {
+        const Plan pl = plan_of(p, rows, sequences * p.kv_heads, q.max_len, 128, int64_t(kListed) * p.page, false);
+        const int64_t join = int64_t(q.max_q) * q.heads, blocks = int64_t(pl.n_chunks) * pl.row_tiles * p.kv_heads + (pl.n_chunks > 16 ? join : pl.n_chunks > 1 ? join / 4 : 0);
+        if (sequences >= most || blocks * weight <= most_blocks(q)) return pl;
+    }
 }
 
 Plan picked_plan(const tbn_kv_pool &p, const KvQueries &q, int32_t n_select) {
@@ -515,30 +526,37 @@ size_t workspace_of(const tbn_kv_pool &p, const KvQueries &q, const Plan &pl) {
     return pl.n_chunks > 1 ? static_cast<size_t>(pl.n_chunks) * q.total_q * q.heads * (p.dim + 4) * 4 : 0;
 }
 
-template <typename T, int DP, int RT, bool PICKED>
+template <typename T, int DP, int RT, bool PICKED, bool TOKENS>
 void launch_even(const AttentionArgs &a, dim3 grid, hipStream_t stream) {
-    if (a.p.dim == DP) hipLaunchKernelGGL((kv_attention_kernel<T, DP, RT, PICKED, true>), grid, dim3(kAttnThreads), 0, stream, a);
-    else hipLaunchKernelGGL((kv_attention_kernel<T, DP, RT, PICKED, false>), grid, dim3(kAttnThreads), 0, stream, a);
+    if (a.p.dim == DP) hipLaunchKernelGGL((kv_attention_kernel<T, DP, RT, PICKED, true, TOKENS>), grid, dim3(kAttnThreads), 0, stream, a);
+    else hipLaunchKernelGGL((kv_attention_kernel<T, DP, RT, PICKED, false, TOKENS>), grid, dim3(kAttnThreads), 0, stream, a);
 }
 
-template <typename T, int DP, bool PICKED>
+template <typename T, int DP, bool PICKED, bool TOKENS>
 void launch_rows(const AttentionArgs &a, int rows, dim3 grid, hipStream_t stream) {
     if constexpr (sizeof(T) == 4 && DP <= 64) {
-        if (rows == 64) return launch_even<T, DP, 4, PICKED>(a, grid, stream);
+        if (rows == 64) return launch_even<T, DP, 4, PICKED, TOKENS>(a, grid, stream);
     }
     if constexpr (sizeof(T) == 4 && DP <= 128) {
-        if (rows == 32) return launch_even<T, DP, 2, PICKED>(a, grid, stream);
+        if (rows == 32) return launch_even<T, DP, 2, PICKED, TOKENS>(a, grid, stream);
     }
-    launch_even<T, DP, 1, PICKED>(a, grid, stream);
+    launch_even<T, DP, 1, PICKED, TOKENS>(a, grid, stream);
 }
 
-template <typename T, bool PICKED>
-void launch_dims(const AttentionArgs &a, int rows, dim3 grid, hipStream_t stream) {
-    switch (padded_dim(a.p.dim)) {
-        case 64: launch_rows<T, 64, PICKED>(a, rows, grid, stream); break;
-        case 128: launch_rows<T, 128, PICKED>(a, rows, grid, stream); break;
-        default: launch_rows<T, 256, PICKED>(a, rows, grid, stream);
-    }
+// Both kernels; pl.staged: the first one is another file's.
+template <typename T, bool PICKED, bool TOKENS>
+void launch_both(const AttentionArgs &a, const Plan &pl, dim3 grid, hipStream_t stream) {
+    if (pl.staged) launch_kv_rows(a, pl.rows / 32, TOKENS, grid, stream);
+    else if (padded_dim(a.p.dim) == 64) launch_rows<T, 64, PICKED, TOKENS>(a, pl.rows, grid, stream);
+    else if (padded_dim(a.p.dim) == 128) launch_rows<T, 128, PICKED, TOKENS>(a, pl.rows, grid, stream);
+    else launch_rows<T, 256, PICKED, TOKENS>(a, pl.rows, grid, stream);
+    if (a.n_chunks > 1) launch_join<T, PICKED, TOKENS>(a, pl.rows, grid.y, stream);
+}
+
+template <bool PICKED, bool TOKENS>
+void launch_type(const AttentionArgs &a, const Plan &pl, dim3 grid, hipStream_t stream) {
+    if (a.p.dt == TBN_F32) launch_both<float, PICKED, TOKENS>(a, pl, grid, stream);
+    else launch_both<uint16_t, PICKED, TOKENS>(a, pl, grid, stream);
 }
 
 float factor_of(float scale) {
@@ -564,14 +582,13 @@ tbn_status launch(AttentionArgs &a, const Plan &pl, float *ws, const char *what,
     a.part_ml = reinterpret_cast<float4 *>(ws ? ws + parts * a.p.dim : nullptr);
     const int64_t x = int64_t(pl.n_chunks) * pl.row_tiles * a.p.kv_heads * (PICKED ? a.q.max_q : 1), jx = int64_t(a.q.max_q) * a.q.heads;
     if (x > kMostBlocks || jx > kMostBlocks) return too_many(what, x > jx ? x : jx);
-    const dim3 grid(static_cast<unsigned>(x), sequences(a));
-    if (pl.staged) launch_kv_rows(a, pl.rows / 32, grid, stream);
-    else if (a.p.dt == TBN_F32) launch_dims<float, PICKED>(a, pl.rows, grid, stream);
-    else launch_dims<uint16_t, PICKED>(a, pl.rows, grid, stream);
-    if (a.n_chunks > 1) {
-        if (a.p.dt == TBN_F32) launch_join<float, PICKED>(a, pl.rows, stream);
-        else launch_join<uint16_t, PICKED>(a, pl.rows, stream);
+    if constexpr (!PICKED) {
+        if (by_token(a.ix, a.q)) {
+            launch_type<false, true>(a, pl, dim3(static_cast<unsigned>(x), static_cast<unsigned>(a.q.total_q)), stream);
+            return check_launch(what);
+        }
     }
+    launch_type<PICKED, false>(a, pl, dim3(static_cast<unsigned>(x), a.ix.n_seqs), stream);
     return check_launch(what);
 }
 
@@ -582,7 +599,6 @@ size_t tree_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, co
 tbn_status launch_tree_attention(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, void *out, float *lse, const uint32_t *mask,
                                  int32_t mask_words, float scale, float *ws, hipStream_t stream) {
     AttentionArgs a{p, ix, q, out, lse, mask, mask_words, nullptr, 0, factor_of(scale), flip_of(p, scale)};
-    a.by_token = q.total_q < ix.n_seqs;
     return launch<false>(a, tree_plan(p, ix, q), ws, "tbn_tree_attention", stream);
 }
 
@@ -593,14 +609,13 @@ size_t block_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, c
 tbn_status launch_block_attention(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, void *out, float *lse, const int32_t *picks,
                                   int32_t n_select, float scale, float *ws, hipStream_t stream) {
     AttentionArgs a{p, ix, q, out, lse, nullptr, 0, picks, n_select, factor_of(scale), flip_of(p, scale)};
-    a.by_token = q.total_q < ix.n_seqs;
     const char *what = "tbn_block_attention";
     if (const int queries = picked_queries(p, ix, q, n_select)) {
         a.n_chunks = 1;
         a.row_tiles = static_cast<int>(ceil_div(q.max_q, queries));
         const int64_t x = int64_t(a.row_tiles) * p.kv_heads;
         if (x > kMostBlocks) return too_many(what, x);
-        launch_kv_picked(a, queries, dim3(static_cast<unsigned>(x), sequences(a)), stream);
+        launch_kv_picked(a, queries, dim3(static_cast<unsigned>(x), ix.n_seqs), stream);
         return check_launch(what);
     }
     return launch<true>(a, picked_plan(p, q, n_select), ws, what, stream);

@@ -59,9 +59,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_picked_ker
     __shared__ int counts[kAttnWaves];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
-    const int s = sequence_of(a);
-    if (s < 0) return;
-    const int H = a.q.heads, KV = a.p.kv_heads, G = H / KV, D = EVEN ? DP : a.p.dim, P = PAIRS ? 32 : a.p.page, shift = __ffs(P) - 1;
+    const int s = blockIdx.y, H = a.q.heads, KV = a.p.kv_heads, G = H / KV, D = EVEN ? DP : a.p.dim, P = PAIRS ? 32 : a.p.page, shift = __ffs(P) - 1;
     const Span v = span_of(a, s);
     const Block blk = block_of(a);
     const int t_first = blk.row_tile * queries;

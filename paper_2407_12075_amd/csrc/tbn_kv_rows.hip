@@ -34,8 +34,8 @@ __device__ __forceinline__ f32x16_t mma(u32x4_t a, u32x4_t b, f32x16_t c) {
 // key of row r of a tile of 32: the instruction's output register 4 i + j of a lane of half h is row 8 i + 4 h + j
 __device__ __forceinline__ int key_of_row(int r) { return 16 * (r >> 4) + 8 * ((r >> 2) & 1) + 4 * ((r >> 3) & 1) + (r & 3); }
 
-// DP: channels (dim <= DP; EVEN: equal).  RW: groups of 32 rows, 4 / RW waves each.
-template <int DP, int RW, bool EVEN>
+// DP: channels (dim <= DP; EVEN: equal).  RW: groups of 32 rows, 4 / RW waves each.  TOKENS: blockIdx.y is a token (sequence_of).
+template <int DP, int RW, bool EVEN, bool TOKENS>
 __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kernel(AttentionArgs a) {
     constexpr int KW = kAttnWaves / RW, KEYS = DP == 256 && KW == 1 ? 32 : 64, TILES = KEYS / 32 / KW;
     constexpr int PITCH = DP == 96 ? 128 : DP;                     // channels of a row of K in LDS
@@ -49,8 +49,8 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
     __shared__ float4 halves[RW][32];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
-    const int s = sequence_of(a);
-    if (s < 0) return;
+    const int s = sequence_of<TOKENS>(a);
+    if (TOKENS && s < 0) return;
     const int H = a.q.heads, KV = a.p.kv_heads, G = H / KV, D = EVEN ? DP : a.p.dim, P = a.p.page;
     const int shift = __ffs(P) - 1, group = wave % RW, half = wave / RW;
     const Span v = span_of(a, s);
@@ -293,25 +293,30 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
         }
 }
 
+template <int DP, int RW, bool EVEN>
+void launch_tokens(const AttentionArgs &a, bool tokens, dim3 grid, hipStream_t stream) {
+    if (tokens) hipLaunchKernelGGL((kv_rows_kernel<DP, RW, EVEN, true>), grid, dim3(kAttnThreads), 0, stream, a);
+    else hipLaunchKernelGGL((kv_rows_kernel<DP, RW, EVEN, false>), grid, dim3(kAttnThreads), 0, stream, a);
+}
+
 template <int DP>
-void launch_dim(const AttentionArgs &a, int tiles, dim3 grid, hipStream_t stream) {
-    const dim3 block(kAttnThreads);
+void launch_dim(const AttentionArgs &a, int tiles, bool tokens, dim3 grid, hipStream_t stream) {
     if (tiles == 4) {
-        if (a.p.dim == DP) hipLaunchKernelGGL((kv_rows_kernel<DP, 4, true>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((kv_rows_kernel<DP, 4, false>), grid, block, 0, stream, a);
+        if (a.p.dim == DP) launch_tokens<DP, 4, true>(a, tokens, grid, stream);
+        else launch_tokens<DP, 4, false>(a, tokens, grid, stream);
     } else {
-        if (a.p.dim == DP) hipLaunchKernelGGL((kv_rows_kernel<DP, 2, true>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((kv_rows_kernel<DP, 2, false>), grid, block, 0, stream, a);
+        if (a.p.dim == DP) launch_tokens<DP, 2, true>(a, tokens, grid, stream);
+        else launch_tokens<DP, 2, false>(a, tokens, grid, stream);
     }
 }
 
 }  // namespace
 
-void launch_kv_rows(const AttentionArgs &a, int tiles, dim3 grid, hipStream_t stream) {
-    if (a.p.dim <= 64) launch_dim<64>(a, tiles, grid, stream);
-    else if (a.p.dim <= 96) launch_dim<96>(a, tiles, grid, stream);
-    else if (a.p.dim <= 128) launch_dim<128>(a, tiles, grid, stream);
-    else launch_dim<256>(a, tiles, grid, stream);
+void launch_kv_rows(const AttentionArgs &a, int tiles, bool tokens, dim3 grid, hipStream_t stream) {
+    if (a.p.dim <= 64) launch_dim<64>(a, tiles, tokens, grid, stream);
+    else if (a.p.dim <= 96) launch_dim<96>(a, tiles, tokens, grid, stream);
+    else if (a.p.dim <= 128) launch_dim<128>(a, tiles, tokens, grid, stream);
+    else launch_dim<256>(a, tiles, tokens, grid, stream);
 }
 
 }  // namespace tbn
