@@ -499,21 +499,22 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, 
 // places are many more.
 bool by_token(const tbn_kv_index &ix, const KvQueries &q) { return q.total_q < ix.n_seqs && (q.max_q == 1 || 16 * q.total_q <= ix.n_seqs); }
 
+// Workgroups of a launch whose rows may mostly be idle, at most: 0.2 - 0.6 ns each where they end at once, small against the work.
+double most_blocks(const KvQueries &q) { return std::min(150000., 16384. + 8. * q.max_len); }
+
 // An index has room for more sequences than are there, so keys are split by the sequences of the call: max_q tokens each would be the fewest; drafts are
 // ragged, half of max_q and more in the mean, so twice that (16 trees of up to 26 tokens: 49 us, 58 with the fewest).  One token on 131000 keys in one of 64
-// places: 101 us, 1070 split by places; a tree of 26: 128 and 1390.  But every place or token has its row of workgroups, 0.2 - 0.6 ns each where all but a few end
-// at once (a token's 1.4 - 6), so there are fewer stretches, as if for twice as many sequences and so on up to one for each row, beyond a number that is small
-// against the work.
-int64_t most_blocks(const KvQueries &q) { return std::min<int64_t>(150000, 16384 + 8 * q.max_len); }
-
+// places: 101 us, 1065 split by places; a tree of 26: 124 and 1383.  But every place (or token, whose idle workgroups take five times as long) has its row
+// of workgroups: beyond most_blocks they are split as if for twice as many sequences, and so on up to one for each row.
 Plan tree_plan(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q) {
     const int64_t rows = int64_t(q.max_q) * (q.heads / p.kv_heads);
     const bool token = by_token(ix, q);
-    const int64_t most = token ? q.total_q : ix.n_seqs, weight = most * (token && q.max_q > 1 ? 5 : 1);
+    const int64_t most = token ? q.total_q : ix.n_seqs;
+    const double weight = most * (token && q.max_q > 1 ? 5. : 1.), join = double(q.max_q) * q.heads;
     int64_t sequences = std::min<int64_t>({ix.n_seqs, q.total_q, 2 * ceil_div(q.total_q, q.max_q)});
     for (;; sequences = std::min(most, 2 * sequences)) {
         const Plan pl = plan_of(p, rows, sequences * p.kv_heads, q.max_len, 128, int64_t(kListed) * p.page, false);
-        const int64_t join = int64_t(q.max_q) * q.heads, blocks = int64_t(pl.n_chunks) * pl.row_tiles * p.kv_heads + (pl.n_chunks > 16 ? join : pl.n_chunks > 1 ? join / 4 : 0);
+        const double blocks = double(pl.n_chunks) * pl.row_tiles * p.kv_heads + (pl.n_chunks > 16 ? join : pl.n_chunks > 1 ? join / 4 : 0.);
         if (sequences >= most || blocks * weight <= most_blocks(q)) return pl;
     }
 }
