@@ -476,6 +476,25 @@ tbn_status tbn_tree_attention(const void *q, int64_t q_stride, void *out, float 
                               size_t workspace_bytes, void *stream);
 
 /*
+ * tbn_tree_attention where a token sees only the first keys of its sequence and the last ones up to its own: arguments, types,
+ * results and errors as there, with
+ *
+ *   n_sink   : >= 0, the first keys, which every token sees
+ *   window   : >= 1; the token whose place is t sees key j if j < n_sink or j > t - window (of the keys that it sees there)
+ *
+ * Without a mask a token's place is the number of its own key.  With one (a tree of drafted tokens) it is that of its key if the draft were
+ * the only one: the keys before the call's tokens, and the tokens that its mask row names (itself among them) less one; the call's own tokens
+ * are seen by the mask alone, so max_q must be at most `window` (TBN_ERR_SHAPE), and no window ends among them.  Pages that lie between the
+ * first keys and the window are not read.
+ */
+size_t tbn_window_attention_workspace_bytes(const tbn_kv_pool *pool, const tbn_kv_index *index, int64_t total_q, int32_t max_q,
+                                            int32_t heads, int32_t n_sink, int32_t window, int32_t masked, int64_t max_len);
+tbn_status tbn_window_attention(const void *q, int64_t q_stride, void *out, float *lse, const tbn_kv_pool *pool,
+                                const tbn_kv_index *index, const int32_t *cu_q, int64_t total_q, int32_t max_q, int32_t heads,
+                                int32_t n_sink, int32_t window, const uint32_t *mask, int32_t mask_words, int64_t max_len, float scale,
+                                void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Which pages of its sequence a query attends to.  Queries, sequences and positions as for tbn_tree_attention without a
  * mask; blocks are a sequence's table slots, a query's own block is the one its key lies in.  Per query and kv head:
  * all blocks up to the own one if they are at most n_select; else the first n_sink, the last n_recent up to the own one,

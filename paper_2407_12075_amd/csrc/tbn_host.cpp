@@ -39,6 +39,8 @@ decltype(&tbn_kv_append) p_kv_append;
 decltype(&tbn_kv_keep) p_kv_keep;
 decltype(&tbn_tree_attention_workspace_bytes) p_tree_attention_workspace_bytes;
 decltype(&tbn_tree_attention) p_tree_attention;
+decltype(&tbn_window_attention_workspace_bytes) p_window_attention_workspace_bytes;
+decltype(&tbn_window_attention) p_window_attention;
 decltype(&tbn_block_select_workspace_bytes) p_block_select_workspace_bytes;
 decltype(&tbn_block_select) p_block_select;
 decltype(&tbn_block_attention_workspace_bytes) p_block_attention_workspace_bytes;
@@ -426,22 +428,54 @@ bool scale_of(PyObject *o, const Held &pool, float &scale) {
     return true;
 }
 
+// mask or None, for n tokens
+bool mask_of(PyObject *o, const Held &ix, int64_t n, const uint32_t *&mask, int32_t &words) {
+    mask = nullptr;
+    words = 0;
+    if (o == Py_None) return true;
+    mask = reinterpret_cast<const uint32_t *>(ints(o, 0, ix.gpu));
+    if (!mask) return false;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (t.dim() != 2 || t.size(0) != n || t.size(1) > INT32_MAX) return false;
+    words = static_cast<int32_t>(t.size(1));
+    return true;
+}
+
+// (.., mask or None, scale or None, n_sink, window)
+PyObject *window_attention(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    QueryArgs a;
+    float scale;
+    int64_t sink, window;
+    const uint32_t *mask;
+    int32_t words;
+    if (n_args != 12 || !queries(args, a) || !scale_of(args[9], a.pool, scale) || !integer(args[10], 0, INT32_MAX, sink) || !integer(args[11], 1, INT32_MAX, window) ||
+        !mask_of(args[8], a.ix, a.q->size(0), mask, words))
+        Py_RETURN_NONE;
+    const int64_t n = a.q->size(0), heads = a.q->size(1);
+    const int32_t max_q = static_cast<int32_t>(a.max_q), H = static_cast<int32_t>(heads), n_sink = static_cast<int32_t>(sink), w = static_cast<int32_t>(window);
+    const auto *pool = pool_of(a.pool);
+    const auto *ix = index_of(a.ix);
+    at::Tensor out = at::empty({n, heads, pool->dim}, a.q->options()), lse = at::empty({n, heads}, a.q->options().dtype(at::kFloat)), ws;
+    const size_t need = p_window_attention_workspace_bytes(pool, ix, n, max_q, H, n_sink, w, mask != nullptr, a.max_len);
+    if (need) ws = bytes_like(*a.q, need);
+    const tbn_status st = unlocked([&] {
+        return p_window_attention(a.q->data_ptr(), a.stride, out.data_ptr(), floats(lse), pool, ix, a.cu, n, max_q, H, n_sink, w, mask, words, a.max_len, scale,
+                                  need ? ws.data_ptr() : nullptr, need, stream());
+    });
+    return result(st, two, out, lse);
+    END_HANDLE_TH_ERRORS
+}
+
 // (.., mask or None, scale or None)
 PyObject *tree_attention(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     HANDLE_TH_ERRORS
     QueryArgs a;
     float scale;
-    if (n_args != 10 || !queries(args, a) || !scale_of(args[9], a.pool, scale)) Py_RETURN_NONE;
+    const uint32_t *mask;
+    int32_t words;
+    if (n_args != 10 || !queries(args, a) || !scale_of(args[9], a.pool, scale) || !mask_of(args[8], a.ix, a.q->size(0), mask, words)) Py_RETURN_NONE;
     const int64_t n = a.q->size(0), heads = a.q->size(1);
-    const int32_t *mask = nullptr;
-    int64_t words = 0;
-    if (args[8] != Py_None) {
-        mask = ints(args[8], 0, a.ix.gpu);
-        if (!mask) Py_RETURN_NONE;
-        const at::Tensor &t = THPVariable_Unpack(args[8]);
-        if (t.dim() != 2 || t.size(0) != n || t.size(1) > INT32_MAX) Py_RETURN_NONE;
-        words = t.size(1);
-    }
     const auto *pool = pool_of(a.pool);
     const auto *ix = index_of(a.ix);
     at::Tensor out = at::empty({n, heads, pool->dim}, a.q->options()), lse = at::empty({n, heads}, a.q->options().dtype(at::kFloat)), ws;
@@ -449,7 +483,7 @@ PyObject *tree_attention(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     if (need) ws = bytes_like(*a.q, need);
     const tbn_status st = unlocked([&] {
         return p_tree_attention(a.q->data_ptr(), a.stride, out.data_ptr(), floats(lse), pool, ix, a.cu, n, static_cast<int32_t>(a.max_q),
-                                static_cast<int32_t>(heads), reinterpret_cast<const uint32_t *>(mask), static_cast<int32_t>(words), a.max_len, scale,
+                                static_cast<int32_t>(heads), mask, words, a.max_len, scale,
                                 need ? ws.data_ptr() : nullptr, need, stream());
     });
     return result(st, two, out, lse);
@@ -530,6 +564,8 @@ PyObject *init(PyObject *, PyObject *args) {
     take(p_kv_keep, "tbn_kv_keep");
     take(p_tree_attention_workspace_bytes, "tbn_tree_attention_workspace_bytes");
     take(p_tree_attention, "tbn_tree_attention");
+    take(p_window_attention_workspace_bytes, "tbn_window_attention_workspace_bytes");
+    take(p_window_attention, "tbn_window_attention");
     take(p_block_select_workspace_bytes, "tbn_block_select_workspace_bytes");
     take(p_block_select, "tbn_block_select");
     take(p_block_attention_workspace_bytes, "tbn_block_attention_workspace_bytes");
@@ -548,7 +584,7 @@ PyObject *init(PyObject *, PyObject *args) {
 PyMethodDef methods[] = {TBN_FAST(linear_forward), TBN_FAST(conv2d_forward), TBN_FAST(linear_coltiled_forward), TBN_FAST(sign_pack),
                          TBN_FAST(linear_forward_binact), TBN_FAST(pack_tile),
                          TBN_FAST(kv_reserve), TBN_FAST(kv_fork), TBN_FAST(kv_release), TBN_FAST(kv_copy_pages), TBN_FAST(kv_append), TBN_FAST(kv_keep),
-                         TBN_FAST(tree_attention), TBN_FAST(block_select), TBN_FAST(block_attention), {"init", init, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         TBN_FAST(tree_attention), TBN_FAST(window_attention), TBN_FAST(block_select), TBN_FAST(block_attention), {"init", init, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tbn_host", "plain calls of the binding on C++ tensors", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

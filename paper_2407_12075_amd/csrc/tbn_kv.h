@@ -32,6 +32,9 @@ tbn_status launch_kv_keep(const tbn_kv_pool &p, const tbn_kv_index &ix, const in
 size_t tree_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q);
 tbn_status launch_tree_attention(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, void *out, float *lse, const uint32_t *mask,
                                  int32_t mask_words, float scale, float *ws, hipStream_t stream);
+size_t window_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, int32_t n_sink, int32_t window, bool masked);
+tbn_status launch_window_attention(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, void *out, float *lse, int32_t n_sink, int32_t window,
+                                   const uint32_t *mask, int32_t mask_words, float scale, float *ws, hipStream_t stream);
 size_t block_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, int32_t n_select);
 tbn_status launch_block_attention(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, void *out, float *lse, const int32_t *picks,
                                   int32_t n_select, float scale, float *ws, hipStream_t stream);

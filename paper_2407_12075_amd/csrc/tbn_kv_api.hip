@@ -186,6 +186,43 @@ tbn_status tbn_tree_attention(const void *q, int64_t q_stride, void *out, float 
     return launch_tree_attention(*pool, *index, a, out, lse, mask, mask_words, scale, static_cast<float *>(workspace), static_cast<hipStream_t>(stream));
 }
 
+// n_sink and window of a call: nothing is beyond the longest sequence
+static tbn_status check_window(const char *fn, const KvQueries &q, bool masked, int32_t &n_sink, int32_t &window) {
+    if (n_sink < 0 || window < 1) return fail(TBN_ERR_SHAPE, fn, "n_sink must be >= 0, window positive");
+    if (masked && q.max_q > window) return fail(TBN_ERR_SHAPE, fn, "with a mask the window must hold max_q tokens");
+    constexpr int32_t kMost = 1 << 30;
+    n_sink = n_sink < kMost ? n_sink : kMost;
+    window = window < kMost ? window : kMost;
+    return TBN_OK;
+}
+
+size_t tbn_window_attention_workspace_bytes(const tbn_kv_pool *pool, const tbn_kv_index *index, int64_t total_q, int32_t max_q, int32_t heads,
+                                            int32_t n_sink, int32_t window, int32_t masked, int64_t max_len) {
+    KvQueries q{nullptr, 0, nullptr, total_q, max_q, heads, max_len};
+    if (check_queries(nullptr, pool, index, q) != TBN_OK || check_window(nullptr, q, masked != 0, n_sink, window) != TBN_OK || total_q == 0 || max_q == 0)
+        return 0;
+    return window_attention_workspace(*pool, *index, q, n_sink, window, masked != 0);
+}
+
+tbn_status tbn_window_attention(const void *q, int64_t q_stride, void *out, float *lse, const tbn_kv_pool *pool, const tbn_kv_index *index,
+                                const int32_t *cu_q, int64_t total_q, int32_t max_q, int32_t heads, int32_t n_sink, int32_t window,
+                                const uint32_t *mask, int32_t mask_words, int64_t max_len, float scale, void *workspace, size_t workspace_bytes,
+                                void *stream) {
+    const char *fn = "tbn_window_attention";
+    KvQueries a{q, q_stride, cu_q, total_q, max_q, heads, max_len};
+    tbn_status st = check_queries(fn, pool, index, a);
+    if (st == TBN_OK) st = check_window(fn, a, mask != nullptr, n_sink, window);
+    if (st != TBN_OK) return st;
+    if (mask && (mask_words < 0 || int64_t(mask_words) * 32 < max_q)) return fail(TBN_ERR_SHAPE, fn, "mask_words must hold max_q bits");
+    if (total_q == 0 || max_q == 0) return TBN_OK;
+    st = check_query_pointers(fn, pool, a, out);
+    if (st == TBN_OK) st = check_workspace(fn, window_attention_workspace(*pool, *index, a, n_sink, window, mask != nullptr), workspace, workspace_bytes, 16);
+    if (st != TBN_OK) return st;
+    drop_stale_error();
+    return launch_window_attention(*pool, *index, a, out, lse, n_sink, window, mask, mask_words, scale, static_cast<float *>(workspace),
+                                   static_cast<hipStream_t>(stream));
+}
+
 static tbn_status check_select(const char *fn, const tbn_kv_pool *pool, const tbn_kv_index *index, KvQueries &q) {
     const tbn_status st = check_queries(fn, pool, index, q);
     if (st != TBN_OK) return st;

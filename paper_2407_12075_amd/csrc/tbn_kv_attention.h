@@ -35,7 +35,11 @@ struct AttentionArgs {   // of one launch
     int32_t chunk;      // keys, or picks, of a workgroup
     int32_t n_chunks;
     int32_t row_tiles;  // tiles of a workgroup's rows
+    int32_t n_sink, window;   // of a call with a window: the first keys that every token sees, and how many up to its own place
 };
+
+// what the rows of a launch see: every key up to their own, the pages they picked, the first keys and a window
+enum Kind { kAll, kPicked, kWindow };
 
 template <typename T> struct Elem;
 template <> struct Elem<uint16_t> {
@@ -192,6 +196,42 @@ __device__ __forceinline__ int keys_end(const AttentionArgs &a, const Span &v, i
     return a.mask ? v.len : min(v.len, v.prefix + last_row / G + 1);
 }
 
+// The keys that the rows [row0, row1] of a call with a window can see, as pages without a gap: the pages of the first keys, then those
+// from the first row's window on.  "Within" counts keys along them; `gap` keys are left out behind the first `head` of them.
+struct Within {
+    int head, gap, end, low;   // keys of the first pages, keys left out, keys in all, the least key of the first row's window
+    __device__ __forceinline__ int key(int x) const { return x < head ? x : x + gap; }
+};
+
+__device__ __forceinline__ Within within_of(const AttentionArgs &a, const Span &v, int row0, int row1, int G, int shift) {
+    const int end = keys_end(a, v, row1, G), pages = (end + a.p.page - 1) >> shift;
+    Within w;
+    // with a mask a row's place is what it has above it, none at least
+    w.low = max((a.mask ? v.prefix - 1 : v.prefix + row0 / G) - a.window + 1, 0);
+    const int sink = (min(a.n_sink, end) + a.p.page - 1) >> shift, from = w.low >> shift;
+    w.head = sink << shift;
+    w.gap = from > sink && from < pages ? (from - sink) << shift : 0;
+    w.end = from >= pages ? min(w.head, end) : end - w.gap;
+    return w;
+}
+
+// The least key of a row's window: its place is its own key's, with a mask the number of the tokens it sees more than the keys before the call.
+// (There max_q <= window, so a window never ends among the call's own tokens.)
+__device__ __forceinline__ int window_of(const AttentionArgs &a, const Span &v, int place) {
+    int at = v.prefix + place;
+    if (a.mask) {
+        const uint32_t *mask = a.mask + int64_t(v.t0 + place) * a.mask_words;
+        at = v.prefix - 1;
+        for (int w = 0; w * 32 < v.T; ++w) at += __popc(mask[w] & (v.T - w * 32 >= 32 ? ~0u : (1u << (v.T - w * 32)) - 1u));
+    }
+    return at - a.window + 1;
+}
+
+// no row's window begins behind this key
+__device__ __forceinline__ int last_window(const AttentionArgs &a, const Span &v, int row1, int G) {
+    return v.prefix + (a.mask ? v.T - 1 : row1 / G) - a.window + 1;
+}
+
 // a word with its first n bits set, as far as it has them
 __device__ __forceinline__ uint32_t first_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
 
@@ -236,6 +276,14 @@ __device__ __forceinline__ uint32_t seen_bits(const AttentionArgs &a, const Span
     return bits & __funnelshift_r(lo, hi, j0 & 31);
 }
 
+// with a window that begins at key `low`
+template <Kind KIND>
+__device__ __forceinline__ uint32_t seen_within(const AttentionArgs &a, const Span &v, int k0, int end, int place, int low) {
+    uint32_t bits = seen_bits<KIND == kPicked>(a, v, k0, end, place);
+    if constexpr (KIND == kWindow) bits &= first_bits(a.n_sink - k0) | ~first_bits(low - k0);
+    return bits;
+}
+
 // Four channels of a row from its sums: to the output, or to the parts of its stretch.  m in units of log2; l the weights' sum, z the
 // rounded weights'.
 template <typename T>
@@ -258,6 +306,6 @@ __device__ __forceinline__ void store_sums(const AttentionArgs &a, int chunk, in
 int picked_queries(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, int32_t n_select);
 void launch_kv_picked(const AttentionArgs &a, int queries, dim3 grid, hipStream_t stream);
 // many rows, bfloat16: `tiles` (2 or 4) of 32 rows per workgroup
-void launch_kv_rows(const AttentionArgs &a, int tiles, bool tokens, dim3 grid, hipStream_t stream);
+void launch_kv_rows(const AttentionArgs &a, Kind kind, int tiles, bool tokens, dim3 grid, hipStream_t stream);
 
 }  // namespace tbn

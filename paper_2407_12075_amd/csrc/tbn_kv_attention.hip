@@ -22,6 +22,10 @@
 // A key that a row does not see: its logit is replaced, not added to.  Its value is still multiplied by a weight of 0, so
 // in steps that hold such keys values behind the last visible key are replaced by 0, and if another value of the step is
 // infinite or not a number it is replaced by 0 too and a third product counts, for each row, the ones that it sees.
+//
+// A window (kWindow): the rows of a workgroup see the first keys and what their windows reach, so its pages are those two runs of the table, one
+// after the other, and stretches are cut along them (Within); steps that no row sees are left out, those that not every row sees take the masked path.
+// One token each of 64 sequences of up to 16384 keys, window 4096, 8 kv heads of 128 channels, bfloat16: 194 us, 5.5 TB/s of the 1.08 GB in reach.
 #include <algorithm>
 #include <cmath>
 
@@ -32,9 +36,10 @@ namespace tbn {
 namespace {
 
 // RT: row tiles of a workgroup.  DP: channels the registers hold (dim <= DP; EVEN: dim == DP).  TOKENS: blockIdx.y is a token (sequence_of).
-template <typename T, int DP, int RT, bool PICKED, bool EVEN, bool TOKENS>
+template <typename T, int DP, int RT, Kind KIND, bool EVEN, bool TOKENS>
 __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_kernel(AttentionArgs a) {
     using E = Elem<T>;
+    constexpr bool PICKED = KIND == kPicked, WINDOW = KIND == kWindow;
     constexpr int KS = E::kStep, OF = E::kOf, NF = DP / 16, NQ = NF / E::kTiles;
     __shared__ int2 listed[kListed];   // slot and page
     __shared__ float sums[RT][kAttnWaves][16][DP + 4];
@@ -51,7 +56,10 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
     const int R = PICKED ? G : v.T * G;   // rows of the sequence (PICKED: of the token)
     if (base >= R || (PICKED && only >= v.T)) return;
     const int own = v.prefix + only;   // PICKED: the query's own key
-    const int end = PICKED ? min(v.len, own + 1) : keys_end(a, v, min(base + 16 * RT, R) - 1, G);
+    const int last = min(base + 16 * RT, R) - 1;
+    const int end = PICKED ? min(v.len, own + 1) : keys_end(a, v, last, G);
+    Within in_reach = {};
+    if constexpr (WINDOW) in_reach = within_of(a, v, base, last, G, shift);
 
     // the pages of this stretch
     const int32_t *table = a.ix.table + int64_t(s) * a.ix.max_pages;
@@ -67,22 +75,23 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
             listed[i] = make_int2(in ? b : -1, in ? page_in(table[b], n_pages) : 0);
         }
     } else {
-        const int first = chunk * a.chunk;
-        if (first >= end && chunk > 0) return;
-        entries = (min(end, first + a.chunk) - first + P - 1) >> shift;
+        const int first = chunk * a.chunk, stop = WINDOW ? in_reach.end : end;
+        if (first >= stop && chunk > 0) return;
+        entries = (min(stop, first + a.chunk) - first + P - 1) >> shift;
         for (int i = tid; i < entries; i += kAttnThreads) {
-            const int slot = (first >> shift) + i;
+            const int slot = (WINDOW ? in_reach.key(first + (i << shift)) : first + (i << shift)) >> shift;
             listed[i] = make_int2(slot, page_in(table[slot], n_pages));
         }
     }
 
     // this lane's query rows: its token's place and the operand of the first product
     u32x4_t q[RT][NQ];
-    int place[RT];
+    int place[RT], low[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         const int row = base + r * 16 + n, in = min(row, R - 1), t = PICKED ? only : in / G;
         place[r] = t;
+        low[r] = WINDOW ? window_of(a, v, t) : 0;
         const T *src = static_cast<const T *>(a.q.q) + (v.t0 + t) * a.q.q_stride + (head * G + (PICKED ? in : in - t * G)) * D;
         // always loaded, so that the loads do not wait for each other
 #pragma unroll
@@ -141,6 +150,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
         page = __builtin_amdgcn_readfirstlane(e.y);
         const int slot = __builtin_amdgcn_readfirstlane(e.x);
         const int key = (slot << shift) + (i & ((1 << sub_shift) - 1)) * KS;
+        if (WINDOW && key >= a.n_sink && key + KS <= in_reach.low) return -1;
         return slot < 0 || key >= end ? -1 : key;
     };
     auto next_step = [&](int i, int &key, int &page) {
@@ -170,6 +180,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
     }
     // keys from here on are not seen by every row
     const int all_see = PICKED ? end : a.mask ? v.prefix : v.prefix + base / G + 1;
+    const int all_from = WINDOW ? last_window(a, v, last, G) : 0;   // keys before this one, the first ones aside, neither
     while (i < steps) {
         int next_key = 0, next_page = 0;
         const int next = next_step(i + kAttnWaves, next_key, next_page);
@@ -203,14 +214,15 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
         }
         if (next < steps) load_k(k, next_page, next_key & (P - 1));
 
-        const bool edge = key + KS > all_see;   // wave-uniform
+        bool edge = key + KS > all_see;   // wave-uniform
+        if constexpr (WINDOW) edge |= key < all_from && key + KS > a.n_sink;
         uint32_t seen[RT];
         bool odd = false;
         if (edge) {
             const int k0 = key + OF * g;   // this lane's keys
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                const uint32_t bits = seen_bits<PICKED>(a, v, k0, end, place[r]);
+                const uint32_t bits = seen_within<KIND>(a, v, k0, end, place[r], low[r]);
 #pragma unroll
                 for (int e = 0; e < OF; ++e) p[r][e] = (bits >> e) & 1u ? p[r][e] : -INFINITY;
                 seen[r] = bits;
@@ -339,7 +351,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
 }
 
 // Joins the parts of one row.  D / 4 lanes (rounded up to a power of two) take a part at a time.  WIDE: a workgroup per row, else a wave.
-template <typename T, bool PICKED, bool WIDE, bool TOKENS>
+template <typename T, Kind KIND, bool WIDE, bool TOKENS>
 __global__ __launch_bounds__(kAttnThreads) void kv_join_kernel(AttentionArgs a, int tile_rows) {
     constexpr int kTeam = WIDE ? kAttnThreads : kWave;
     __shared__ f32x4_t sums[WIDE ? kAttnThreads : 1];
@@ -353,9 +365,10 @@ __global__ __launch_bounds__(kAttnThreads) void kv_join_kernel(AttentionArgs a, 
     const Span v = span_of(a, s);
     if (t >= v.T) return;
     int parts = a.n_chunks;
-    if (!PICKED) {
-        const int r = t * G + h % G, last = min(r / tile_rows * tile_rows + tile_rows, v.T * G) - 1;
-        parts = max(1, (keys_end(a, v, last, G) + a.chunk - 1) / a.chunk);
+    if (KIND != kPicked) {
+        const int r = t * G + h % G, base = r / tile_rows * tile_rows, last = min(base + tile_rows, v.T * G) - 1;
+        const int end = KIND == kWindow ? within_of(a, v, base, last, G, __ffs(a.p.page) - 1).end : keys_end(a, v, last, G);
+        parts = max(1, (end + a.chunk - 1) / a.chunk);
     }
     const int64_t at = int64_t(v.t0 + t) * H + h, stride = a.q.total_q * H;
     const int shift = D <= 64 ? 4 : D <= 128 ? 5 : 6, group = tid >> shift, groups = kTeam >> shift, d = (tid & ((1 << shift) - 1)) * 4;
@@ -421,12 +434,12 @@ __global__ __launch_bounds__(kAttnThreads) void kv_join_kernel(AttentionArgs a, 
     if (tid == 0 && a.lse) a.lse[at] = l == 0.f ? -INFINITY : (best + log2f(l)) * kLn2;
 }
 
-template <typename T, bool PICKED, bool TOKENS>
+template <typename T, Kind KIND, bool TOKENS>
 void launch_join(const AttentionArgs &a, int tile_rows, unsigned groups, hipStream_t stream) {
     const int64_t rows = int64_t(a.q.max_q) * a.q.heads;   // checked by the caller
     // many parts of a row: a workgroup each; few: a wave each (13000 rows of at most 4 parts: 14 us with a workgroup each)
-    if (a.n_chunks > 16) hipLaunchKernelGGL((kv_join_kernel<T, PICKED, true, TOKENS>), dim3(static_cast<unsigned>(rows), groups), dim3(kAttnThreads), 0, stream, a, tile_rows);
-    else hipLaunchKernelGGL((kv_join_kernel<T, PICKED, false, TOKENS>), dim3(static_cast<unsigned>((rows + kAttnWaves - 1) / kAttnWaves), groups), dim3(kAttnThreads), 0, stream, a, tile_rows);
+    if (a.n_chunks > 16) hipLaunchKernelGGL((kv_join_kernel<T, KIND, true, TOKENS>), dim3(static_cast<unsigned>(rows), groups), dim3(kAttnThreads), 0, stream, a, tile_rows);
+    else hipLaunchKernelGGL((kv_join_kernel<T, KIND, false, TOKENS>), dim3(static_cast<unsigned>((rows + kAttnWaves - 1) / kAttnWaves), groups), dim3(kAttnThreads), 0, stream, a, tile_rows);
 }
 
 struct Plan {
@@ -500,22 +513,23 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, 
 bool by_token(const tbn_kv_index &ix, const KvQueries &q) { return q.total_q < ix.n_seqs && (q.max_q == 1 || 16 * q.total_q <= ix.n_seqs); }
 
 // Workgroups of a launch whose rows may mostly be idle, at most: 0.2 - 0.6 ns each where they end at once, small against the work.
-double most_blocks(const KvQueries &q) { return std::min(150000., 16384. + 8. * q.max_len); }
+double most_blocks(int64_t keys) { return std::min(150000., 16384. + 8. * keys); }
 
 // An index has room for more sequences than are there, so keys are split by the sequences of the call: max_q tokens each would be the fewest; drafts are
 // ragged, half of max_q and more in the mean, so twice that (16 trees of up to 26 tokens: 49 us, 58 with the fewest).  One token on 131000 keys in one of 64
 // places: 101 us, 1065 split by places; a tree of 26: 124 and 1383.  But every place (or token, whose idle workgroups take five times as long) has its row
 // of workgroups: beyond most_blocks they are split as if for twice as many sequences, and so on up to one for each row.
-Plan tree_plan(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q) {
+// keys: that a sequence of the call has for a row of workgroups to go through, at most.
+Plan tree_plan(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, int64_t keys) {
     const int64_t rows = int64_t(q.max_q) * (q.heads / p.kv_heads);
     const bool token = by_token(ix, q);
     const int64_t most = token ? q.total_q : ix.n_seqs;
     const double weight = most * (token && q.max_q > 1 ? 5. : 1.), join = double(q.max_q) * q.heads;
     int64_t sequences = std::min<int64_t>({ix.n_seqs, q.total_q, 2 * ceil_div(q.total_q, q.max_q)});
     for (;; sequences = std::min(most, 2 * sequences)) {
-        const Plan pl = plan_of(p, rows, sequences * p.kv_heads, q.max_len, 128, int64_t(kListed) * p.page, false);
+        const Plan pl = plan_of(p, rows, sequences * p.kv_heads, keys, 128, int64_t(kListed) * p.page, false);
         const double blocks = double(pl.n_chunks) * pl.row_tiles * p.kv_heads + (pl.n_chunks > 16 ? join : pl.n_chunks > 1 ? join / 4 : 0.);
-        if (sequences >= most || blocks * weight <= most_blocks(q)) return pl;
+        if (sequences >= most || blocks * weight <= most_blocks(keys)) return pl;
     }
 }
 
@@ -527,37 +541,37 @@ size_t workspace_of(const tbn_kv_pool &p, const KvQueries &q, const Plan &pl) {
     return pl.n_chunks > 1 ? static_cast<size_t>(pl.n_chunks) * q.total_q * q.heads * (p.dim + 4) * 4 : 0;
 }
 
-template <typename T, int DP, int RT, bool PICKED, bool TOKENS>
+template <typename T, int DP, int RT, Kind KIND, bool TOKENS>
 void launch_even(const AttentionArgs &a, dim3 grid, hipStream_t stream) {
-    if (a.p.dim == DP) hipLaunchKernelGGL((kv_attention_kernel<T, DP, RT, PICKED, true, TOKENS>), grid, dim3(kAttnThreads), 0, stream, a);
-    else hipLaunchKernelGGL((kv_attention_kernel<T, DP, RT, PICKED, false, TOKENS>), grid, dim3(kAttnThreads), 0, stream, a);
+    if (a.p.dim == DP) hipLaunchKernelGGL((kv_attention_kernel<T, DP, RT, KIND, true, TOKENS>), grid, dim3(kAttnThreads), 0, stream, a);
+    else hipLaunchKernelGGL((kv_attention_kernel<T, DP, RT, KIND, false, TOKENS>), grid, dim3(kAttnThreads), 0, stream, a);
 }
 
-template <typename T, int DP, bool PICKED, bool TOKENS>
+template <typename T, int DP, Kind KIND, bool TOKENS>
 void launch_rows(const AttentionArgs &a, int rows, dim3 grid, hipStream_t stream) {
     if constexpr (sizeof(T) == 4 && DP <= 64) {
-        if (rows == 64) return launch_even<T, DP, 4, PICKED, TOKENS>(a, grid, stream);
+        if (rows == 64) return launch_even<T, DP, 4, KIND, TOKENS>(a, grid, stream);
     }
     if constexpr (sizeof(T) == 4 && DP <= 128) {
-        if (rows == 32) return launch_even<T, DP, 2, PICKED, TOKENS>(a, grid, stream);
+        if (rows == 32) return launch_even<T, DP, 2, KIND, TOKENS>(a, grid, stream);
     }
-    launch_even<T, DP, 1, PICKED, TOKENS>(a, grid, stream);
+    launch_even<T, DP, 1, KIND, TOKENS>(a, grid, stream);
 }
 
 // Both kernels; pl.staged: the first one is another file's.
-template <typename T, bool PICKED, bool TOKENS>
+template <typename T, Kind KIND, bool TOKENS>
 void launch_both(const AttentionArgs &a, const Plan &pl, dim3 grid, hipStream_t stream) {
-    if (pl.staged) launch_kv_rows(a, pl.rows / 32, TOKENS, grid, stream);
-    else if (padded_dim(a.p.dim) == 64) launch_rows<T, 64, PICKED, TOKENS>(a, pl.rows, grid, stream);
-    else if (padded_dim(a.p.dim) == 128) launch_rows<T, 128, PICKED, TOKENS>(a, pl.rows, grid, stream);
-    else launch_rows<T, 256, PICKED, TOKENS>(a, pl.rows, grid, stream);
-    if (a.n_chunks > 1) launch_join<T, PICKED, TOKENS>(a, pl.rows, grid.y, stream);
+    if (pl.staged) launch_kv_rows(a, KIND, pl.rows / 32, TOKENS, grid, stream);
+    else if (padded_dim(a.p.dim) == 64) launch_rows<T, 64, KIND, TOKENS>(a, pl.rows, grid, stream);
+    else if (padded_dim(a.p.dim) == 128) launch_rows<T, 128, KIND, TOKENS>(a, pl.rows, grid, stream);
+    else launch_rows<T, 256, KIND, TOKENS>(a, pl.rows, grid, stream);
+    if (a.n_chunks > 1) launch_join<T, KIND, TOKENS>(a, pl.rows, grid.y, stream);
 }
 
-template <bool PICKED, bool TOKENS>
+template <Kind KIND, bool TOKENS>
 void launch_type(const AttentionArgs &a, const Plan &pl, dim3 grid, hipStream_t stream) {
-    if (a.p.dt == TBN_F32) launch_both<float, PICKED, TOKENS>(a, pl, grid, stream);
-    else launch_both<uint16_t, PICKED, TOKENS>(a, pl, grid, stream);
+    if (a.p.dt == TBN_F32) launch_both<float, KIND, TOKENS>(a, pl, grid, stream);
+    else launch_both<uint16_t, KIND, TOKENS>(a, pl, grid, stream);
 }
 
 float factor_of(float scale) {
@@ -573,7 +587,7 @@ tbn_status too_many(const char *what, int64_t blocks) {
     return TBN_ERR_UNSUPPORTED;
 }
 
-template <bool PICKED>
+template <Kind KIND>
 tbn_status launch(AttentionArgs &a, const Plan &pl, float *ws, const char *what, hipStream_t stream) {
     a.chunk = pl.chunk;
     a.n_chunks = pl.n_chunks;
@@ -581,26 +595,44 @@ tbn_status launch(AttentionArgs &a, const Plan &pl, float *ws, const char *what,
     const int64_t parts = int64_t(pl.n_chunks) * a.q.total_q * a.q.heads;
     a.part_o = ws;
     a.part_ml = reinterpret_cast<float4 *>(ws ? ws + parts * a.p.dim : nullptr);
-    const int64_t x = int64_t(pl.n_chunks) * pl.row_tiles * a.p.kv_heads * (PICKED ? a.q.max_q : 1), jx = int64_t(a.q.max_q) * a.q.heads;
+    const int64_t x = int64_t(pl.n_chunks) * pl.row_tiles * a.p.kv_heads * (KIND == kPicked ? a.q.max_q : 1), jx = int64_t(a.q.max_q) * a.q.heads;
     if (x > kMostBlocks || jx > kMostBlocks) return too_many(what, x > jx ? x : jx);
-    if constexpr (!PICKED) {
+    if constexpr (KIND != kPicked) {
         if (by_token(a.ix, a.q)) {
-            launch_type<false, true>(a, pl, dim3(static_cast<unsigned>(x), static_cast<unsigned>(a.q.total_q)), stream);
+            launch_type<KIND, true>(a, pl, dim3(static_cast<unsigned>(x), static_cast<unsigned>(a.q.total_q)), stream);
             return check_launch(what);
         }
     }
-    launch_type<PICKED, false>(a, pl, dim3(static_cast<unsigned>(x), a.ix.n_seqs), stream);
+    launch_type<KIND, false>(a, pl, dim3(static_cast<unsigned>(x), a.ix.n_seqs), stream);
     return check_launch(what);
 }
 
 }  // namespace
 
-size_t tree_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q) { return workspace_of(p, q, tree_plan(p, ix, q)); }
+size_t tree_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q) { return workspace_of(p, q, tree_plan(p, ix, q, q.max_len)); }
 
 tbn_status launch_tree_attention(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, void *out, float *lse, const uint32_t *mask,
                                  int32_t mask_words, float scale, float *ws, hipStream_t stream) {
     AttentionArgs a{p, ix, q, out, lse, mask, mask_words, nullptr, 0, factor_of(scale), flip_of(p, scale)};
-    return launch<false>(a, tree_plan(p, ix, q), ws, "tbn_tree_attention", stream);
+    return launch<kAll>(a, tree_plan(p, ix, q, q.max_len), ws, "tbn_tree_attention", stream);
+}
+
+// Keys that a workgroup of a call with a window goes through, at most: the first pages, the window of its first row and what its other rows add.
+static int64_t window_keys(const tbn_kv_pool &p, const KvQueries &q, int32_t n_sink, int32_t window, bool masked) {
+    const int64_t tokens = masked ? q.max_q : std::min<int64_t>(q.max_q, 128 / (q.heads / p.kv_heads) + 2);
+    return std::min(q.max_len, ceil_div(n_sink, p.page) * p.page + window + tokens + 2 * p.page);
+}
+
+size_t window_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, int32_t n_sink, int32_t window, bool masked) {
+    return workspace_of(p, q, tree_plan(p, ix, q, window_keys(p, q, n_sink, window, masked)));
+}
+
+tbn_status launch_window_attention(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, void *out, float *lse, int32_t n_sink, int32_t window,
+                                   const uint32_t *mask, int32_t mask_words, float scale, float *ws, hipStream_t stream) {
+    AttentionArgs a{p, ix, q, out, lse, mask, mask_words, nullptr, 0, factor_of(scale), flip_of(p, scale)};
+    a.n_sink = n_sink;
+    a.window = window;
+    return launch<kWindow>(a, tree_plan(p, ix, q, window_keys(p, q, n_sink, window, mask != nullptr)), ws, "tbn_window_attention", stream);
 }
 
 size_t block_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, int32_t n_select) {
@@ -619,7 +651,7 @@ tbn_status launch_block_attention(const tbn_kv_pool &p, const tbn_kv_index &ix, 
         launch_kv_picked(a, queries, dim3(static_cast<unsigned>(x), ix.n_seqs), stream);
         return check_launch(what);
     }
-    return launch<true>(a, picked_plan(p, q, n_select), ws, what, stream);
+    return launch<kPicked>(a, picked_plan(p, q, n_select), ws, what, stream);
 }
 
 }  // namespace tbn

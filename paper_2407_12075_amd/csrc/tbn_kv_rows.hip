@@ -35,8 +35,9 @@ __device__ __forceinline__ f32x16_t mma(u32x4_t a, u32x4_t b, f32x16_t c) {
 __device__ __forceinline__ int key_of_row(int r) { return 16 * (r >> 4) + 8 * ((r >> 2) & 1) + 4 * ((r >> 3) & 1) + (r & 3); }
 
 // DP: channels (dim <= DP; EVEN: equal).  RW: groups of 32 rows, 4 / RW waves each.  TOKENS: blockIdx.y is a token (sequence_of).
-template <int DP, int RW, bool EVEN, bool TOKENS>
+template <int DP, int RW, Kind KIND, bool EVEN, bool TOKENS>
 __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kernel(AttentionArgs a) {
+    constexpr bool WINDOW = KIND == kWindow;
     constexpr int KW = kAttnWaves / RW, KEYS = DP == 256 && KW == 1 ? 32 : 64, TILES = KEYS / 32 / KW;
     constexpr int PITCH = DP == 96 ? 128 : DP;                     // channels of a row of K in LDS
     constexpr bool FULL = EVEN && PITCH == DP;                     // every piece of such a row is the head's
@@ -57,14 +58,20 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
     const Block blk = block_of(a);
     const int R = v.T * G, base = blk.row_tile * (32 * RW);
     if (base >= R) return;
-    const int end = keys_end(a, v, min(base + 32 * RW, R) - 1, G);
+    // a window's keys are counted along the pages that are gone through
+    const int last = min(base + 32 * RW, R) - 1;
+    Within in_reach = {};
+    if constexpr (WINDOW) in_reach = within_of(a, v, base, last, G, shift);
+    const int end = WINDOW ? in_reach.end : keys_end(a, v, last, G);
     const int first = blk.chunk * a.chunk;
     if (first >= end && blk.chunk > 0) return;
     const int stop = min(end, first + a.chunk), entries = (stop - first + P - 1) >> shift;
-    const int32_t *table = a.ix.table + int64_t(s) * a.ix.max_pages + (first >> shift);
-    for (int i = tid; i < entries; i += kAttnThreads) listed[i] = page_in(table[i], static_cast<int>(a.p.n_pages));
+    const int32_t *table = a.ix.table + int64_t(s) * a.ix.max_pages + (WINDOW ? 0 : first >> shift);
+    for (int i = tid; i < entries; i += kAttnThreads)
+        listed[i] = page_in(table[WINDOW ? in_reach.key(first + (i << shift)) >> shift : i], static_cast<int>(a.p.n_pages));
 
     const int row = base + group * 32 + n, in = min(row, R - 1), place = in / G;
+    const int low = WINDOW ? window_of(a, v, place) : 0;
     const int64_t at = int64_t(v.t0 + place) * H + blk.head * G + (in - place * G);   // of the outputs, where row < R
     u32x4_t q[NQ];
     {
@@ -128,6 +135,12 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
         for (int e = 0; e < 16; ++e) o[f][e] = 0.f;
     float m = -INFINITY, l = 0.f, z = 0.f;
     const int all_see = a.mask ? v.prefix : v.prefix + base / G + 1;   // keys from here on are not seen by every row
+    const int all_from = WINDOW ? last_window(a, v, last, G) : 0;                  // keys before this one, the first ones aside, neither
+    // which of eight keys, counted as the steps are, this lane's row sees
+    auto seen = [&](int x) {
+        const int k = WINDOW ? in_reach.key(x) : x;
+        return seen_within<KIND>(a, v, k, stop + (k - x), place, low);
+    };
 
     auto compute = [&](int i, const uint16_t *kt, uint16_t *vt) {
         f32x16_t p[TILES];
@@ -141,13 +154,22 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
             for (int t = 0; t < TILES; ++t)
                 p[t] = mma(*reinterpret_cast<const u32x4_t *>(kt + ((KW > 1 ? half : t) * 32 + n) * PITCH + ((2 * f + h) ^ (n & 7)) * 8), q[f], p[t]);
         const int key = first + i * KEYS;
-        const bool edge = key + KEYS > all_see || key + KEYS > stop;   // the same for all lanes
+        bool edge = key + KEYS > stop;   // the same for all lanes
+        if constexpr (WINDOW) {
+#pragma unroll
+            for (int t = 0; t < KEYS; t += 32) {
+                const int k = in_reach.key(key + t);
+                edge |= k + 32 > all_see || (k < all_from && k + 32 > a.n_sink);
+            }
+        } else {
+            edge |= key + KEYS > all_see;
+        }
         if (edge) {
 #pragma unroll
             for (int t = 0; t < TILES; ++t)
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const uint32_t bits = seen_bits<false>(a, v, key + (KW > 1 ? half : t) * 32 + 16 * u + 8 * h, stop, place);
+                    const uint32_t bits = seen(key + (KW > 1 ? half : t) * 32 + 16 * u + 8 * h);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) p[t][8 * u + e] = (bits >> e) & 1u ? p[t][8 * u + e] : -INFINITY;
                 }
@@ -188,7 +210,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
 #pragma unroll 1
                 for (int u = 0; u < 2 * TILES; ++u) {
                     const int c = (KW > 1 ? half * 4 : 0) + 2 * u + h;
-                    const u32x4_t ones = Elem<uint16_t>::ones(seen_bits<false>(a, v, key + c * 8, stop, place));
+                    const u32x4_t ones = Elem<uint16_t>::ones(seen(key + c * 8));
 #pragma unroll
                     for (int f = 0; f < ND; ++f) {
                         const int d = f * 32 + n;
@@ -293,30 +315,36 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
         }
 }
 
-template <int DP, int RW, bool EVEN>
+template <int DP, int RW, Kind KIND, bool EVEN>
 void launch_tokens(const AttentionArgs &a, bool tokens, dim3 grid, hipStream_t stream) {
-    if (tokens) hipLaunchKernelGGL((kv_rows_kernel<DP, RW, EVEN, true>), grid, dim3(kAttnThreads), 0, stream, a);
-    else hipLaunchKernelGGL((kv_rows_kernel<DP, RW, EVEN, false>), grid, dim3(kAttnThreads), 0, stream, a);
+    if (tokens) hipLaunchKernelGGL((kv_rows_kernel<DP, RW, KIND, EVEN, true>), grid, dim3(kAttnThreads), 0, stream, a);
+    else hipLaunchKernelGGL((kv_rows_kernel<DP, RW, KIND, EVEN, false>), grid, dim3(kAttnThreads), 0, stream, a);
+}
+
+template <int DP, Kind KIND>
+void launch_tiles(const AttentionArgs &a, int tiles, bool tokens, dim3 grid, hipStream_t stream) {
+    if (tiles == 4) {
+        if (a.p.dim == DP) launch_tokens<DP, 4, KIND, true>(a, tokens, grid, stream);
+        else launch_tokens<DP, 4, KIND, false>(a, tokens, grid, stream);
+    } else {
+        if (a.p.dim == DP) launch_tokens<DP, 2, KIND, true>(a, tokens, grid, stream);
+        else launch_tokens<DP, 2, KIND, false>(a, tokens, grid, stream);
+    }
 }
 
 template <int DP>
-void launch_dim(const AttentionArgs &a, int tiles, bool tokens, dim3 grid, hipStream_t stream) {
-    if (tiles == 4) {
-        if (a.p.dim == DP) launch_tokens<DP, 4, true>(a, tokens, grid, stream);
-        else launch_tokens<DP, 4, false>(a, tokens, grid, stream);
-    } else {
-        if (a.p.dim == DP) launch_tokens<DP, 2, true>(a, tokens, grid, stream);
-        else launch_tokens<DP, 2, false>(a, tokens, grid, stream);
-    }
+void launch_dim(const AttentionArgs &a, Kind kind, int tiles, bool tokens, dim3 grid, hipStream_t stream) {
+    if (kind == kWindow) launch_tiles<DP, kWindow>(a, tiles, tokens, grid, stream);
+    else launch_tiles<DP, kAll>(a, tiles, tokens, grid, stream);
 }
 
 }  // namespace
 
-void launch_kv_rows(const AttentionArgs &a, int tiles, bool tokens, dim3 grid, hipStream_t stream) {
-    if (a.p.dim <= 64) launch_dim<64>(a, tiles, tokens, grid, stream);
-    else if (a.p.dim <= 96) launch_dim<96>(a, tiles, tokens, grid, stream);
-    else if (a.p.dim <= 128) launch_dim<128>(a, tiles, tokens, grid, stream);
-    else launch_dim<256>(a, tiles, tokens, grid, stream);
+void launch_kv_rows(const AttentionArgs &a, Kind kind, int tiles, bool tokens, dim3 grid, hipStream_t stream) {
+    if (a.p.dim <= 64) launch_dim<64>(a, kind, tiles, tokens, grid, stream);
+    else if (a.p.dim <= 96) launch_dim<96>(a, kind, tiles, tokens, grid, stream);
+    else if (a.p.dim <= 128) launch_dim<128>(a, kind, tiles, tokens, grid, stream);
+    else launch_dim<256>(a, kind, tiles, tokens, grid, stream);
 }
 
 }  // namespace tbn

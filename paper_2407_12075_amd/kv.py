@@ -263,6 +263,41 @@ def tbn_tree_attention(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: torc
     return out, lse
 
 
+def _mask(mask: Optional[torch.Tensor], q: torch.Tensor):
+    """Address and words of a row of a mask, int32 (tokens, words)."""
+    if mask is None:
+        return None, 0
+    if mask.dim() != 2 or mask.shape[0] != q.shape[0]:
+        raise ValueError("mask must be (tokens, words)")
+    _same_device(q.device, mask)
+    return _dev(mask, "mask", torch.int32), mask.shape[1]
+
+
+def tbn_window_attention_workspace_bytes(q: torch.Tensor, pool: KVPool, index: KVIndex, max_q: int, n_sink: int, window: int, masked: bool = False,
+                                         max_len: int = 0) -> int:
+    return int(lib().tbn_window_attention_workspace_bytes(pool._at, index._at, q.shape[0], max_q, q.shape[1], n_sink, window, int(masked), max_len))
+
+
+def tbn_window_attention(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: torch.Tensor, max_q: int, n_sink: int, window: int,
+                         mask: Optional[torch.Tensor] = None, scale: Optional[float] = None, max_len: Optional[int] = None,
+                         out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                         stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """tbn_tree_attention over the sequence's first n_sink keys and the last `window` keys up to the token's own (with a mask: up to its place
+    in the tree; then max_q <= window).  Returns (out, lse)."""
+    if _plain(out, lse, workspace, stream):
+        r = tbn._host.window_attention(q, pool._at, pool._gpu, index._at, index._gpu, cu_q, max_q, max_len, mask, scale, n_sink, window)
+        if r is not None:
+            return r
+    at, stride, cu = _queries(q, pool, index, cu_q)
+    out, lse = _outputs(q, out, lse, stream)
+    mask_at, words = _mask(mask, q)
+    need = int(lib().tbn_window_attention_workspace_bytes(pool._at, index._at, q.shape[0], max_q, q.shape[1], n_sink, window, int(mask is not None), max_len or 0))
+    ws, size = _workspace(need, workspace, q.device, stream)
+    _done(_call("tbn_window_attention", at, stride, _dev(out, "out"), _dev(lse, "lse", torch.float32), pool._at, index._at, cu, q.shape[0], max_q, q.shape[1],
+                n_sink, window, mask_at, words, max_len or 0, 1.0 / math.sqrt(pool.dim) if scale is None else scale, ws, size, _stream(stream)))
+    return out, lse
+
+
 def tbn_block_select_workspace_bytes(q: torch.Tensor, pool: KVPool, index: KVIndex, max_q: int, max_len: int = 0) -> int:
     return int(lib().tbn_block_select_workspace_bytes(pool._at, index._at, q.shape[0], max_q, q.shape[1], max_len))
 
