@@ -495,6 +495,63 @@ tbn_status tbn_window_attention(const void *q, int64_t q_stride, void *out, floa
                                 void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * The cache held in 4 bits: keys and values of half a byte and a power of two for each 32 channels, a quarter of bfloat16's bytes (136 in place of
+ * 512 for a key and value of 128 channels).  A tbn_kv4_pool stands in the place of a layer's tbn_kv_pool; the index, and with it tbn_kv_reserve, _fork, _release
+ * and _compact, are the same.
+ *
+ * A group is 32 neighbouring channels of one key (or value) of one head, 32 c .. 32 c + 31.  With a its largest magnitude, x is the smallest whole
+ * number, -100 .. 125, with a <= 6 * 2^x (125 if there is none); each element becomes the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times 2^x
+ * with its sign (a tie: the one whose code is even; beyond 6 * 2^x: 6).  A code is the place in that list, bit 3 set for negative numbers.  A key and
+ * value of a head of which any element is infinite or not a number stand for not-a-number in all channels of both: exponents are then -128.
+ *
+ *   k    [page][kv_head][row][dim / 2]                          byte b: channels 2 b (low half) and 2 b + 1
+ *   v    [page][kv_head][row / 32][4][16][dim / 16][4]          byte [b][g][n][f][j]: channel 16 f + n of rows 32 b + 8 g + 2 j (low half) and the next
+ *   k_exp, v_exp  [page][kv_head][row][E]                       x of group c at c; E = 4 for dim <= 128, 8 beyond; bytes from dim / 32 on are not looked at
+ */
+typedef struct {
+    void *k;            /* DEVICE, n_pages x kv_heads x page x dim / 2 bytes, 16-byte aligned */
+    void *v;            /* DEVICE, the same */
+    int8_t *k_exp;      /* DEVICE, n_pages x kv_heads x page x E, 16-byte aligned */
+    int8_t *v_exp;      /* DEVICE, the same */
+    int64_t n_pages;    /* at most 2^31 - 1 */
+    int32_t kv_heads;   /* 1 .. 1024 */
+    int32_t dim;        /* a multiple of 32, 32 .. 256 */
+    int32_t page;       /* 32, 64 or 128 */
+} tbn_kv4_pool;
+
+/* tbn_kv_append into this cache; dt: of k_new and v_new.  Keys of a page before the new ones stay as they are. */
+tbn_status tbn_kv4_append(const tbn_kv4_pool *pool, const tbn_kv_index *index, const void *k_new, int64_t k_stride, const void *v_new,
+                          int64_t v_stride, tbn_dtype dt, const int32_t *cu_new, int64_t total, int32_t max_new, void *stream);
+
+/*
+ * The last n = cu[s + 1] - cu[s] keys and values of each sequence as the numbers they stand for (which both types hold exactly), tokens
+ * cu[s] onwards of k_out and v_out: what tbn_kv_append takes, for instance to hand a sequence to another cache.  Nothing is written
+ * for a sequence that has fewer.
+ *   k_out, v_out : DEVICE, total x kv_heads x dim of type dt, dense;  cu : DEVICE, n_seqs + 1, ascending from 0 to total;
+ *   max_n : at least the largest n
+ */
+tbn_status tbn_kv4_read(const tbn_kv4_pool *pool, const tbn_kv_index *index, void *k_out, void *v_out, tbn_dtype dt, const int32_t *cu,
+                        int64_t total, int32_t max_n, void *stream);
+
+/* tbn_kv_copy_pages and tbn_kv_keep of this cache. */
+tbn_status tbn_kv4_copy_pages(const tbn_kv4_pool *pool, const int32_t *src, const int32_t *dst, int64_t n, const int32_t *count,
+                              void *stream);
+tbn_status tbn_kv4_keep(const tbn_kv4_pool *pool, const tbn_kv_index *index, const int32_t *base, const int32_t *picks, int32_t width,
+                        const int32_t *counts, void *stream);
+
+/*
+ * tbn_tree_attention over this cache, with window > 0 tbn_window_attention (n_sink and window as there; window 0: no window, n_sink is not
+ * looked at).  dt: of q and out.  The products are those of the numbers that the codes stand for, with binary32 sums; float32 queries and their weights are
+ * not rounded to fewer than 24 bits, with bfloat16 ones the weights are, as there.
+ */
+size_t tbn_kv4_attention_workspace_bytes(const tbn_kv4_pool *pool, const tbn_kv_index *index, tbn_dtype dt, int64_t total_q,
+                                         int32_t max_q, int32_t heads, int32_t n_sink, int32_t window, int32_t masked, int64_t max_len);
+tbn_status tbn_kv4_attention(const void *q, int64_t q_stride, tbn_dtype dt, void *out, float *lse, const tbn_kv4_pool *pool,
+                             const tbn_kv_index *index, const int32_t *cu_q, int64_t total_q, int32_t max_q, int32_t heads,
+                             int32_t n_sink, int32_t window, const uint32_t *mask, int32_t mask_words, int64_t max_len, float scale,
+                             void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Which pages of its sequence a query attends to.  Queries, sequences and positions as for tbn_tree_attention without a
  * mask; blocks are a sequence's table slots, a query's own block is the one its key lies in.  Per query and kv head:
  * all blocks up to the own one if they are at most n_select; else the first n_sink, the last n_recent up to the own one,

@@ -41,6 +41,12 @@ decltype(&tbn_tree_attention_workspace_bytes) p_tree_attention_workspace_bytes;
 decltype(&tbn_tree_attention) p_tree_attention;
 decltype(&tbn_window_attention_workspace_bytes) p_window_attention_workspace_bytes;
 decltype(&tbn_window_attention) p_window_attention;
+decltype(&tbn_kv4_append) p_kv4_append;
+decltype(&tbn_kv4_read) p_kv4_read;
+decltype(&tbn_kv4_copy_pages) p_kv4_copy_pages;
+decltype(&tbn_kv4_keep) p_kv4_keep;
+decltype(&tbn_kv4_attention_workspace_bytes) p_kv4_attention_workspace_bytes;
+decltype(&tbn_kv4_attention) p_kv4_attention;
 decltype(&tbn_block_select_workspace_bytes) p_block_select_workspace_bytes;
 decltype(&tbn_block_select) p_block_select;
 decltype(&tbn_block_attention_workspace_bytes) p_block_attention_workspace_bytes;
@@ -280,6 +286,7 @@ bool held(PyObject *address, PyObject *gpu, Held &h) {
 }
 
 const tbn_kv_pool *pool_of(const Held &h) { return static_cast<const tbn_kv_pool *>(h.at); }
+const tbn_kv4_pool *pool4_of(const Held &h) { return static_cast<const tbn_kv4_pool *>(h.at); }
 const tbn_kv_index *index_of(const Held &h) { return static_cast<const tbn_kv_index *>(h.at); }
 
 // a dense int32 tensor of at least n entries on the GPU
@@ -289,20 +296,29 @@ int32_t *ints(PyObject *o, int64_t n, int64_t gpu) {
     return static_cast<int32_t *>(t->data_ptr());
 }
 
-// (tokens, heads, dim) of the pool's type, heads dense, tokens `stride` elements apart (heads 0: any number)
-const at::Tensor *rows(PyObject *o, const Held &pool, int64_t heads, int64_t &stride) {
+// (tokens, heads, dim) of type dt, heads dense, tokens `stride` elements apart (heads 0: any number)
+const at::Tensor *rows_of(PyObject *o, int64_t gpu, int64_t dim, at::ScalarType dt, int64_t heads, int64_t &stride) {
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor &t = THPVariable_Unpack(o);
     constexpr c10::DispatchKeySet kWrapped({c10::DispatchKey::FuncTorchBatched, c10::DispatchKey::FuncTorchGradWrapper,
                                             c10::DispatchKey::Functionalize, c10::DispatchKey::Python});
     if (!t.defined() || !t.is_cuda() || t.layout() != at::kStrided || t.dim() != 3 || t.key_set().has_any(kWrapped)) return nullptr;
-    const tbn_kv_pool *p = pool_of(pool);
-    if (t.device().index() != pool.gpu || t.scalar_type() != (p->dt == TBN_F32 ? at::kFloat : at::kBFloat16)) return nullptr;
+    if (t.device().index() != gpu || t.scalar_type() != dt) return nullptr;
     const int64_t n = t.size(0), h = t.size(1), d = t.size(2);
-    if (d != p->dim || h < 1 || h > 65536 || (heads && h != heads) || n < 1) return nullptr;
+    if (d != dim || h < 1 || h > 65536 || (heads && h != heads) || n < 1) return nullptr;
     if (t.stride(2) != 1 || (h > 1 && t.stride(1) != d) || (n > 1 && t.stride(0) < h * d)) return nullptr;
     stride = n > 1 ? t.stride(0) : h * d;
     return &t;
+}
+// of the pool's type
+const at::Tensor *rows(PyObject *o, const Held &pool, int64_t heads, int64_t &stride) {
+    return rows_of(o, pool.gpu, pool_of(pool)->dim, pool_of(pool)->dt == TBN_F32 ? at::kFloat : at::kBFloat16, heads, stride);
+}
+// for a pool in 4 bits: of either type
+const at::Tensor *rows4(PyObject *o, const Held &pool, int64_t heads, int64_t &stride, tbn_dtype &dt) {
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    return t.defined() && activations(t, dt) ? rows_of(o, pool.gpu, pool4_of(pool)->dim, t.scalar_type(), heads, stride) : nullptr;
 }
 
 // the library's call, without the interpreter's lock: a launch may wait for room in a queue
@@ -365,15 +381,28 @@ PyObject *kv_release(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
 }
 
 // (pool, gpu, src, dst, count or None)
-PyObject *kv_copy_pages(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
-    HANDLE_TH_ERRORS
+template <typename Call>
+PyObject *copy_pages(PyObject *const *args, Py_ssize_t n_args, Call call) {
     Held pool;
     if (n_args != 5 || !ordinary_context() || !held(args[0], args[1], pool)) Py_RETURN_NONE;
     const int32_t *a = ints(args[2], 0, pool.gpu), *b = ints(args[3], 0, pool.gpu), *count = args[4] == Py_None ? nullptr : ints(args[4], 1, pool.gpu);
     if (!a || !b || (!count && args[4] != Py_None)) Py_RETURN_NONE;
     const int64_t n = THPVariable_Unpack(args[2]).numel();
     if (THPVariable_Unpack(args[3]).numel() != n) Py_RETURN_NONE;
-    return none(unlocked([&] { return p_kv_copy_pages(pool_of(pool), a, b, n, count, stream()); }));
+    return none(unlocked([&] { return call(pool, a, b, n, count); }));
+}
+PyObject *kv_copy_pages(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    return copy_pages(args, n_args, [](const Held &pool, const int32_t *a, const int32_t *b, int64_t n, const int32_t *count) {
+        return p_kv_copy_pages(pool_of(pool), a, b, n, count, stream());
+    });
+    END_HANDLE_TH_ERRORS
+}
+PyObject *kv4_copy_pages(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    return copy_pages(args, n_args, [](const Held &pool, const int32_t *a, const int32_t *b, int64_t n, const int32_t *count) {
+        return p_kv4_copy_pages(pool4_of(pool), a, b, n, count, stream());
+    });
     END_HANDLE_TH_ERRORS
 }
 
@@ -390,9 +419,42 @@ PyObject *kv_append(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     END_HANDLE_TH_ERRORS
 }
 
-// (pool, gpu, index, gpu, base, picks, counts)
-PyObject *kv_keep(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+// (pool, gpu, index, gpu, k_new, v_new, cu_new, max_new)
+PyObject *kv4_append(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     HANDLE_TH_ERRORS
+    Held pool, ix;
+    int64_t most, ks, vs;
+    tbn_dtype dt, vt;
+    if (n_args != 8 || !ordinary_context() || !held(args[0], args[1], pool) || !held(args[2], args[3], ix) || pool.gpu != ix.gpu) Py_RETURN_NONE;
+    const at::Tensor *k = rows4(args[4], pool, pool4_of(pool)->kv_heads, ks, dt), *v = rows4(args[5], pool, pool4_of(pool)->kv_heads, vs, vt);
+    const int32_t *cu = ints(args[6], int64_t(index_of(ix)->n_seqs) + 1, ix.gpu);
+    if (!k || !v || !cu || dt != vt || k->size(0) != v->size(0) || !integer(args[7], 0, INT32_MAX, most)) Py_RETURN_NONE;
+    return none(unlocked([&] { return p_kv4_append(pool4_of(pool), index_of(ix), k->data_ptr(), ks, v->data_ptr(), vs, dt, cu, k->size(0), static_cast<int32_t>(most), stream()); }));
+    END_HANDLE_TH_ERRORS
+}
+
+// (pool, gpu, index, gpu, cu, max_n, total, float32)
+PyObject *kv4_read(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    Held pool, ix;
+    int64_t most, total;
+    if (n_args != 8 || !ordinary_context() || !held(args[0], args[1], pool) || !held(args[2], args[3], ix) || pool.gpu != ix.gpu) Py_RETURN_NONE;
+    const int32_t *cu = ints(args[4], int64_t(index_of(ix)->n_seqs) + 1, ix.gpu);
+    if (!cu || !integer(args[5], 0, INT32_MAX, most) || !integer(args[6], 1, 1 << 30, total) || !PyBool_Check(args[7])) Py_RETURN_NONE;
+    const bool f32 = args[7] == Py_True;
+    const auto *p = pool4_of(pool);
+    const auto options = THPVariable_Unpack(args[4]).options().dtype(f32 ? at::kFloat : at::kBFloat16);
+    at::Tensor k = at::empty({total, p->kv_heads, p->dim}, options), v = at::empty({total, p->kv_heads, p->dim}, options);
+    const tbn_status st = unlocked([&] {
+        return p_kv4_read(p, index_of(ix), k.data_ptr(), v.data_ptr(), f32 ? TBN_F32 : TBN_BF16, cu, total, static_cast<int32_t>(most), stream());
+    });
+    return result(st, two, k, v);
+    END_HANDLE_TH_ERRORS
+}
+
+// (pool, gpu, index, gpu, base, picks, counts)
+template <typename Call>
+PyObject *keep_keys(PyObject *const *args, Py_ssize_t n_args, Call call) {
     Held pool, ix;
     if (n_args != 7 || !ordinary_context() || !held(args[0], args[1], pool) || !held(args[2], args[3], ix) || pool.gpu != ix.gpu) Py_RETURN_NONE;
     const int64_t n = index_of(ix)->n_seqs;
@@ -400,7 +462,20 @@ PyObject *kv_keep(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     if (!base || !picks || !counts) Py_RETURN_NONE;
     const at::Tensor &t = THPVariable_Unpack(args[5]);
     if (t.dim() != 2 || t.size(0) != n || t.size(1) > INT32_MAX) Py_RETURN_NONE;
-    return none(unlocked([&] { return p_kv_keep(pool_of(pool), index_of(ix), base, picks, static_cast<int32_t>(t.size(1)), counts, stream()); }));
+    return none(unlocked([&] { return call(pool, index_of(ix), base, picks, static_cast<int32_t>(t.size(1)), counts); }));
+}
+PyObject *kv_keep(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    return keep_keys(args, n_args, [](const Held &pool, const tbn_kv_index *ix, const int32_t *base, const int32_t *picks, int32_t width, const int32_t *counts) {
+        return p_kv_keep(pool_of(pool), ix, base, picks, width, counts, stream());
+    });
+    END_HANDLE_TH_ERRORS
+}
+PyObject *kv4_keep(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    return keep_keys(args, n_args, [](const Held &pool, const tbn_kv_index *ix, const int32_t *base, const int32_t *picks, int32_t width, const int32_t *counts) {
+        return p_kv4_keep(pool4_of(pool), ix, base, picks, width, counts, stream());
+    });
     END_HANDLE_TH_ERRORS
 }
 
@@ -409,20 +484,21 @@ struct QueryArgs {
     const at::Tensor *q;
     int64_t stride, max_q, max_len;
     const int32_t *cu;
+    tbn_dtype dt;
 };
 
 // (q, pool, gpu, index, gpu, cu_q, max_q, max_len or None, ...)
-bool queries(PyObject *const *args, QueryArgs &a) {
+bool queries(PyObject *const *args, QueryArgs &a, bool four = false) {
     if (!ordinary_context() || !held(args[1], args[2], a.pool) || !held(args[3], args[4], a.ix) || a.pool.gpu != a.ix.gpu) return false;
-    a.q = rows(args[0], a.pool, 0, a.stride);
-    if (!a.q || a.q->size(1) % pool_of(a.pool)->kv_heads) return false;
+    a.q = four ? rows4(args[0], a.pool, 0, a.stride, a.dt) : rows(args[0], a.pool, 0, a.stride);
+    if (!a.q || a.q->size(1) % (four ? pool4_of(a.pool)->kv_heads : pool_of(a.pool)->kv_heads)) return false;
     a.cu = ints(args[5], int64_t(index_of(a.ix)->n_seqs) + 1, a.ix.gpu);
     a.max_len = 0;
     return a.cu && integer(args[6], 0, INT32_MAX, a.max_q) && (args[7] == Py_None || integer(args[7], 0, kMaxElems, a.max_len));
 }
 
-bool scale_of(PyObject *o, const Held &pool, float &scale) {
-    if (o == Py_None) scale = static_cast<float>(1.0 / std::sqrt(static_cast<double>(pool_of(pool)->dim)));
+bool scale_of(PyObject *o, int32_t dim, float &scale) {
+    if (o == Py_None) scale = static_cast<float>(1.0 / std::sqrt(static_cast<double>(dim)));
     else if (PyFloat_CheckExact(o)) scale = static_cast<float>(PyFloat_AS_DOUBLE(o));
     else return false;
     return true;
@@ -449,7 +525,7 @@ PyObject *window_attention(PyObject *, PyObject *const *args, Py_ssize_t n_args)
     int64_t sink, window;
     const uint32_t *mask;
     int32_t words;
-    if (n_args != 12 || !queries(args, a) || !scale_of(args[9], a.pool, scale) || !integer(args[10], 0, INT32_MAX, sink) || !integer(args[11], 1, INT32_MAX, window) ||
+    if (n_args != 12 || !queries(args, a) || !scale_of(args[9], pool_of(a.pool)->dim, scale) || !integer(args[10], 0, INT32_MAX, sink) || !integer(args[11], 1, INT32_MAX, window) ||
         !mask_of(args[8], a.ix, a.q->size(0), mask, words))
         Py_RETURN_NONE;
     const int64_t n = a.q->size(0), heads = a.q->size(1);
@@ -467,6 +543,31 @@ PyObject *window_attention(PyObject *, PyObject *const *args, Py_ssize_t n_args)
     END_HANDLE_TH_ERRORS
 }
 
+PyObject *kv4_attention(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    QueryArgs a;
+    float scale;
+    int64_t sink, window;
+    const uint32_t *mask;
+    int32_t words;
+    if (n_args != 12 || !queries(args, a, true) || !scale_of(args[9], pool4_of(a.pool)->dim, scale) || !integer(args[10], 0, INT32_MAX, sink) ||
+        !integer(args[11], 0, INT32_MAX, window) || !mask_of(args[8], a.ix, a.q->size(0), mask, words))
+        Py_RETURN_NONE;
+    const int64_t n = a.q->size(0), heads = a.q->size(1);
+    const int32_t max_q = static_cast<int32_t>(a.max_q), H = static_cast<int32_t>(heads), n_sink = static_cast<int32_t>(sink), w = static_cast<int32_t>(window);
+    const auto *pool = pool4_of(a.pool);
+    const auto *ix = index_of(a.ix);
+    at::Tensor out = at::empty({n, heads, pool->dim}, a.q->options()), lse = at::empty({n, heads}, a.q->options().dtype(at::kFloat)), ws;
+    const size_t need = p_kv4_attention_workspace_bytes(pool, ix, a.dt, n, max_q, H, n_sink, w, mask != nullptr, a.max_len);
+    if (need) ws = bytes_like(*a.q, need);
+    const tbn_status st = unlocked([&] {
+        return p_kv4_attention(a.q->data_ptr(), a.stride, a.dt, out.data_ptr(), floats(lse), pool, ix, a.cu, n, max_q, H, n_sink, w, mask, words, a.max_len, scale,
+                               need ? ws.data_ptr() : nullptr, need, stream());
+    });
+    return result(st, two, out, lse);
+    END_HANDLE_TH_ERRORS
+}
+
 // (.., mask or None, scale or None)
 PyObject *tree_attention(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     HANDLE_TH_ERRORS
@@ -474,7 +575,7 @@ PyObject *tree_attention(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     float scale;
     const uint32_t *mask;
     int32_t words;
-    if (n_args != 10 || !queries(args, a) || !scale_of(args[9], a.pool, scale) || !mask_of(args[8], a.ix, a.q->size(0), mask, words)) Py_RETURN_NONE;
+    if (n_args != 10 || !queries(args, a) || !scale_of(args[9], pool_of(a.pool)->dim, scale) || !mask_of(args[8], a.ix, a.q->size(0), mask, words)) Py_RETURN_NONE;
     const int64_t n = a.q->size(0), heads = a.q->size(1);
     const auto *pool = pool_of(a.pool);
     const auto *ix = index_of(a.ix);
@@ -516,7 +617,7 @@ PyObject *block_attention(PyObject *, PyObject *const *args, Py_ssize_t n_args) 
     HANDLE_TH_ERRORS
     QueryArgs a;
     float scale;
-    if (n_args != 10 || !queries(args, a) || !scale_of(args[9], a.pool, scale)) Py_RETURN_NONE;
+    if (n_args != 10 || !queries(args, a) || !scale_of(args[9], pool_of(a.pool)->dim, scale)) Py_RETURN_NONE;
     const int64_t n = a.q->size(0), heads = a.q->size(1);
     const auto *pool = pool_of(a.pool);
     const auto *ix = index_of(a.ix);
@@ -566,6 +667,12 @@ PyObject *init(PyObject *, PyObject *args) {
     take(p_tree_attention, "tbn_tree_attention");
     take(p_window_attention_workspace_bytes, "tbn_window_attention_workspace_bytes");
     take(p_window_attention, "tbn_window_attention");
+    take(p_kv4_append, "tbn_kv4_append");
+    take(p_kv4_read, "tbn_kv4_read");
+    take(p_kv4_copy_pages, "tbn_kv4_copy_pages");
+    take(p_kv4_keep, "tbn_kv4_keep");
+    take(p_kv4_attention_workspace_bytes, "tbn_kv4_attention_workspace_bytes");
+    take(p_kv4_attention, "tbn_kv4_attention");
     take(p_block_select_workspace_bytes, "tbn_block_select_workspace_bytes");
     take(p_block_select, "tbn_block_select");
     take(p_block_attention_workspace_bytes, "tbn_block_attention_workspace_bytes");
@@ -584,7 +691,8 @@ PyObject *init(PyObject *, PyObject *args) {
 PyMethodDef methods[] = {TBN_FAST(linear_forward), TBN_FAST(conv2d_forward), TBN_FAST(linear_coltiled_forward), TBN_FAST(sign_pack),
                          TBN_FAST(linear_forward_binact), TBN_FAST(pack_tile),
                          TBN_FAST(kv_reserve), TBN_FAST(kv_fork), TBN_FAST(kv_release), TBN_FAST(kv_copy_pages), TBN_FAST(kv_append), TBN_FAST(kv_keep),
-                         TBN_FAST(tree_attention), TBN_FAST(window_attention), TBN_FAST(block_select), TBN_FAST(block_attention), {"init", init, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         TBN_FAST(tree_attention), TBN_FAST(window_attention), TBN_FAST(kv4_append), TBN_FAST(kv4_read),
+                         TBN_FAST(kv4_copy_pages), TBN_FAST(kv4_keep), TBN_FAST(kv4_attention), TBN_FAST(block_select), TBN_FAST(block_attention), {"init", init, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tbn_host", "plain calls of the binding on C++ tensors", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

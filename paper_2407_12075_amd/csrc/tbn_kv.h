@@ -42,6 +42,18 @@ size_t block_select_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, cons
 tbn_status launch_block_select(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, int32_t *picks, int32_t n_select, int32_t n_sink,
                                int32_t n_recent, uint32_t *ws, hipStream_t stream);
 
+tbn_status launch_kv4_append(const tbn_kv4_pool &p, const tbn_kv_index &ix, const void *k_new, int64_t k_stride, const void *v_new, int64_t v_stride,
+                             tbn_dtype dt, const int32_t *cu_new, int64_t total, int32_t max_new, hipStream_t stream);
+tbn_status launch_kv4_read(const tbn_kv4_pool &p, const tbn_kv_index &ix, void *k, void *v, tbn_dtype dt, const int32_t *cu, int64_t total, int32_t most,
+                           hipStream_t stream);
+tbn_status launch_kv4_copy_pages(const tbn_kv4_pool &p, const int32_t *src, const int32_t *dst, int64_t n, const int32_t *count, hipStream_t stream);
+tbn_status launch_kv4_keep(const tbn_kv4_pool &p, const tbn_kv_index &ix, const int32_t *base, const int32_t *picks, int32_t width, const int32_t *counts,
+                           hipStream_t stream);
+// window: 0 for none
+size_t kv4_attention_workspace(const tbn_kv4_pool &p, const tbn_kv_index &ix, const KvQueries &q, tbn_dtype dt, int32_t n_sink, int32_t window, bool masked);
+tbn_status launch_kv4_attention(const tbn_kv4_pool &p, const tbn_kv_index &ix, const KvQueries &q, tbn_dtype dt, void *out, float *lse, int32_t n_sink,
+                                int32_t window, const uint32_t *mask, int32_t mask_words, float scale, float *ws, hipStream_t stream);
+
 #if defined(__HIPCC__)
 
 // what the GPU's data say is bounded before it becomes an address

@@ -37,13 +37,6 @@ tbn_status check_pool(const char *fn, const tbn_kv_pool *p) {
     return TBN_OK;
 }
 
-tbn_status check_both(const char *fn, const tbn_kv_pool *p, const tbn_kv_index *ix) {
-    tbn_status st = check_pool(fn, p);
-    if (st == TBN_OK) st = check_index(fn, ix);
-    if (st == TBN_OK && (p->page != ix->page || p->n_pages != ix->n_pages)) st = fail(TBN_ERR_SHAPE, fn, "pool and index must agree on page and n_pages");
-    return st;
-}
-
 tbn_status check_workspace(const char *fn, size_t need, const void *ws, size_t bytes, unsigned to) {
     if (need && (!ws || bytes < need || !aligned(ws, to))) {
         set_error("%s: workspace of %zu bytes, %u-byte aligned, required (got %zu at %p)", fn, need, to, bytes, ws);
@@ -52,8 +45,30 @@ tbn_status check_workspace(const char *fn, size_t need, const void *ws, size_t b
     return TBN_OK;
 }
 
+tbn_status check_pool(const char *fn, const tbn_kv4_pool *p) {
+    if (!p) return fail(TBN_ERR_NULL, fn, "pool must not be NULL");
+    if (!p->k || !p->v || !p->k_exp || !p->v_exp) return fail(TBN_ERR_NULL, fn, "k, v, k_exp and v_exp of the pool must not be NULL");
+    if (p->n_pages < 1 || p->kv_heads < 1 || p->dim < 1 || p->page < 1) return fail(TBN_ERR_SHAPE, fn, "sizes of the pool must be positive");
+    if (!page_ok(p->page) || p->dim % 32 || p->dim > kMaxDim || p->kv_heads > 1024 || p->n_pages > INT32_MAX)
+        return fail(TBN_ERR_UNSUPPORTED, fn, "pages of 32, 64 or 128 keys, dim a multiple of 32 up to 256, at most 1024 kv heads and 2^31 - 1 pages");
+    if (!aligned(p->k, 16) || !aligned(p->v, 16) || !aligned(p->k_exp, 16) || !aligned(p->v_exp, 16))
+        return fail(TBN_ERR_UNSUPPORTED, fn, "k, v, k_exp and v_exp of the pool must be 16-byte aligned");
+    return TBN_OK;
+}
+
+template <typename Pool>
+tbn_status check_both(const char *fn, const Pool *p, const tbn_kv_index *ix) {
+    tbn_status st = check_pool(fn, p);
+    if (st == TBN_OK) st = check_index(fn, ix);
+    if (st == TBN_OK && (p->page != ix->page || p->n_pages != ix->n_pages)) st = fail(TBN_ERR_SHAPE, fn, "pool and index must agree on page and n_pages");
+    return st;
+}
+
+tbn_status check_type(const char *fn, tbn_dtype dt) { return dt == TBN_F32 || dt == TBN_BF16 ? TBN_OK : fail(TBN_ERR_UNSUPPORTED, fn, "unknown dtype"); }
+
 // pool, index, queries; max_len becomes 1 .. max_pages * page
-tbn_status check_queries(const char *fn, const tbn_kv_pool *p, const tbn_kv_index *ix, KvQueries &q) {
+template <typename Pool>
+tbn_status check_queries(const char *fn, const Pool *p, const tbn_kv_index *ix, KvQueries &q) {
     const tbn_status st = check_both(fn, p, ix);
     if (st != TBN_OK) return st;
     const int64_t most = int64_t(ix->max_pages) * ix->page;
@@ -66,11 +81,28 @@ tbn_status check_queries(const char *fn, const tbn_kv_pool *p, const tbn_kv_inde
     return TBN_OK;
 }
 
-tbn_status check_query_pointers(const char *fn, const tbn_kv_pool *p, const KvQueries &q, const void *out) {
+template <typename Pool>
+tbn_status check_query_pointers(const char *fn, const Pool *p, const KvQueries &q, const void *out) {
     if (!q.q || !out || !q.cu_q) return fail(TBN_ERR_NULL, fn, "q, the output and cu_q must not be NULL");
     if (q.q_stride < int64_t(q.heads) * p->dim || q.q_stride > (int64_t(1) << 40)) return fail(TBN_ERR_SHAPE, fn, "q_stride must be at least heads * dim (and at most 2^40)");
     return TBN_OK;
 }
+
+// tokens of a call that appends to a pool or reads from it
+tbn_status check_tokens(const char *fn, int64_t total, int32_t most) {
+    if (total < 0 || most < 0) return fail(TBN_ERR_SHAPE, fn, "the number of tokens, all and of a sequence, must be >= 0");
+    if (total > (1 << 30)) return fail(TBN_ERR_UNSUPPORTED, fn, "at most 2^30 tokens");
+    return TBN_OK;
+}
+
+template <typename Pool>
+tbn_status check_strides(const char *fn, const Pool *pool, int64_t k_stride, int64_t v_stride) {
+    const int64_t row = int64_t(pool->kv_heads) * pool->dim, lim = int64_t(1) << 40;
+    if (k_stride < row || v_stride < row || k_stride > lim || v_stride > lim) return fail(TBN_ERR_SHAPE, fn, "k_stride and v_stride must be at least kv_heads * dim (and at most 2^40)");
+    return TBN_OK;
+}
+
+int32_t least(int32_t a, int64_t b) { return a < b ? a : static_cast<int32_t>(b); }
 
 }  // namespace
 
@@ -139,16 +171,14 @@ tbn_status tbn_kv_copy_pages(const tbn_kv_pool *pool, const int32_t *src, const 
 tbn_status tbn_kv_append(const tbn_kv_pool *pool, const tbn_kv_index *index, const void *k_new, int64_t k_stride, const void *v_new,
                          int64_t v_stride, const int32_t *cu_new, int64_t total, int32_t max_new, void *stream) {
     const char *fn = "tbn_kv_append";
-    const tbn_status st = check_both(fn, pool, index);
+    tbn_status st = check_both(fn, pool, index);
     if (st != TBN_OK) return st;
-    if (total < 0 || max_new < 0) return fail(TBN_ERR_SHAPE, fn, "total and max_new must be >= 0");
-    if (total > (1 << 30)) return fail(TBN_ERR_UNSUPPORTED, fn, "at most 2^30 tokens");
+    if ((st = check_tokens(fn, total, max_new)) != TBN_OK) return st;
     if (total == 0 || max_new == 0) return TBN_OK;
     if (!k_new || !v_new || !cu_new) return fail(TBN_ERR_NULL, fn, "k_new, v_new and cu_new must not be NULL");
-    const int64_t row = int64_t(pool->kv_heads) * pool->dim, lim = int64_t(1) << 40;
-    if (k_stride < row || v_stride < row || k_stride > lim || v_stride > lim) return fail(TBN_ERR_SHAPE, fn, "k_stride and v_stride must be at least kv_heads * dim (and at most 2^40)");
+    if ((st = check_strides(fn, pool, k_stride, v_stride)) != TBN_OK) return st;
     drop_stale_error();
-    return launch_kv_append(*pool, *index, k_new, k_stride, v_new, v_stride, cu_new, total, max_new < total ? max_new : static_cast<int32_t>(total), static_cast<hipStream_t>(stream));
+    return launch_kv_append(*pool, *index, k_new, k_stride, v_new, v_stride, cu_new, total, least(max_new, total), static_cast<hipStream_t>(stream));
 }
 
 tbn_status tbn_kv_keep(const tbn_kv_pool *pool, const tbn_kv_index *index, const int32_t *base, const int32_t *picks, int32_t width,
@@ -221,6 +251,87 @@ tbn_status tbn_window_attention(const void *q, int64_t q_stride, void *out, floa
     drop_stale_error();
     return launch_window_attention(*pool, *index, a, out, lse, n_sink, window, mask, mask_words, scale, static_cast<float *>(workspace),
                                    static_cast<hipStream_t>(stream));
+}
+
+tbn_status tbn_kv4_append(const tbn_kv4_pool *pool, const tbn_kv_index *index, const void *k_new, int64_t k_stride, const void *v_new, int64_t v_stride,
+                          tbn_dtype dt, const int32_t *cu_new, int64_t total, int32_t max_new, void *stream) {
+    const char *fn = "tbn_kv4_append";
+    tbn_status st = check_both(fn, pool, index);
+    if (st == TBN_OK) st = check_type(fn, dt);
+    if (st == TBN_OK) st = check_tokens(fn, total, max_new);
+    if (st != TBN_OK || total == 0 || max_new == 0) return st;
+    if (!k_new || !v_new || !cu_new) return fail(TBN_ERR_NULL, fn, "k_new, v_new and cu_new must not be NULL");
+    if ((st = check_strides(fn, pool, k_stride, v_stride)) != TBN_OK) return st;
+    drop_stale_error();
+    return launch_kv4_append(*pool, *index, k_new, k_stride, v_new, v_stride, dt, cu_new, total, least(max_new, total), static_cast<hipStream_t>(stream));
+}
+
+tbn_status tbn_kv4_read(const tbn_kv4_pool *pool, const tbn_kv_index *index, void *k_out, void *v_out, tbn_dtype dt, const int32_t *cu, int64_t total,
+                        int32_t max_n, void *stream) {
+    const char *fn = "tbn_kv4_read";
+    tbn_status st = check_both(fn, pool, index);
+    if (st == TBN_OK) st = check_type(fn, dt);
+    if (st == TBN_OK) st = check_tokens(fn, total, max_n);
+    if (st != TBN_OK || total == 0 || max_n == 0) return st;
+    if (!k_out || !v_out || !cu) return fail(TBN_ERR_NULL, fn, "k_out, v_out and cu must not be NULL");
+    drop_stale_error();
+    return launch_kv4_read(*pool, *index, k_out, v_out, dt, cu, total, least(max_n, total), static_cast<hipStream_t>(stream));
+}
+
+tbn_status tbn_kv4_copy_pages(const tbn_kv4_pool *pool, const int32_t *src, const int32_t *dst, int64_t n, const int32_t *count, void *stream) {
+    const char *fn = "tbn_kv4_copy_pages";
+    const tbn_status st = check_pool(fn, pool);
+    if (st != TBN_OK) return st;
+    if (n < 0 || n > INT32_MAX) return fail(TBN_ERR_SHAPE, fn, "n must be 0 .. 2^31 - 1");
+    if (n == 0) return TBN_OK;
+    if (!src || !dst) return fail(TBN_ERR_NULL, fn, "src and dst must not be NULL");
+    drop_stale_error();
+    return launch_kv4_copy_pages(*pool, src, dst, n, count, static_cast<hipStream_t>(stream));
+}
+
+tbn_status tbn_kv4_keep(const tbn_kv4_pool *pool, const tbn_kv_index *index, const int32_t *base, const int32_t *picks, int32_t width,
+                        const int32_t *counts, void *stream) {
+    const char *fn = "tbn_kv4_keep";
+    const tbn_status st = check_both(fn, pool, index);
+    if (st != TBN_OK) return st;
+    if (width < 0) return fail(TBN_ERR_SHAPE, fn, "width must be >= 0");
+    if (width == 0) return TBN_OK;
+    if (!base || !picks || !counts) return fail(TBN_ERR_NULL, fn, "base, picks and counts must not be NULL");
+    drop_stale_error();
+    return launch_kv4_keep(*pool, *index, base, picks, width, counts, static_cast<hipStream_t>(stream));
+}
+
+// a call on the cache in 4 bits without a window passes with any n_sink
+static tbn_status check_kv4(const char *fn, const tbn_kv4_pool *pool, const tbn_kv_index *index, tbn_dtype dt, KvQueries &q, bool masked, int32_t &n_sink,
+                            int32_t &window) {
+    tbn_status st = check_queries(fn, pool, index, q);
+    if (st == TBN_OK) st = check_type(fn, dt);
+    if (st == TBN_OK && window != 0) st = check_window(fn, q, masked, n_sink, window);
+    return st;
+}
+
+size_t tbn_kv4_attention_workspace_bytes(const tbn_kv4_pool *pool, const tbn_kv_index *index, tbn_dtype dt, int64_t total_q, int32_t max_q, int32_t heads,
+                                         int32_t n_sink, int32_t window, int32_t masked, int64_t max_len) {
+    KvQueries q{nullptr, 0, nullptr, total_q, max_q, heads, max_len};
+    if (check_kv4(nullptr, pool, index, dt, q, masked != 0, n_sink, window) != TBN_OK || total_q == 0 || max_q == 0) return 0;
+    return kv4_attention_workspace(*pool, *index, q, dt, n_sink, window, masked != 0);
+}
+
+tbn_status tbn_kv4_attention(const void *q, int64_t q_stride, tbn_dtype dt, void *out, float *lse, const tbn_kv4_pool *pool, const tbn_kv_index *index,
+                             const int32_t *cu_q, int64_t total_q, int32_t max_q, int32_t heads, int32_t n_sink, int32_t window, const uint32_t *mask,
+                             int32_t mask_words, int64_t max_len, float scale, void *workspace, size_t workspace_bytes, void *stream) {
+    const char *fn = "tbn_kv4_attention";
+    KvQueries a{q, q_stride, cu_q, total_q, max_q, heads, max_len};
+    tbn_status st = check_kv4(fn, pool, index, dt, a, mask != nullptr, n_sink, window);
+    if (st != TBN_OK) return st;
+    if (mask && (mask_words < 0 || int64_t(mask_words) * 32 < max_q)) return fail(TBN_ERR_SHAPE, fn, "mask_words must hold max_q bits");
+    if (total_q == 0 || max_q == 0) return TBN_OK;
+    st = check_query_pointers(fn, pool, a, out);
+    if (st == TBN_OK) st = check_workspace(fn, kv4_attention_workspace(*pool, *index, a, dt, n_sink, window, mask != nullptr), workspace, workspace_bytes, 16);
+    if (st != TBN_OK) return st;
+    drop_stale_error();
+    return launch_kv4_attention(*pool, *index, a, dt, out, lse, n_sink, window, mask, mask_words, scale, static_cast<float *>(workspace),
+                                static_cast<hipStream_t>(stream));
 }
 
 static tbn_status check_select(const char *fn, const tbn_kv_pool *pool, const tbn_kv_index *index, KvQueries &q) {

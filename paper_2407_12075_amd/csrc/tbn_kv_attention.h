@@ -1,6 +1,8 @@
 // What the attention kernels share (tbn_kv_attention.hip, tbn_kv_rows.hip): arguments, operands, masks.
 #pragma once
+#include <algorithm>
 #include <cfloat>
+#include <cmath>
 
 #include "tbn_kv.h"
 
@@ -36,6 +38,7 @@ struct AttentionArgs {   // of one launch
     int32_t n_chunks;
     int32_t row_tiles;  // tiles of a workgroup's rows
     int32_t n_sink, window;   // of a call with a window: the first keys that every token sees, and how many up to its own place
+    const int8_t *k_exp, *v_exp;   // of a cache in 4 bits (p.k, p.v: its codes, p.dt: the queries' type)
 };
 
 // what the rows of a launch see: every key up to their own, the pages they picked, the first keys and a window
@@ -301,6 +304,65 @@ __device__ __forceinline__ void store_sums(const AttentionArgs &a, int chunk, in
         if (d == 0 && a.lse) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
     }
 }
+
+// How a call is spread over workgroups.
+struct Plan {
+    int rows, chunk, n_chunks, row_tiles;   // rows of a workgroup; stretches of keys
+    bool staged;                            // by a kernel that stages keys in LDS
+};
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Whether a launch has a row of workgroups per token of the call instead of per place of the index (sequence_of): where no token is without work, or
+// places are many more.
+inline bool by_token(const tbn_kv_index &ix, const KvQueries &q) { return q.total_q < ix.n_seqs && (q.max_q == 1 || 16 * q.total_q <= ix.n_seqs); }
+
+// Workgroups of a launch whose rows may mostly be idle, at most: 0.2 - 0.6 ns each where they end at once, small against the work.
+inline double most_blocks(int64_t keys) { return std::min(150000., 16384. + 8. * keys); }
+
+// An index has room for more sequences than are there, so keys are split by the sequences of the call: max_q tokens each would be the fewest; drafts are
+// ragged, half of max_q and more in the mean, so twice that (16 trees of up to 26 tokens: 49 us, 58 with the fewest).  One token on 131000 keys in one of 64
+// places: 101 us, 1065 split by places; a tree of 26: 124 and 1383.  But every place (or token, whose idle workgroups take five times as long) has its row
+// of workgroups: beyond most_blocks they are split as if for twice as many sequences, and so on up to one for each row.
+// keys: that a sequence of the call has for a row of workgroups to go through, at most.  plan(rows of a sequence, sequences x kv heads, keys).
+template <typename F>
+Plan plan_by_sequences(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, int64_t keys, F plan) {
+    const int64_t rows = int64_t(q.max_q) * (q.heads / p.kv_heads);
+    const bool token = by_token(ix, q);
+    const int64_t most = token ? q.total_q : ix.n_seqs;
+    const double weight = most * (token && q.max_q > 1 ? 5. : 1.), join = double(q.max_q) * q.heads;
+    int64_t sequences = std::min<int64_t>({ix.n_seqs, q.total_q, 2 * ceil_div(q.total_q, q.max_q)});
+    for (;; sequences = std::min(most, 2 * sequences)) {
+        const Plan pl = plan(rows, sequences * p.kv_heads, keys);
+        const double blocks = double(pl.n_chunks) * pl.row_tiles * p.kv_heads + (pl.n_chunks > 16 ? join : pl.n_chunks > 1 ? join / 4 : 0.);
+        if (sequences >= most || blocks * weight <= most_blocks(keys)) return pl;
+    }
+}
+
+// Keys that a workgroup of `rows` rows at most goes through in a call with a window, at most: the first pages, the window of its first row and
+// what its other rows add.
+inline int64_t window_keys(const tbn_kv_pool &p, const KvQueries &q, int32_t n_sink, int32_t window, bool masked, int rows = 128) {
+    const int64_t tokens = masked ? q.max_q : std::min<int64_t>(q.max_q, rows / (q.heads / p.kv_heads) + 2);
+    return std::min(q.max_len, ceil_div(n_sink, p.page) * p.page + window + tokens + 2 * p.page);
+}
+
+inline size_t workspace_of(const tbn_kv_pool &p, const KvQueries &q, const Plan &pl) {
+    return pl.n_chunks > 1 ? static_cast<size_t>(pl.n_chunks) * q.total_q * q.heads * (p.dim + 4) * 4 : 0;
+}
+
+// c and the sign of a call's scale
+inline float factor_of(float scale) {
+    const float c = fabsf(scale) * kLog2e;
+    return c < 1e-37f ? 1e-37f : c;
+}
+inline uint32_t flip_of(const tbn_kv_pool &p, float scale) { return !(scale < 0.f) ? 0u : p.dt == TBN_F32 ? 0x80000000u : 0x80008000u; }
+
+constexpr int64_t kMostBlocks = 0x7fffffff;   // workgroups of a sequence
+
+// Fills in how `pl` splits the call and the grid of its launch; an error where one launch cannot hold it.
+tbn_status spread(AttentionArgs &a, const Plan &pl, float *ws, Kind kind, const char *what, dim3 &grid, bool &tokens);
+// the second kernel of a split call
+void launch_kv_join(const AttentionArgs &a, Kind kind, int tile_rows, bool tokens, unsigned groups, hipStream_t stream);
 
 // picked blocks, bfloat16: queries that share a workgroup (0: none), 32 rows at most
 int picked_queries(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, int32_t n_select);

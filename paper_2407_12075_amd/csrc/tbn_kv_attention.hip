@@ -442,13 +442,6 @@ void launch_join(const AttentionArgs &a, int tile_rows, unsigned groups, hipStre
     else hipLaunchKernelGGL((kv_join_kernel<T, KIND, false, TOKENS>), dim3(static_cast<unsigned>((rows + kAttnWaves - 1) / kAttnWaves), groups), dim3(kAttnThreads), 0, stream, a, tile_rows);
 }
 
-struct Plan {
-    int rows, chunk, n_chunks, row_tiles;   // rows of a workgroup: 16 (float32 up to 64) in this file's kernel, 64 or 128 in the one for many rows
-    bool staged;                            // the latter
-};
-
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
 int padded_dim(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 
 // Rows of a workgroup of this file's kernel: what the registers hold of queries and sums.  (bfloat16: more rows go to the other kernel.)
@@ -508,37 +501,12 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, 
     return pl;
 }
 
-// Whether a launch has a row of workgroups per token of the call instead of per place of the index (sequence_of): where no token is without work, or
-// places are many more.
-bool by_token(const tbn_kv_index &ix, const KvQueries &q) { return q.total_q < ix.n_seqs && (q.max_q == 1 || 16 * q.total_q <= ix.n_seqs); }
-
-// Workgroups of a launch whose rows may mostly be idle, at most: 0.2 - 0.6 ns each where they end at once, small against the work.
-double most_blocks(int64_t keys) { return std::min(150000., 16384. + 8. * keys); }
-
-// An index has room for more sequences than are there, so keys are split by the sequences of the call: max_q tokens each would be the fewest; drafts are
-// ragged, half of max_q and more in the mean, so twice that (16 trees of up to 26 tokens: 49 us, 58 with the fewest).  One token on 131000 keys in one of 64
-// places: 101 us, 1065 split by places; a tree of 26: 124 and 1383.  But every place (or token, whose idle workgroups take five times as long) has its row
-// of workgroups: beyond most_blocks they are split as if for twice as many sequences, and so on up to one for each row.
-// keys: that a sequence of the call has for a row of workgroups to go through, at most.
 Plan tree_plan(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, int64_t keys) {
-    const int64_t rows = int64_t(q.max_q) * (q.heads / p.kv_heads);
-    const bool token = by_token(ix, q);
-    const int64_t most = token ? q.total_q : ix.n_seqs;
-    const double weight = most * (token && q.max_q > 1 ? 5. : 1.), join = double(q.max_q) * q.heads;
-    int64_t sequences = std::min<int64_t>({ix.n_seqs, q.total_q, 2 * ceil_div(q.total_q, q.max_q)});
-    for (;; sequences = std::min(most, 2 * sequences)) {
-        const Plan pl = plan_of(p, rows, sequences * p.kv_heads, keys, 128, int64_t(kListed) * p.page, false);
-        const double blocks = double(pl.n_chunks) * pl.row_tiles * p.kv_heads + (pl.n_chunks > 16 ? join : pl.n_chunks > 1 ? join / 4 : 0.);
-        if (sequences >= most || blocks * weight <= most_blocks(keys)) return pl;
-    }
+    return plan_by_sequences(p, ix, q, keys, [&](int64_t rows, int64_t groups, int64_t units) { return plan_of(p, rows, groups, units, 128, int64_t(kListed) * p.page, false); });
 }
 
 Plan picked_plan(const tbn_kv_pool &p, const KvQueries &q, int32_t n_select) {
     return plan_of(p, q.heads / p.kv_heads, q.total_q * p.kv_heads, n_select, p.page <= 64 ? 128 / p.page : 1, kListed, true);
-}
-
-size_t workspace_of(const tbn_kv_pool &p, const KvQueries &q, const Plan &pl) {
-    return pl.n_chunks > 1 ? static_cast<size_t>(pl.n_chunks) * q.total_q * q.heads * (p.dim + 4) * 4 : 0;
 }
 
 template <typename T, int DP, int RT, Kind KIND, bool TOKENS>
@@ -574,14 +542,6 @@ void launch_type(const AttentionArgs &a, const Plan &pl, dim3 grid, hipStream_t 
     else launch_both<uint16_t, KIND, TOKENS>(a, pl, grid, stream);
 }
 
-float factor_of(float scale) {
-    const float c = fabsf(scale) * kLog2e;
-    return c < 1e-37f ? 1e-37f : c;
-}
-uint32_t flip_of(const tbn_kv_pool &p, float scale) { return !(scale < 0.f) ? 0u : p.dt == TBN_F32 ? 0x80000000u : 0x80008000u; }
-
-constexpr int64_t kMostBlocks = 0x7fffffff;   // workgroups of a sequence
-
 tbn_status too_many(const char *what, int64_t blocks) {
     set_error("%s: %lld workgroups per sequence are beyond one launch", what, (long long)blocks);
     return TBN_ERR_UNSUPPORTED;
@@ -589,25 +549,46 @@ tbn_status too_many(const char *what, int64_t blocks) {
 
 template <Kind KIND>
 tbn_status launch(AttentionArgs &a, const Plan &pl, float *ws, const char *what, hipStream_t stream) {
+    dim3 grid;
+    bool tokens;
+    const tbn_status st = spread(a, pl, ws, KIND, what, grid, tokens);
+    if (st != TBN_OK) return st;
+    if (KIND != kPicked && tokens) launch_type<KIND, KIND != kPicked>(a, pl, grid, stream);
+    else launch_type<KIND, false>(a, pl, grid, stream);
+    return check_launch(what);
+}
+
+}  // namespace
+
+tbn_status spread(AttentionArgs &a, const Plan &pl, float *ws, Kind kind, const char *what, dim3 &grid, bool &tokens) {
     a.chunk = pl.chunk;
     a.n_chunks = pl.n_chunks;
     a.row_tiles = pl.row_tiles;
     const int64_t parts = int64_t(pl.n_chunks) * a.q.total_q * a.q.heads;
     a.part_o = ws;
     a.part_ml = reinterpret_cast<float4 *>(ws ? ws + parts * a.p.dim : nullptr);
-    const int64_t x = int64_t(pl.n_chunks) * pl.row_tiles * a.p.kv_heads * (KIND == kPicked ? a.q.max_q : 1), jx = int64_t(a.q.max_q) * a.q.heads;
+    const int64_t x = int64_t(pl.n_chunks) * pl.row_tiles * a.p.kv_heads * (kind == kPicked ? a.q.max_q : 1), jx = int64_t(a.q.max_q) * a.q.heads;
     if (x > kMostBlocks || jx > kMostBlocks) return too_many(what, x > jx ? x : jx);
-    if constexpr (KIND != kPicked) {
-        if (by_token(a.ix, a.q)) {
-            launch_type<KIND, true>(a, pl, dim3(static_cast<unsigned>(x), static_cast<unsigned>(a.q.total_q)), stream);
-            return check_launch(what);
-        }
-    }
-    launch_type<KIND, false>(a, pl, dim3(static_cast<unsigned>(x), a.ix.n_seqs), stream);
-    return check_launch(what);
+    tokens = kind != kPicked && by_token(a.ix, a.q);
+    grid = dim3(static_cast<unsigned>(x), tokens ? static_cast<unsigned>(a.q.total_q) : a.ix.n_seqs);
+    return TBN_OK;
 }
 
-}  // namespace
+template <typename T>
+static void launch_join_typed(const AttentionArgs &a, Kind kind, int tile_rows, bool tokens, unsigned groups, hipStream_t stream) {
+    if (kind == kWindow) {
+        if (tokens) launch_join<T, kWindow, true>(a, tile_rows, groups, stream);
+        else launch_join<T, kWindow, false>(a, tile_rows, groups, stream);
+    } else {
+        if (tokens) launch_join<T, kAll, true>(a, tile_rows, groups, stream);
+        else launch_join<T, kAll, false>(a, tile_rows, groups, stream);
+    }
+}
+
+void launch_kv_join(const AttentionArgs &a, Kind kind, int tile_rows, bool tokens, unsigned groups, hipStream_t stream) {
+    if (a.p.dt == TBN_F32) launch_join_typed<float>(a, kind, tile_rows, tokens, groups, stream);
+    else launch_join_typed<uint16_t>(a, kind, tile_rows, tokens, groups, stream);
+}
 
 size_t tree_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q) { return workspace_of(p, q, tree_plan(p, ix, q, q.max_len)); }
 
@@ -615,12 +596,6 @@ tbn_status launch_tree_attention(const tbn_kv_pool &p, const tbn_kv_index &ix, c
                                  int32_t mask_words, float scale, float *ws, hipStream_t stream) {
     AttentionArgs a{p, ix, q, out, lse, mask, mask_words, nullptr, 0, factor_of(scale), flip_of(p, scale)};
     return launch<kAll>(a, tree_plan(p, ix, q, q.max_len), ws, "tbn_tree_attention", stream);
-}
-
-// Keys that a workgroup of a call with a window goes through, at most: the first pages, the window of its first row and what its other rows add.
-static int64_t window_keys(const tbn_kv_pool &p, const KvQueries &q, int32_t n_sink, int32_t window, bool masked) {
-    const int64_t tokens = masked ? q.max_q : std::min<int64_t>(q.max_q, 128 / (q.heads / p.kv_heads) + 2);
-    return std::min(q.max_len, ceil_div(n_sink, p.page) * p.page + window + tokens + 2 * p.page);
 }
 
 size_t window_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, int32_t n_sink, int32_t window, bool masked) {

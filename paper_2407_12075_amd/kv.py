@@ -9,9 +9,14 @@ marshalling only, PyTorch supplies device memory and the stream, there is no CPU
     out, lse = kv.tbn_tree_attention(q, pool, index, cu_q, max_q, mask=...)
     picks = kv.tbn_block_select(q, pool, index, cu_q, max_q, n_select)
     out, lse = kv.tbn_block_attention(q, pool, index, cu_q, max_q, picks)
+    out, lse = kv.tbn_window_attention(q, pool, index, cu_q, max_q, n_sink, window, mask=...)
     kv.tbn_kv_keep / tbn_kv_release / tbn_kv_fork / tbn_kv_compact / tbn_kv_copy_pages
 
-``KVPool`` and ``KVIndex`` hold the tensors and the C structs that describe them; build them once.
+    pool = kv.kv4_pool(n_pages, kv_heads, dim, page)                                  # in place of kv_pool: keys and values in 4 bits
+    kv.tbn_kv4_append / tbn_kv4_read / tbn_kv4_keep / tbn_kv4_copy_pages
+    out, lse = kv.tbn_kv4_attention(q, pool, index, cu_q, max_q, mask=..., n_sink=..., window=...)
+
+``KVPool``, ``KV4Pool`` and ``KVIndex`` hold the tensors and the C structs that describe them; build them once.
 """
 from __future__ import annotations
 
@@ -32,6 +37,11 @@ class _Pool(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("summary", ctypes.c_void_p), ("step", ctypes.c_void_p),
                 ("n_pages", ctypes.c_int64), ("kv_heads", ctypes.c_int32), ("dim", ctypes.c_int32), ("page", ctypes.c_int32),
                 ("dt", ctypes.c_int32)]
+
+
+class _Pool4(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int64), ("kv_heads", ctypes.c_int32), ("dim", ctypes.c_int32), ("page", ctypes.c_int32)]
 
 
 class _Index(ctypes.Structure):
@@ -61,6 +71,26 @@ class KVPool:
         self._at, self._gpu = ctypes.addressof(self._c), k.device.index
 
 
+class KV4Pool:
+    """Pages of one layer in 4 bits: k uint8 (n_pages, kv_heads, page, dim / 2), v uint8 (n_pages, kv_heads, page / 32, 4, 16, dim / 16, 4), k_exp
+    and v_exp int8 (n_pages, kv_heads, page, 4 or, for more than 128 channels, 8); what they hold: include/tbn.h."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_exp: torch.Tensor, v_exp: torch.Tensor):
+        if k.dim() != 4:
+            raise ValueError("k must be (n_pages, kv_heads, page, dim / 2)")
+        n, h, p, half = k.shape
+        d = 2 * half
+        if tuple(v.shape) != (n, h, p // 32, 4, 16, d // 16, 4):
+            raise ValueError("v must be (n_pages, kv_heads, page / 32, 4, 16, dim / 16, 4)")
+        if any(tuple(t.shape) != (n, h, p, 4 if d <= 128 else 8) for t in (k_exp, v_exp)):
+            raise ValueError("k_exp and v_exp must be (n_pages, kv_heads, page, 4 or, for more than 128 channels, 8)")
+        _same_device(k.device, v, k_exp, v_exp)
+        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self.n_pages, self.kv_heads, self.page, self.dim, self.dtype, self.device = n, h, p, d, None, k.device
+        self._c = _Pool4(_dev(k, "k", torch.uint8), _dev(v, "v", torch.uint8), _dev(k_exp, "k_exp", torch.int8), _dev(v_exp, "v_exp", torch.int8), n, h, d, p)
+        self._at, self._gpu = ctypes.addressof(self._c), k.device.index
+
+
 class KVIndex:
     """Bookkeeping that the layers of a model share, int32: table (n_seqs, max_pages), lens (n_seqs), refs (n_pages), status (1)."""
 
@@ -83,6 +113,15 @@ def kv_pool(n_pages: int, kv_heads: int, dim: int, page: int, dtype: torch.dtype
                   torch.empty(n_pages, kv_heads, dtype=torch.float32, device=device) if summary else None)
 
 
+def kv4_pool(n_pages: int, kv_heads: int, dim: int, page: int, device="cuda") -> KV4Pool:
+    """A pool of pages in 4 bits; their contents are undefined until keys are appended."""
+    if dim % 32 or page % 32:
+        raise ValueError("dim and page must be multiples of 32")
+    new = lambda dtype, *shape: torch.empty(n_pages, kv_heads, *shape, dtype=dtype, device=device)  # noqa: E731
+    exps = 4 if dim <= 128 else 8
+    return KV4Pool(new(torch.uint8, page, dim // 2), new(torch.uint8, page // 32, 4, 16, dim // 16, 4), new(torch.int8, page, exps), new(torch.int8, page, exps))
+
+
 def kv_index(n_seqs: int, max_pages: int, n_pages: int, page: int, device="cuda") -> KVIndex:
     """Bookkeeping of empty sequences and free pages."""
     z = lambda *shape: torch.zeros(shape, dtype=torch.int32, device=device)  # noqa: E731
@@ -102,10 +141,10 @@ def _ints(t: torch.Tensor, name: str, at_least: int, device: torch.device) -> in
     return _dev(t, name, torch.int32)
 
 
-def _rows(t: torch.Tensor, name: str, heads: int, dim: int, like: KVPool) -> Tuple[int, int]:
-    """Address and token stride of (tokens, heads, dim) whose last two axes are dense."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.dtype != like.dtype:
-        raise ValueError(f"{name} must be (tokens, {heads}, {dim}) with dtype {like.dtype}")
+def _rows(t: torch.Tensor, name: str, heads: int, dim: int, like) -> Tuple[int, int]:
+    """Address and token stride of (tokens, heads, dim) whose last two axes are dense; of the pool's type, where it has one."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.dtype not in ((like.dtype,) if like.dtype else (torch.float32, torch.bfloat16)):
+        raise ValueError(f"{name} must be (tokens, {heads}, {dim}) with dtype {like.dtype or 'float32 or bfloat16'}")
     if not t.is_cuda or t.device != like.device:
         raise ValueError(f"{name} must be a device tensor on {like.device}")
     st = t.stride()
@@ -115,7 +154,7 @@ def _rows(t: torch.Tensor, name: str, heads: int, dim: int, like: KVPool) -> Tup
     return t.data_ptr(), st[0] if n > 1 else heads * dim
 
 
-def _agree(pool: KVPool, index: KVIndex):
+def _agree(pool, index: KVIndex):
     if pool.device != index.device:
         raise ValueError(f"pool and index must live on one device, got {pool.device} and {index.device}")
 
@@ -214,7 +253,7 @@ def tbn_kv_keep(pool: KVPool, index: KVIndex, base: torch.Tensor, picks: torch.T
                 picks.shape[1], _ints(counts, "counts", index.n_seqs, index.device), _stream(stream)))
 
 
-def _queries(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: torch.Tensor):
+def _queries(q: torch.Tensor, pool, index: KVIndex, cu_q: torch.Tensor):
     _agree(pool, index)
     if q.dim() != 3 or q.shape[2] != pool.dim:
         raise ValueError(f"q must be (tokens, heads, {pool.dim})")
@@ -345,4 +384,79 @@ def tbn_block_attention(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: tor
     ws, size = _workspace(need, workspace, q.device, stream)
     _done(_call("tbn_block_attention", at, stride, _dev(out, "out"), _dev(lse, "lse", torch.float32), pool._at, index._at, cu, q.shape[0], max_q, q.shape[1],
                 _dev(picks, "picks", torch.int32), n, 1.0 / math.sqrt(pool.dim) if scale is None else scale, ws, size, _stream(stream)))
+    return out, lse
+
+
+def tbn_kv4_append(pool: KV4Pool, index: KVIndex, k_new: torch.Tensor, v_new: torch.Tensor, cu_new: torch.Tensor, max_new: int, stream=None) -> None:
+    """tbn_kv_append into a pool in 4 bits; k_new and v_new float32 or bfloat16."""
+    if _plain(stream) and tbn._host.kv4_append(pool._at, pool._gpu, index._at, index._gpu, k_new, v_new, cu_new, max_new):
+        return
+    _agree(pool, index)
+    k, ks = _rows(k_new, "k_new", pool.kv_heads, pool.dim, pool)
+    v, vs = _rows(v_new, "v_new", pool.kv_heads, pool.dim, pool)
+    if k_new.shape[0] != v_new.shape[0] or k_new.dtype != v_new.dtype:
+        raise ValueError("k_new and v_new must have the same number of tokens and dtype")
+    _done(_call("tbn_kv4_append", pool._at, index._at, k, ks, v, vs, _dt(k_new), _ints(cu_new, "cu_new", index.n_seqs + 1, index.device), k_new.shape[0], max_new,
+                _stream(stream)))
+
+
+def tbn_kv4_read(pool: KV4Pool, index: KVIndex, cu: torch.Tensor, max_n: int, total: int, dtype: torch.dtype = torch.bfloat16,
+                 stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The last cu[s + 1] - cu[s] <= max_n keys and values of each sequence, (total, kv_heads, dim) each, as the numbers they stand for (rows of
+    a sequence that has fewer keys are undefined)."""
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("dtype must be float32 or bfloat16")
+    if _plain(stream):
+        r = tbn._host.kv4_read(pool._at, pool._gpu, index._at, index._gpu, cu, max_n, total, dtype is torch.float32)
+        if r is not None:
+            return r
+    _agree(pool, index)
+    k, v = (_empty((total, pool.kv_heads, pool.dim), dtype, pool.device, stream) for _ in range(2))
+    _done(_call("tbn_kv4_read", pool._at, index._at, k.data_ptr(), v.data_ptr(), _dt(k), _ints(cu, "cu", index.n_seqs + 1, index.device), total, max_n, _stream(stream)))
+    return k, v
+
+
+def tbn_kv4_copy_pages(pool: KV4Pool, src: torch.Tensor, dst: torch.Tensor, count: Optional[torch.Tensor] = None, stream=None) -> None:
+    """tbn_kv_copy_pages of a pool in 4 bits."""
+    if _plain(stream) and tbn._host.kv4_copy_pages(pool._at, pool._gpu, src, dst, count):
+        return
+    n = src.numel()
+    if dst.numel() != n:
+        raise ValueError("src and dst must have the same length")
+    _done(_call("tbn_kv4_copy_pages", pool._at, _ints(src, "src", 0, pool.device), _ints(dst, "dst", 0, pool.device), n,
+                None if count is None else _ints(count, "count", 1, pool.device), _stream(stream)))
+
+
+def tbn_kv4_keep(pool: KV4Pool, index: KVIndex, base: torch.Tensor, picks: torch.Tensor, counts: torch.Tensor, stream=None) -> None:
+    """tbn_kv_keep of a pool in 4 bits."""
+    if _plain(stream) and tbn._host.kv4_keep(pool._at, pool._gpu, index._at, index._gpu, base, picks, counts):
+        return
+    _agree(pool, index)
+    if picks.dim() != 2 or picks.shape[0] != index.n_seqs:
+        raise ValueError("picks must be (n_seqs, width)")
+    _done(_call("tbn_kv4_keep", pool._at, index._at, _ints(base, "base", index.n_seqs, index.device), _ints(picks, "picks", 0, index.device),
+                picks.shape[1], _ints(counts, "counts", index.n_seqs, index.device), _stream(stream)))
+
+
+def tbn_kv4_attention_workspace_bytes(q: torch.Tensor, pool: KV4Pool, index: KVIndex, max_q: int, n_sink: int = 0, window: int = 0, masked: bool = False,
+                                      max_len: int = 0) -> int:
+    return int(lib().tbn_kv4_attention_workspace_bytes(pool._at, index._at, _dt(q), q.shape[0], max_q, q.shape[1], n_sink, window, int(masked), max_len))
+
+
+def tbn_kv4_attention(q: torch.Tensor, pool: KV4Pool, index: KVIndex, cu_q: torch.Tensor, max_q: int, mask: Optional[torch.Tensor] = None,
+                      n_sink: int = 0, window: int = 0, scale: Optional[float] = None, max_len: Optional[int] = None,
+                      out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                      stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """tbn_tree_attention over a pool in 4 bits, with window > 0 tbn_window_attention; q float32 or bfloat16.  Returns (out, lse)."""
+    if _plain(out, lse, workspace, stream):
+        r = tbn._host.kv4_attention(q, pool._at, pool._gpu, index._at, index._gpu, cu_q, max_q, max_len, mask, scale, n_sink, window)
+        if r is not None:
+            return r
+    at, stride, cu = _queries(q, pool, index, cu_q)
+    out, lse = _outputs(q, out, lse, stream)
+    mask_at, words = _mask(mask, q)
+    need = int(lib().tbn_kv4_attention_workspace_bytes(pool._at, index._at, _dt(q), q.shape[0], max_q, q.shape[1], n_sink, window, int(mask is not None), max_len or 0))
+    ws, size = _workspace(need, workspace, q.device, stream)
+    _done(_call("tbn_kv4_attention", at, stride, _dt(q), _dev(out, "out"), _dev(lse, "lse", torch.float32), pool._at, index._at, cu, q.shape[0], max_q, q.shape[1],
+                n_sink, window, mask_at, words, max_len or 0, 1.0 / math.sqrt(pool.dim) if scale is None else scale, ws, size, _stream(stream)))
     return out, lse
