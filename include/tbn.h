@@ -589,6 +589,35 @@ tbn_status tbn_block_attention(const void *q, int64_t q_stride, void *out, float
                                void *stream);
 
 /*
+ * Verification of drafted tokens by sampling: which of them stand, and the token that follows, so that what is emitted has the target's
+ * distribution whatever the draft was.  Sequence s has T = cu_q[s + 1] - cu_q[s] tokens, rows cu_q[s] onwards of every array; the first one (place 0) was emitted
+ * before, the others are drafted and hang each on an earlier one, parents[i] (place within the sequence; NULL: on the one before).  Row i of target holds the
+ * probabilities of what follows token i, row i of draft those that the tokens which hang on i were drawn from, independently.  u holds uniform numbers of [0, 1).
+ *
+ * From place x = 0 on:  r = target[x], m = 1.  The tokens c that hang on x are asked in ascending order, with t = tokens[c], q = draft[x]:
+ *   u[c] * (m * q[t]) < r[t] : c is accepted, x = c, and so on from there;
+ *   otherwise                : r[v] = max(r[v] - m * q[v], 0) for all v, m = sum of r, and the next one is asked.
+ * Without a draft (tokens that were picked, not drawn) q[v] is 1 for v = t and 0 for all others; m is then m less r[t].
+ * When none is left:  next[s] = the least v with r[0] + .. + r[v] > u[of place 0] * (sum of r).
+ *
+ * Numbers are binary64 from the first product on.  Negative numbers and not-a-numbers of target and draft count as 0.  If nothing is left of r, the token is
+ * drawn from target[x]; -1 if that has no positive finite sum.  A draw at or beyond the sum takes the last v with r[v] > 0.  A token outside of the vocabulary,
+ * or that hangs on none before it, is not accepted (the former counts as asked, with q[t] = r[t] = 0).
+ *
+ *   target, draft : DEVICE, total_q rows of vocab floats, target_stride / draft_stride elements apart (at least vocab); draft NULL: see above
+ *   tokens, u     : DEVICE, total_q;  parents : DEVICE, total_q, or NULL;  those of place 0 are not looked at, but for u
+ *   cu_q          : DEVICE, n_seqs + 1, ascending from 0 to total_q;  max_q : at least the largest T, at most 2048
+ *   picks         : DEVICE, n_seqs x max_q: the accepted places, 0 first, ascending, -1 behind the last (what tbn_kv_keep takes)
+ *   counts, next  : DEVICE, n_seqs: accepted places (1 at least; 0 for a sequence without tokens), the token that follows (there -1)
+ *   workspace     : DEVICE, 16-byte aligned, the bytes of the query (may be 0)
+ * Errors: TBN_ERR_NULL, TBN_ERR_SHAPE, TBN_ERR_UNSUPPORTED, TBN_ERR_WORKSPACE, TBN_ERR_DEVICE.
+ */
+size_t tbn_verify_workspace_bytes(int64_t total_q, int32_t max_q, int32_t n_seqs, int64_t vocab);
+tbn_status tbn_verify(const float *target, int64_t target_stride, const float *draft, int64_t draft_stride, const int32_t *tokens,
+                      const int32_t *parents, const float *u, const int32_t *cu_q, int64_t total_q, int32_t max_q, int32_t n_seqs,
+                      int64_t vocab, int32_t *picks, int32_t *counts, int32_t *next, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Measurement aids.  No part of the method (the paper reports no kernel timings; its Section "GPU Inference Kernel"
  * measures memory only): they give the benchmark its denominators, measured the same way as the layer kernels.
  *

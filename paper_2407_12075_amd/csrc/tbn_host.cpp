@@ -47,6 +47,8 @@ decltype(&tbn_kv4_copy_pages) p_kv4_copy_pages;
 decltype(&tbn_kv4_keep) p_kv4_keep;
 decltype(&tbn_kv4_attention_workspace_bytes) p_kv4_attention_workspace_bytes;
 decltype(&tbn_kv4_attention) p_kv4_attention;
+decltype(&tbn_verify_workspace_bytes) p_verify_workspace_bytes;
+decltype(&tbn_verify) p_verify;
 decltype(&tbn_block_select_workspace_bytes) p_block_select_workspace_bytes;
 decltype(&tbn_block_select) p_block_select;
 decltype(&tbn_block_attention_workspace_bytes) p_block_attention_workspace_bytes;
@@ -637,6 +639,53 @@ PyObject *block_attention(PyObject *, PyObject *const *args, Py_ssize_t n_args) 
     END_HANDLE_TH_ERRORS
 }
 
+// float32 (tokens, vocab) with dense rows
+const at::Tensor *probabilities(PyObject *o, int64_t &stride) {
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    constexpr c10::DispatchKeySet kWrapped({c10::DispatchKey::FuncTorchBatched, c10::DispatchKey::FuncTorchGradWrapper,
+                                            c10::DispatchKey::Functionalize, c10::DispatchKey::Python});
+    if (!t.defined() || !t.is_cuda() || t.layout() != at::kStrided || t.dim() != 2 || t.scalar_type() != at::kFloat || t.key_set().has_any(kWrapped)) return nullptr;
+    const int64_t n = t.size(0), v = t.size(1);
+    if (n < 1 || v < 1 || t.stride(1) != 1 || (n > 1 && t.stride(0) < v)) return nullptr;
+    stride = n > 1 ? t.stride(0) : v;
+    return &t;
+}
+
+// (target, tokens, u, cu_q, max_q, draft or None, parents or None)
+PyObject *verify(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    int64_t ps, qs = 0, most;
+    if (n_args != 7 || !ordinary_context()) Py_RETURN_NONE;
+    const at::Tensor *p = probabilities(args[0], ps), *q = nullptr;
+    if (!p || !integer(args[4], 0, 1 << 30, most)) Py_RETURN_NONE;
+    const int64_t n = p->size(0), vocab = p->size(1), gpu = p->device().index();
+    const int32_t *tokens = ints(args[1], n, gpu), *cu = ints(args[3], 2, gpu), *parents = nullptr;
+    const at::Tensor *u = plain(args[2], at::kFloat, *p);
+    if (!tokens || !cu || !u || u->numel() < n) Py_RETURN_NONE;
+    if (args[5] != Py_None && (!(q = probabilities(args[5], qs)) || q->sizes() != p->sizes() || q->device() != p->device())) Py_RETURN_NONE;
+    if (args[6] != Py_None && !(parents = ints(args[6], n, gpu))) Py_RETURN_NONE;
+    const int64_t n_seqs = THPVariable_Unpack(args[3]).numel() - 1;
+    if (n_seqs > INT32_MAX) Py_RETURN_NONE;
+    const auto options = THPVariable_Unpack(args[3]).options();
+    at::Tensor picks = at::empty({n_seqs, most}, options), counts = at::empty({n_seqs}, options), next = at::empty({n_seqs}, options), ws;
+    const int32_t max_q = static_cast<int32_t>(most), seqs = static_cast<int32_t>(n_seqs);
+    const size_t need = p_verify_workspace_bytes(n, max_q, seqs, vocab);
+    if (need) ws = bytes_like(*p, need);
+    const tbn_status st = unlocked([&] {
+        return p_verify(floats(*p), ps, q ? floats(*q) : nullptr, qs, tokens, parents, floats(*u), cu, n, max_q, seqs, vocab, static_cast<int32_t *>(picks.data_ptr()),
+                        static_cast<int32_t *>(counts.data_ptr()), static_cast<int32_t *>(next.data_ptr()), need ? ws.data_ptr() : nullptr, need, stream());
+    });
+    if (st != TBN_OK) return result(st, one, picks, picks);
+    PyObject *a = THPVariable_Wrap(picks), *b = THPVariable_Wrap(counts), *c = THPVariable_Wrap(next);
+    PyObject *r = a && b && c ? PyTuple_Pack(3, a, b, c) : nullptr;
+    Py_XDECREF(a);
+    Py_XDECREF(b);
+    Py_XDECREF(c);
+    return r;
+    END_HANDLE_TH_ERRORS
+}
+
 // (raise, {name: address})
 PyObject *init(PyObject *, PyObject *args) {
     PyObject *raise, *table;
@@ -673,6 +722,8 @@ PyObject *init(PyObject *, PyObject *args) {
     take(p_kv4_keep, "tbn_kv4_keep");
     take(p_kv4_attention_workspace_bytes, "tbn_kv4_attention_workspace_bytes");
     take(p_kv4_attention, "tbn_kv4_attention");
+    take(p_verify_workspace_bytes, "tbn_verify_workspace_bytes");
+    take(p_verify, "tbn_verify");
     take(p_block_select_workspace_bytes, "tbn_block_select_workspace_bytes");
     take(p_block_select, "tbn_block_select");
     take(p_block_attention_workspace_bytes, "tbn_block_attention_workspace_bytes");
@@ -692,7 +743,8 @@ PyMethodDef methods[] = {TBN_FAST(linear_forward), TBN_FAST(conv2d_forward), TBN
                          TBN_FAST(linear_forward_binact), TBN_FAST(pack_tile),
                          TBN_FAST(kv_reserve), TBN_FAST(kv_fork), TBN_FAST(kv_release), TBN_FAST(kv_copy_pages), TBN_FAST(kv_append), TBN_FAST(kv_keep),
                          TBN_FAST(tree_attention), TBN_FAST(window_attention), TBN_FAST(kv4_append), TBN_FAST(kv4_read),
-                         TBN_FAST(kv4_copy_pages), TBN_FAST(kv4_keep), TBN_FAST(kv4_attention), TBN_FAST(block_select), TBN_FAST(block_attention), {"init", init, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         TBN_FAST(kv4_copy_pages), TBN_FAST(kv4_keep), TBN_FAST(kv4_attention), TBN_FAST(verify),
+                         TBN_FAST(block_select), TBN_FAST(block_attention), {"init", init, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tbn_host", "plain calls of the binding on C++ tensors", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -54,6 +54,21 @@ size_t kv4_attention_workspace(const tbn_kv4_pool &p, const tbn_kv_index &ix, co
 tbn_status launch_kv4_attention(const tbn_kv4_pool &p, const tbn_kv_index &ix, const KvQueries &q, tbn_dtype dt, void *out, float *lse, int32_t n_sink,
                                 int32_t window, const uint32_t *mask, int32_t mask_words, float scale, float *ws, hipStream_t stream);
 
+struct VerifyCall {
+    const float *target, *draft;
+    int64_t target_stride, draft_stride;
+    const int32_t *tokens, *parents;
+    const float *u;
+    const int32_t *cu_q;
+    int64_t total;
+    int32_t max_q, n_seqs;
+    int64_t vocab;
+    int32_t *picks, *counts, *next;
+};
+int verify_most_tokens();   // of a sequence
+size_t verify_workspace(int64_t total, int32_t max_q, int32_t n_seqs, int64_t vocab);
+tbn_status launch_verify(const VerifyCall &c, void *ws, hipStream_t stream);
+
 #if defined(__HIPCC__)
 
 // what the GPU's data say is bounded before it becomes an address

@@ -394,4 +394,34 @@ tbn_status tbn_block_attention(const void *q, int64_t q_stride, void *out, float
     return launch_block_attention(*pool, *index, a, out, lse, picks, n_select, scale, static_cast<float *>(workspace), static_cast<hipStream_t>(stream));
 }
 
+static tbn_status check_verify(const char *fn, int64_t total, int32_t max_q, int32_t n_seqs, int64_t vocab) {
+    if (total < 0 || max_q < 0 || n_seqs < 1 || vocab < 1) return fail(TBN_ERR_SHAPE, fn, "total_q and max_q must be >= 0, n_seqs and vocab positive");
+    if (n_seqs > kMaxSeqs || total > (1 << 30) || vocab > (1 << 28)) return fail(TBN_ERR_UNSUPPORTED, fn, "at most 8192 sequences, 2^30 tokens and a vocabulary of 2^28");
+    return TBN_OK;
+}
+
+size_t tbn_verify_workspace_bytes(int64_t total_q, int32_t max_q, int32_t n_seqs, int64_t vocab) {
+    if (check_verify(nullptr, total_q, max_q, n_seqs, vocab) != TBN_OK || max_q > verify_most_tokens()) return 0;
+    return verify_workspace(total_q, max_q, n_seqs, vocab);
+}
+
+tbn_status tbn_verify(const float *target, int64_t target_stride, const float *draft, int64_t draft_stride, const int32_t *tokens, const int32_t *parents,
+                      const float *u, const int32_t *cu_q, int64_t total_q, int32_t max_q, int32_t n_seqs, int64_t vocab, int32_t *picks, int32_t *counts,
+                      int32_t *next, void *workspace, size_t workspace_bytes, void *stream) {
+    const char *fn = "tbn_verify";
+    tbn_status st = check_verify(fn, total_q, max_q, n_seqs, vocab);
+    if (st != TBN_OK) return st;
+    if (max_q > verify_most_tokens()) return fail(TBN_ERR_UNSUPPORTED, fn, "at most 2048 tokens of a sequence");
+    if (!cu_q || !counts || !next || (max_q && !picks)) return fail(TBN_ERR_NULL, fn, "cu_q, picks, counts and next must not be NULL");
+    if (total_q && max_q && (!target || !tokens || !u)) return fail(TBN_ERR_NULL, fn, "target, tokens and u must not be NULL");
+    const int64_t lim = int64_t(1) << 40;
+    if (target_stride < vocab || target_stride > lim || (draft && (draft_stride < vocab || draft_stride > lim)))
+        return fail(TBN_ERR_SHAPE, fn, "target_stride and draft_stride must be at least vocab (and at most 2^40)");
+    st = check_workspace(fn, verify_workspace(total_q, max_q, n_seqs, vocab), workspace, workspace_bytes, 16);
+    if (st != TBN_OK) return st;
+    drop_stale_error();
+    return launch_verify(VerifyCall{target, draft, target_stride, draft_stride, tokens, parents, u, cu_q, total_q, max_q, n_seqs, vocab, picks, counts, next}, workspace,
+                         static_cast<hipStream_t>(stream));
+}
+
 }  // extern "C"

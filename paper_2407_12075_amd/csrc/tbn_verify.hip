@@ -1,0 +1,490 @@
+// Verification of drafted tokens: which of them the target accepts, and the token that follows.
+//
+// At an accepted token x (the first of a sequence to begin with) r = target[x], m = 1.  The tokens that hang on x are asked in order: c is accepted where
+// u_c m q(c) < r(c), q = draft[x] (without a draft q is 1 at c and 0 elsewhere); if it is not, r = max(r - m q, 0), m = sum of r, and the next one is
+// asked.  When none is left the token that follows is the first whose prefix sum of r is above u sum(r).
+//
+// Everything is in binary64: a product of a few 24-bit numbers is exact or off by 2^-53, so that a border is hit only by numbers that lie on it, and
+// sums of a row are off by about 1e-16 of it, whatever their order.  (It is fixed all the same.)  No product is fused with a sum: r has one value.
+//
+// The path needs two numbers of each drafted token, loaded side by side; it is walked by every wave alike, in LDS.  A sum over a row is needed where a
+// token was refused and another one hangs on the same (with a draft), and at the end.  What bounds it is the latency of a handful of dependent
+// loads and, for many sequences with large vocabularies, the bytes of the last rows: there slices of a row are summed by many workgroups, each of which
+// walks the path for itself, and a second launch finds the slice and the token in it.
+#include <algorithm>
+
+#include "tbn_kv.h"
+
+namespace tbn {
+
+namespace {
+
+constexpr int kBig = 1024, kSmall = 256;   // threads of a workgroup
+constexpr int kSlice = 4096;               // elements of a row that a workgroup sums
+
+struct VerifyArgs {
+    const float *target, *draft;
+    int64_t target_stride, draft_stride;
+    const int32_t *tokens, *parents;
+    const float *u;
+    const int32_t *cu;
+    int32_t *picks, *counts, *next;
+    int64_t total;
+    int32_t max_q, n_seqs, vocab;
+    // split rows: sums of slices, where each sequence's path ends and what was refused there
+    double *parts;
+    int2 *ends;       // row of the target (-1: no tokens), refused ones
+    double *refused;  // (sequence, max_q): m with a draft, else the token
+    int32_t slices;
+};
+
+// What is left of a row of the target.
+struct Rest {
+    const float *p, *q;
+    const double *refused;
+    int n;
+};
+
+// r at element v.  Negative numbers and not-a-numbers count as 0.
+template <bool DRAFT>
+__device__ __forceinline__ double left_of(const Rest &x, int v, float p, float q) {
+#pragma clang fp contract(off)
+    double r = p > 0.f ? static_cast<double>(p) : 0.;
+    const double qd = q > 0.f ? static_cast<double>(q) : 0.;
+    for (int i = 0; i < x.n; ++i) {
+        if constexpr (DRAFT) {
+            const double part = x.refused[i] * qd, d = r - part;
+            r = d > 0. ? d : 0.;
+        } else {
+            r = x.refused[i] == static_cast<double>(v) ? 0. : r;
+        }
+    }
+    return r;
+}
+
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+
+// four elements from v on, those below hi
+template <bool DRAFT>
+__device__ __forceinline__ void four_of(const Rest &x, int v, int hi, double (&r)[4]) {
+    float p[4] = {0.f, 0.f, 0.f, 0.f}, q[4] = {0.f, 0.f, 0.f, 0.f};
+    if (v + 4 <= hi) {
+        const f32x4_any a = *reinterpret_cast<const f32x4_any *>(x.p + v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[e] = a[e];
+        if (DRAFT && x.n) {
+            const f32x4_any b = *reinterpret_cast<const f32x4_any *>(x.q + v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) q[e] = b[e];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (v + e < hi) {
+                p[e] = x.p[v + e];
+                if (DRAFT && x.n) q[e] = x.q[v + e];
+            }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = left_of<DRAFT>(x, v + e, p[e], q[e]);
+}
+
+__device__ __forceinline__ double sum_of_wave(double s) {
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) s += __shfl_xor(s, d);
+    return s;
+}
+
+// Sum of a wave's elements [lo, hi).
+template <bool DRAFT>
+__device__ __forceinline__ double sum_of(const Rest &x, int lo, int hi) {
+    double s = 0.;
+#pragma unroll 4
+    for (int v = lo + 4 * (threadIdx.x & 63); v < hi; v += 4 * kWave) {
+        double r[4];
+        four_of<DRAFT>(x, v, hi, r);
+        s += (r[0] + r[1]) + (r[2] + r[3]);
+    }
+    return sum_of_wave(s);
+}
+
+struct DrawLds {
+    double sums[kBig / kWave];
+    int token;
+};
+
+// Every wave of the workgroup takes an equal run of [lo, hi); their sums in order.  Every thread calls it.
+template <bool DRAFT, int THREADS>
+__device__ __forceinline__ double sums_of_waves(const Rest &x, int lo, int hi, DrawLds &l, int &run) {
+    constexpr int kWaves = THREADS / kWave;
+    const int wave = threadIdx.x >> 6;
+    run = ((hi - lo + kWaves - 1) / kWaves + 3) & ~3;
+    const int from = min(lo + wave * run, hi), to = min(from + run, hi);
+    __syncthreads();   // the sums may still be read from the call before
+    const double s = sum_of<DRAFT>(x, from, to);
+    if ((threadIdx.x & 63) == 0) l.sums[wave] = s;
+    __syncthreads();
+    double all = 0.;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) all += l.sums[w];
+    return all;
+}
+
+// Narrows [lo, hi) to the run in which the prefix sum passes `at`, which becomes what is left of it there: the first run whose end is above, else
+// the last one that holds anything.
+template <int N>
+__device__ __forceinline__ void narrow(const double *sums, int run, int &lo, int &hi, double &at) {
+    double before = 0., start = 0.;
+    int pick = -1, last = -1;
+    double last_start = 0.;
+    for (int w = 0; w < N; ++w) {
+        const double s = sums[w];
+        if (pick < 0 && s > 0.) {
+            last = w;
+            last_start = before;
+            if (before + s > at) {
+                pick = w;
+                start = before;
+            }
+        }
+        before += s;
+    }
+    if (pick < 0) {
+        pick = max(last, 0);
+        start = last_start;
+    }
+    at -= start;
+    lo = min(lo + pick * run, hi);
+    hi = min(lo + run, hi);
+}
+
+// The first element of [lo, hi) whose prefix sum is above `at`, else the last one that is not 0 (-1: none).  One wave.
+template <bool DRAFT>
+__device__ int find_in(const Rest &x, int lo, int hi, double at) {
+    const int lane = threadIdx.x & 63;
+    int last = -1;
+    for (int base = lo; base < hi; base += 4 * kWave) {
+        double r[4];
+        four_of<DRAFT>(x, min(base + 4 * lane, hi), hi, r);
+        const double own = (r[0] + r[1]) + (r[2] + r[3]);
+        double sum = own;   // inclusive prefix over the lanes
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) {
+            const double below = __shfl_up(sum, d);
+            if (lane >= d) sum += below;
+        }
+        double s = sum - own;
+        int mine = -1, mine_last = -1;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            s += r[e];
+            if (r[e] > 0.) {
+                mine_last = base + 4 * lane + e;
+                if (mine < 0 && s > at) mine = mine_last;
+            }
+        }
+        const uint64_t hit = __ballot(mine >= 0), any = __ballot(mine_last >= 0);
+        if (hit) return __shfl(mine, __ffsll(static_cast<unsigned long long>(hit)) - 1);
+        if (any) last = __shfl(mine_last, 63 - __clzll(static_cast<long long>(any)));
+        at -= __shfl(sum, 63);
+    }
+    return last;
+}
+
+// The token of a row, given the sum over [lo, hi) and where in it the draw lies.  Every thread calls it; the result is every thread's.
+template <bool DRAFT, int THREADS>
+__device__ int find_token(const Rest &x, int lo, int hi, double at, DrawLds &l) {
+    while (hi - lo > 8 * kWave) {
+        int run;
+        (void)sums_of_waves<DRAFT, THREADS>(x, lo, hi, l, run);
+        narrow<THREADS / kWave>(l.sums, run, lo, hi, at);
+    }
+    if (threadIdx.x < kWave) {
+        const int token = find_in<DRAFT>(x, lo, hi, at);
+        if (threadIdx.x == 0) l.token = token;
+    }
+    __syncthreads();
+    return l.token;
+}
+
+// What the walk leaves behind.
+struct End {
+    int at, n;   // place of the last accepted token, tokens refused there
+    int count;   // accepted ones
+};
+// What was refused at the token of place `at` lies from place at + 1 on: those tokens' own places are above it and below the next accepted one's, so
+// the list of one token never overwrites another's, which a slower wave may still read.
+
+struct Nodes {   // of a sequence, in LDS
+    double *refused;
+    float *p, *q, *u;
+    int32_t *parent, *token;
+};
+
+__device__ __forceinline__ Nodes nodes_at(void *lds, int most) {
+    Nodes n;
+    n.refused = static_cast<double *>(lds);
+    n.p = reinterpret_cast<float *>(n.refused + most);
+    n.q = n.p + most;
+    n.u = n.q + most;
+    n.parent = reinterpret_cast<int32_t *>(n.u + most);
+    n.token = n.parent + most;
+    return n;
+}
+constexpr int kNodeBytes = 28;
+constexpr int kMaxNodes = 2048;
+
+// Every wave walks alike.  PASSES: a row is summed where a token was refused and another one hangs on the same.
+template <bool DRAFT, bool PASSES, int THREADS>
+__device__ End walk(const VerifyArgs &a, int t0, int T, const Nodes &nodes, DrawLds &l, int32_t *picks) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    for (int j = tid; j < T; j += THREADS) {
+        const int parent = j == 0 ? -1 : a.parents ? a.parents[t0 + j] : j - 1, token = a.tokens[t0 + j];
+        const bool in = token >= 0 && token < a.vocab && parent >= 0 && parent < j;
+        const float p = in ? a.target[(t0 + parent) * a.target_stride + token] : 0.f;
+        nodes.q[j] = !DRAFT ? 1.f : in ? a.draft[(t0 + parent) * a.draft_stride + token] : 0.f;
+        nodes.p[j] = p;
+        nodes.u[j] = a.u[t0 + j];
+        nodes.parent[j] = parent;
+        nodes.token[j] = token;
+    }
+    __syncthreads();
+    End end{0, 0, 1};
+    if (picks && tid == 0) picks[0] = 0;
+    double m = 1.;
+    bool known = true;   // m is the sum of what is left
+    for (int after = 0;;) {
+        int c = -1;   // the next one that hangs on it
+        for (int j0 = (after + 1) & ~63; j0 < T; j0 += kWave) {
+            const int j = j0 + lane;
+            const uint64_t here = __ballot(j < T && j > after && nodes.parent[min(j, T - 1)] == end.at);
+            if (here) {
+                c = j0 + __ffsll(static_cast<unsigned long long>(here)) - 1;
+                break;
+            }
+        }
+        if (c < 0) break;
+        after = c;
+        if (PASSES && !known) {
+            Rest x{a.target + (t0 + end.at) * a.target_stride, a.draft + (t0 + end.at) * a.draft_stride, nodes.refused + end.at + 1, end.n};
+            int run;
+            m = sums_of_waves<DRAFT, THREADS>(x, 0, a.vocab, l, run);
+            known = true;
+        }
+        const Rest one{nullptr, nullptr, nodes.refused + end.at + 1, end.n};
+        const double r = left_of<DRAFT>(one, nodes.token[c], nodes.p[c], nodes.q[c]);
+        const double q = nodes.q[c] > 0.f ? static_cast<double>(nodes.q[c]) : 0.;
+        const double limit = DRAFT ? m * q : m;
+        if (static_cast<double>(nodes.u[c]) * limit < r) {
+            if (picks && tid == 0) picks[end.count] = c;
+            end = End{c, 0, end.count + 1};
+            m = 1.;
+            known = true;
+        } else {
+            nodes.refused[end.at + 1 + end.n++] = DRAFT ? m : static_cast<double>(nodes.token[c]);   // every wave writes the same
+            if (DRAFT) known = false;
+            else m = m - r > 0. ? m - r : 0.;
+        }
+    }
+    if (picks)
+        for (int j = end.count + tid; j < a.max_q; j += THREADS) picks[j] = -1;
+    return end;
+}
+
+__device__ __forceinline__ bool sequence_at(const VerifyArgs &a, int s, int &t0, int &T) {
+    t0 = max(a.cu[s], 0);
+    T = min(min(a.cu[s + 1], static_cast<int>(a.total)) - t0, a.max_q);
+    return T > 0;
+}
+
+__device__ __forceinline__ void nothing(const VerifyArgs &a, int s) {
+    for (int j = threadIdx.x; j < a.max_q; j += blockDim.x) a.picks[int64_t(s) * a.max_q + j] = -1;
+    if (threadIdx.x == 0) {
+        a.counts[s] = 0;
+        a.next[s] = -1;
+    }
+}
+
+__device__ __forceinline__ bool drawable(double sum) { return sum > 0. && sum < INFINITY; }
+
+// A workgroup for each sequence does everything.
+template <bool DRAFT>
+__global__ __launch_bounds__(kBig) void verify_kernel(VerifyArgs a) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ DrawLds l;
+    const int s = blockIdx.x;
+    int t0, T;
+    if (!sequence_at(a, s, t0, T)) return nothing(a, s);
+    const Nodes nodes = nodes_at(lds, a.max_q);
+    const End end = walk<DRAFT, DRAFT, kBig>(a, t0, T, nodes, l, a.picks + int64_t(s) * a.max_q);
+    Rest x{a.target + (t0 + end.at) * a.target_stride, DRAFT ? a.draft + (t0 + end.at) * a.draft_stride : nullptr, nodes.refused + end.at + 1, end.n};
+    int run, lo = 0, hi = a.vocab;
+    double sum = sums_of_waves<DRAFT, kBig>(x, lo, hi, l, run);
+    if (!drawable(sum) && x.n) {   // nothing is left: the target's row itself
+        x.n = 0;
+        sum = sums_of_waves<DRAFT, kBig>(x, lo, hi, l, run);
+    }
+    int token = -1;
+    if (drawable(sum)) {
+        double at = static_cast<double>(nodes.u[0]) * sum;
+        narrow<kBig / kWave>(l.sums, run, lo, hi, at);
+        token = find_token<DRAFT, kBig>(x, lo, hi, at, l);
+    }
+    if (threadIdx.x == 0) {
+        a.counts[s] = end.count;
+        a.next[s] = token;
+    }
+}
+
+// Rows in slices.  First launch: each workgroup walks the path (WALK; else verify_walk_kernel has) and sums its slice of the last row.
+template <bool DRAFT, bool WALK>
+__global__ __launch_bounds__(kSmall) void verify_slices_kernel(VerifyArgs a) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ DrawLds l;
+    const int s = blockIdx.y, slice = blockIdx.x, tid = threadIdx.x;
+    Rest x;
+    if constexpr (WALK) {
+        int t0, T;
+        if (!sequence_at(a, s, t0, T)) {
+            if (slice == 0) {
+                nothing(a, s);
+                if (tid == 0) a.ends[s] = make_int2(-1, 0);
+            }
+            return;
+        }
+        const Nodes nodes = nodes_at(lds, a.max_q);
+        const End end = walk<DRAFT, false, kSmall>(a, t0, T, nodes, l, slice == 0 ? a.picks + int64_t(s) * a.max_q : nullptr);
+        if (slice == 0) {
+            for (int i = tid; i < end.n; i += kSmall) a.refused[int64_t(s) * a.max_q + i] = nodes.refused[end.at + 1 + i];
+            if (tid == 0) {
+                a.counts[s] = end.count;
+                a.ends[s] = make_int2(t0 + end.at, end.n);
+            }
+        }
+        x = Rest{a.target + (t0 + end.at) * a.target_stride, DRAFT ? a.draft + (t0 + end.at) * a.draft_stride : nullptr, nodes.refused + end.at + 1, end.n};
+    } else {
+        const int2 end = a.ends[s];
+        if (end.x < 0) return;
+        x = Rest{a.target + end.x * a.target_stride, DRAFT ? a.draft + end.x * a.draft_stride : nullptr, a.refused + int64_t(s) * a.max_q, end.y};
+    }
+    const int lo = slice * kSlice, hi = min(lo + kSlice, a.vocab);
+    int run;
+    const double sum = sums_of_waves<DRAFT, kSmall>(x, lo, hi, l, run);
+    if (tid == 0) a.parts[int64_t(s) * a.slices + slice] = sum;
+}
+
+template <bool DRAFT>
+__global__ __launch_bounds__(kBig) void verify_walk_kernel(VerifyArgs a) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ DrawLds l;
+    const int s = blockIdx.x;
+    int t0, T;
+    if (!sequence_at(a, s, t0, T)) {
+        nothing(a, s);
+        if (threadIdx.x == 0) a.ends[s] = make_int2(-1, 0);
+        return;
+    }
+    const Nodes nodes = nodes_at(lds, a.max_q);
+    const End end = walk<DRAFT, DRAFT, kBig>(a, t0, T, nodes, l, a.picks + int64_t(s) * a.max_q);
+    for (int i = threadIdx.x; i < end.n; i += kBig) a.refused[int64_t(s) * a.max_q + i] = nodes.refused[end.at + 1 + i];
+    if (threadIdx.x == 0) {
+        a.counts[s] = end.count;
+        a.ends[s] = make_int2(t0 + end.at, end.n);
+    }
+}
+
+// Last launch: the slice and the token in it.
+template <bool DRAFT>
+__global__ __launch_bounds__(kSmall) void verify_draw_kernel(VerifyArgs a) {
+    __shared__ DrawLds l;
+    const int s = blockIdx.x, lane = threadIdx.x & 63;
+    const int2 end = a.ends[s];
+    if (end.x < 0) return;
+    Rest x{a.target + end.x * a.target_stride, DRAFT ? a.draft + end.x * a.draft_stride : nullptr, a.refused + int64_t(s) * a.max_q, end.y};
+    const double *parts = a.parts + int64_t(s) * a.slices;
+    double sum = 0.;
+    for (int i = lane; i < a.slices; i += kWave) sum += parts[i];
+    sum = sum_of_wave(sum);
+    const double u = static_cast<double>(a.u[max(a.cu[s], 0)]);
+    int token = -1;
+    if (drawable(sum)) {
+        double at = u * sum;
+        // the first slice whose end is above, else the last one that holds anything; every wave alike
+        int pick = -1, last = 0;
+        double before = 0., last_start = 0.;
+        for (int base = 0; base < a.slices && pick < 0; base += kWave) {
+            const double own = base + lane < a.slices ? parts[base + lane] : 0.;
+            double incl = own;
+#pragma unroll
+            for (int d = 1; d < kWave; d <<= 1) {
+                const double below = __shfl_up(incl, d);
+                if (lane >= d) incl += below;
+            }
+            const uint64_t hit = __ballot(own > 0. && before + incl > at), any = __ballot(own > 0.);
+            if (any) {
+                const int from = hit ? __ffsll(static_cast<unsigned long long>(hit)) - 1 : 63 - __clzll(static_cast<long long>(any));
+                last = base + from;
+                last_start = before + __shfl(incl - own, from);
+                if (hit) pick = last;
+            }
+            before += __shfl(incl, 63);
+        }
+        at -= last_start;
+        const int lo = last * kSlice, hi = min(lo + kSlice, a.vocab);
+        token = find_token<DRAFT, kSmall>(x, lo, hi, at, l);
+    } else if (x.n) {   // nothing is left: the target's row itself
+        x.n = 0;
+        int run, lo = 0, hi = a.vocab;
+        sum = sums_of_waves<DRAFT, kSmall>(x, lo, hi, l, run);
+        if (drawable(sum)) {
+            double at = u * sum;
+            narrow<kSmall / kWave>(l.sums, run, lo, hi, at);
+            token = find_token<DRAFT, kSmall>(x, lo, hi, at, l);
+        }
+    }
+    if (threadIdx.x == 0) a.next[s] = token;
+}
+
+// Rows go in slices where they are long and the sequences are too few to give every CU one.
+int slices_of(int64_t vocab, int64_t sequences) { return vocab > 4 * kSlice && sequences < 256 ? static_cast<int>((vocab + kSlice - 1) / kSlice) : 0; }
+
+template <bool DRAFT>
+void launch(const VerifyArgs &a, hipStream_t stream) {
+    const unsigned lds = static_cast<unsigned>(kNodeBytes * a.max_q);
+    if (!a.slices) {
+        hipLaunchKernelGGL((verify_kernel<DRAFT>), dim3(a.n_seqs), dim3(kBig), lds, stream, a);
+        return;
+    }
+    const dim3 grid(a.slices, a.n_seqs);
+    if (DRAFT && a.parents) {   // rows may have to be summed on the way
+        hipLaunchKernelGGL((verify_walk_kernel<DRAFT>), dim3(a.n_seqs), dim3(kBig), lds, stream, a);
+        hipLaunchKernelGGL((verify_slices_kernel<DRAFT, false>), grid, dim3(kSmall), 0, stream, a);
+    } else {
+        hipLaunchKernelGGL((verify_slices_kernel<DRAFT, true>), grid, dim3(kSmall), lds, stream, a);
+    }
+    hipLaunchKernelGGL((verify_draw_kernel<DRAFT>), dim3(a.n_seqs), dim3(kSmall), 0, stream, a);
+}
+
+}  // namespace
+
+int verify_most_tokens() { return kMaxNodes; }
+
+size_t verify_workspace(int64_t total, int32_t max_q, int32_t n_seqs, int64_t vocab) {
+    const int slices = slices_of(vocab, std::min<int64_t>(n_seqs, total));
+    return slices ? 8 * static_cast<size_t>(n_seqs) * (static_cast<size_t>(slices) + 1 + max_q) : 0;
+}
+
+tbn_status launch_verify(const VerifyCall &c, void *ws, hipStream_t stream) {
+    VerifyArgs a{c.target, c.draft, c.target_stride, c.draft_stride, c.tokens, c.parents, c.u, c.cu_q, c.picks, c.counts, c.next, c.total, c.max_q, c.n_seqs,
+                 static_cast<int32_t>(c.vocab), nullptr, nullptr, nullptr, slices_of(c.vocab, std::min<int64_t>(c.n_seqs, c.total))};
+    if (a.slices) {
+        a.parts = static_cast<double *>(ws);
+        a.refused = a.parts + int64_t(a.n_seqs) * a.slices;
+        a.ends = reinterpret_cast<int2 *>(a.refused + int64_t(a.n_seqs) * a.max_q);
+    }
+    if (a.draft) launch<true>(a, stream);
+    else launch<false>(a, stream);
+    return check_launch("tbn_verify");
+}
+
+}  // namespace tbn

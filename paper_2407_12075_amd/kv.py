@@ -16,6 +16,8 @@ marshalling only, PyTorch supplies device memory and the stream, there is no CPU
     kv.tbn_kv4_append / tbn_kv4_read / tbn_kv4_keep / tbn_kv4_copy_pages
     out, lse = kv.tbn_kv4_attention(q, pool, index, cu_q, max_q, mask=..., n_sink=..., window=...)
 
+    picks, counts, next = kv.tbn_verify(target, tokens, u, cu_q, max_q, draft=..., parents=...)   # picks and counts go to tbn_kv_keep
+
 ``KVPool``, ``KV4Pool`` and ``KVIndex`` hold the tensors and the C structs that describe them; build them once.
 """
 from __future__ import annotations
@@ -460,3 +462,43 @@ def tbn_kv4_attention(q: torch.Tensor, pool: KV4Pool, index: KVIndex, cu_q: torc
     _done(_call("tbn_kv4_attention", at, stride, _dt(q), _dev(out, "out"), _dev(lse, "lse", torch.float32), pool._at, index._at, cu, q.shape[0], max_q, q.shape[1],
                 n_sink, window, mask_at, words, max_len or 0, 1.0 / math.sqrt(pool.dim) if scale is None else scale, ws, size, _stream(stream)))
     return out, lse
+
+
+def _probabilities(t: torch.Tensor, name: str, like: Optional[torch.Tensor] = None) -> Tuple[int, int]:
+    """Address and row stride of (tokens, vocab) float32 whose rows are dense."""
+    if t.dim() != 2 or t.dtype != torch.float32 or (like is not None and t.shape != like.shape):
+        raise ValueError(f"{name} must be float32 (tokens, vocab)")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    n, v = t.shape
+    st = t.stride()
+    if t.numel() and ((v > 1 and st[1] != 1) or (n > 1 and st[0] < v)):
+        raise ValueError(f"{name}: rows must be dense and must not overlap (strides {st})")
+    return t.data_ptr(), st[0] if n > 1 else v
+
+
+def tbn_verify(target: torch.Tensor, tokens: torch.Tensor, u: torch.Tensor, cu_q: torch.Tensor, max_q: int, draft: Optional[torch.Tensor] = None,
+               parents: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+               stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Which drafted tokens stand.  target and draft (tokens, vocab) float32 probabilities, tokens and parents int32, u float32, cu_q int32 (sequences + 1).
+    Returns picks (sequences, max_q), counts and next (sequences), int32."""
+    if _plain(workspace, stream):
+        r = tbn._host.verify(target, tokens, u, cu_q, max_q, draft, parents)
+        if r is not None:
+            return r
+    dev, n_seqs = target.device, cu_q.numel() - 1
+    p, ps = _probabilities(target, "target")
+    q, qs = (None, 0) if draft is None else _probabilities(draft, "draft", target)
+    _same_device(dev, draft, tokens, u, cu_q, parents)
+    n, vocab = target.shape
+    for t, name in ((tokens, "tokens"), (u, "u"), (parents, "parents")):
+        if t is not None and t.numel() < n:
+            raise ValueError(f"{name} has {t.numel()} entries, {n} needed")
+    if n_seqs < 1 or max_q < 0:
+        raise ValueError("cu_q must have an entry more than there are sequences, max_q must be >= 0")
+    picks, counts, follows = (_empty(shape, torch.int32, dev, stream) for shape in ((n_seqs, max_q), (n_seqs,), (n_seqs,)))
+    ws, size = _workspace(int(lib().tbn_verify_workspace_bytes(n, max_q, n_seqs, vocab)), workspace, dev, stream)
+    _done(_call("tbn_verify", p, ps, q, qs, _dev(tokens, "tokens", torch.int32), None if parents is None else _dev(parents, "parents", torch.int32),
+                _dev(u, "u", torch.float32), _dev(cu_q, "cu_q", torch.int32), n, max_q, n_seqs, vocab, picks.data_ptr(), counts.data_ptr(), follows.data_ptr(),
+                ws, size, _stream(stream)))
+    return picks, counts, follows

@@ -136,6 +136,10 @@ def lib() -> ctypes.CDLL:
         L.tbn_kv4_attention_workspace_bytes.argtypes = [_c_vp, _c_vp, ctypes.c_int, _c_i64, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32, _c_i64]
         L.tbn_kv4_attention.argtypes = [_c_vp, _c_i64, ctypes.c_int, _c_vp, _c_vp, _c_vp, _c_vp, _c_vp, _c_i64, _c_i32, _c_i32, _c_i32, _c_i32, _c_vp,
                                         _c_i32, _c_i64, ctypes.c_float, _c_vp, _c_sz, _c_vp]
+        L.tbn_verify_workspace_bytes.restype = _c_sz
+        L.tbn_verify_workspace_bytes.argtypes = [_c_i64, _c_i32, _c_i32, _c_i64]
+        L.tbn_verify.restype = ctypes.c_int
+        L.tbn_verify.argtypes = [_c_vp, _c_i64, _c_vp, _c_i64, _c_vp, _c_vp, _c_vp, _c_vp, _c_i64, _c_i32, _c_i32, _c_i64, _c_vp, _c_vp, _c_vp, _c_vp, _c_sz, _c_vp]
         for name in ("append", "read", "copy_pages", "keep"):
             getattr(L, f"tbn_kv4_{name}").restype = ctypes.c_int
         for name in ("tree_attention", "window_attention", "kv4_attention", "block_select", "block_attention"):
@@ -151,7 +155,8 @@ def lib() -> ctypes.CDLL:
                 "tbn_linear_coltiled_workspace_bytes", "tbn_linear_coltiled_forward", "tbn_linear_forward_binact", "tbn_kv_workspace_bytes",
                 "tbn_kv_reserve", "tbn_kv_fork", "tbn_kv_release", "tbn_kv_copy_pages", "tbn_kv_append", "tbn_kv_keep",
                 "tbn_tree_attention_workspace_bytes", "tbn_tree_attention", "tbn_window_attention_workspace_bytes", "tbn_window_attention",
-                "tbn_kv4_append", "tbn_kv4_read", "tbn_kv4_copy_pages", "tbn_kv4_keep", "tbn_kv4_attention_workspace_bytes", "tbn_kv4_attention", "tbn_block_select_workspace_bytes", "tbn_block_select",
+                "tbn_kv4_append", "tbn_kv4_read", "tbn_kv4_copy_pages", "tbn_kv4_keep", "tbn_kv4_attention_workspace_bytes", "tbn_kv4_attention",
+                "tbn_verify_workspace_bytes", "tbn_verify", "tbn_block_select_workspace_bytes", "tbn_block_select",
                 "tbn_block_attention_workspace_bytes", "tbn_block_attention")})
             _host = _tbn_host
         except ImportError as e:   # not built, or built against another torch: the wrappers serve every call by themselves
