@@ -402,6 +402,7 @@ PyObject *kv_copy_pages(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
 }
 PyObject *kv4_copy_pages(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     HANDLE_TH_ERRORS
+    if (!p_kv4_copy_pages) Py_RETURN_NONE;
     return copy_pages(args, n_args, [](const Held &pool, const int32_t *a, const int32_t *b, int64_t n, const int32_t *count) {
         return p_kv4_copy_pages(pool4_of(pool), a, b, n, count, stream());
     });
@@ -427,7 +428,7 @@ PyObject *kv4_append(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     Held pool, ix;
     int64_t most, ks, vs;
     tbn_dtype dt, vt;
-    if (n_args != 8 || !ordinary_context() || !held(args[0], args[1], pool) || !held(args[2], args[3], ix) || pool.gpu != ix.gpu) Py_RETURN_NONE;
+    if (!p_kv4_append || n_args != 8 || !ordinary_context() || !held(args[0], args[1], pool) || !held(args[2], args[3], ix) || pool.gpu != ix.gpu) Py_RETURN_NONE;
     const at::Tensor *k = rows4(args[4], pool, pool4_of(pool)->kv_heads, ks, dt), *v = rows4(args[5], pool, pool4_of(pool)->kv_heads, vs, vt);
     const int32_t *cu = ints(args[6], int64_t(index_of(ix)->n_seqs) + 1, ix.gpu);
     if (!k || !v || !cu || dt != vt || k->size(0) != v->size(0) || !integer(args[7], 0, INT32_MAX, most)) Py_RETURN_NONE;
@@ -440,7 +441,7 @@ PyObject *kv4_read(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     HANDLE_TH_ERRORS
     Held pool, ix;
     int64_t most, total;
-    if (n_args != 8 || !ordinary_context() || !held(args[0], args[1], pool) || !held(args[2], args[3], ix) || pool.gpu != ix.gpu) Py_RETURN_NONE;
+    if (!p_kv4_read || n_args != 8 || !ordinary_context() || !held(args[0], args[1], pool) || !held(args[2], args[3], ix) || pool.gpu != ix.gpu) Py_RETURN_NONE;
     const int32_t *cu = ints(args[4], int64_t(index_of(ix)->n_seqs) + 1, ix.gpu);
     if (!cu || !integer(args[5], 0, INT32_MAX, most) || !integer(args[6], 1, 1 << 30, total) || !PyBool_Check(args[7])) Py_RETURN_NONE;
     const bool f32 = args[7] == Py_True;
@@ -475,6 +476,7 @@ PyObject *kv_keep(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
 }
 PyObject *kv4_keep(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     HANDLE_TH_ERRORS
+    if (!p_kv4_keep) Py_RETURN_NONE;
     return keep_keys(args, n_args, [](const Held &pool, const tbn_kv_index *ix, const int32_t *base, const int32_t *picks, int32_t width, const int32_t *counts) {
         return p_kv4_keep(pool4_of(pool), ix, base, picks, width, counts, stream());
     });
@@ -527,7 +529,7 @@ PyObject *window_attention(PyObject *, PyObject *const *args, Py_ssize_t n_args)
     int64_t sink, window;
     const uint32_t *mask;
     int32_t words;
-    if (n_args != 12 || !queries(args, a) || !scale_of(args[9], pool_of(a.pool)->dim, scale) || !integer(args[10], 0, INT32_MAX, sink) || !integer(args[11], 1, INT32_MAX, window) ||
+    if (!p_window_attention_workspace_bytes || !p_window_attention || n_args != 12 || !queries(args, a) || !scale_of(args[9], pool_of(a.pool)->dim, scale) || !integer(args[10], 0, INT32_MAX, sink) || !integer(args[11], 1, INT32_MAX, window) ||
         !mask_of(args[8], a.ix, a.q->size(0), mask, words))
         Py_RETURN_NONE;
     const int64_t n = a.q->size(0), heads = a.q->size(1);
@@ -552,7 +554,7 @@ PyObject *kv4_attention(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     int64_t sink, window;
     const uint32_t *mask;
     int32_t words;
-    if (n_args != 12 || !queries(args, a, true) || !scale_of(args[9], pool4_of(a.pool)->dim, scale) || !integer(args[10], 0, INT32_MAX, sink) ||
+    if (!p_kv4_attention_workspace_bytes || !p_kv4_attention || n_args != 12 || !queries(args, a, true) || !scale_of(args[9], pool4_of(a.pool)->dim, scale) || !integer(args[10], 0, INT32_MAX, sink) ||
         !integer(args[11], 0, INT32_MAX, window) || !mask_of(args[8], a.ix, a.q->size(0), mask, words))
         Py_RETURN_NONE;
     const int64_t n = a.q->size(0), heads = a.q->size(1);
@@ -656,7 +658,7 @@ const at::Tensor *probabilities(PyObject *o, int64_t &stride) {
 PyObject *verify(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     HANDLE_TH_ERRORS
     int64_t ps, qs = 0, most;
-    if (n_args != 7 || !ordinary_context()) Py_RETURN_NONE;
+    if (!p_verify_workspace_bytes || !p_verify || n_args != 7 || !ordinary_context()) Py_RETURN_NONE;
     const at::Tensor *p = probabilities(args[0], ps), *q = nullptr;
     if (!p || !integer(args[4], 0, 1 << 30, most)) Py_RETURN_NONE;
     const int64_t n = p->size(0), vocab = p->size(1), gpu = p->device().index();
@@ -714,20 +716,24 @@ PyObject *init(PyObject *, PyObject *args) {
     take(p_kv_keep, "tbn_kv_keep");
     take(p_tree_attention_workspace_bytes, "tbn_tree_attention_workspace_bytes");
     take(p_tree_attention, "tbn_tree_attention");
-    take(p_window_attention_workspace_bytes, "tbn_window_attention_workspace_bytes");
-    take(p_window_attention, "tbn_window_attention");
-    take(p_kv4_append, "tbn_kv4_append");
-    take(p_kv4_read, "tbn_kv4_read");
-    take(p_kv4_copy_pages, "tbn_kv4_copy_pages");
-    take(p_kv4_keep, "tbn_kv4_keep");
-    take(p_kv4_attention_workspace_bytes, "tbn_kv4_attention_workspace_bytes");
-    take(p_kv4_attention, "tbn_kv4_attention");
-    take(p_verify_workspace_bytes, "tbn_verify_workspace_bytes");
-    take(p_verify, "tbn_verify");
     take(p_block_select_workspace_bytes, "tbn_block_select_workspace_bytes");
     take(p_block_select, "tbn_block_select");
     take(p_block_attention_workspace_bytes, "tbn_block_attention_workspace_bytes");
     take(p_block_attention, "tbn_block_attention");
+    // A table may leave these out: they stay as they were, and without an address their calls are not taken.
+    auto take_if = [&](auto &fn, const char *name) {
+        if (PyDict_GetItemString(table, name)) take(fn, name);
+    };
+    take_if(p_window_attention_workspace_bytes, "tbn_window_attention_workspace_bytes");
+    take_if(p_window_attention, "tbn_window_attention");
+    take_if(p_kv4_append, "tbn_kv4_append");
+    take_if(p_kv4_read, "tbn_kv4_read");
+    take_if(p_kv4_copy_pages, "tbn_kv4_copy_pages");
+    take_if(p_kv4_keep, "tbn_kv4_keep");
+    take_if(p_kv4_attention_workspace_bytes, "tbn_kv4_attention_workspace_bytes");
+    take_if(p_kv4_attention, "tbn_kv4_attention");
+    take_if(p_verify_workspace_bytes, "tbn_verify_workspace_bytes");
+    take_if(p_verify, "tbn_verify");
     if (!ok) {
         PyErr_SetString(PyExc_ImportError, "_tbn_host: an entry point of the library is missing");
         return nullptr;
