@@ -7,8 +7,10 @@ cache (``kv.py``), and its operators run together as a server would use them:
 * the keys of the accepted path move together, the others are given back; a sequence that has ended frees its pages, and
   compaction brings the rest to the front of the pool.
 
-What is emitted is what the whole model picks (its highest logit) after each prefix: drafts change the speed only.  Weights
-are synthetic; embeddings, norms, residual sums and the choice of tokens are PyTorch's, everything else is the library's.  At this
+What is emitted is what the whole model picks (its highest logit) after each prefix, or, with a temperature, a draw from its probabilities
+(``tbn_verify`` accepts drafts so that they leave that distribution as it is): drafts change the speed only.  A model may look at a window of
+its text and the first tokens only (``window``, ``sinks``), and its cache may be held in 4 bits (``four_bit``; its drafts look at a window, too: picked
+blocks need the other cache).  Weights are synthetic; embeddings, norms, residual sums and the choice of tokens are PyTorch's, everything else is the library's.  At this
 size the host's launches set the pace (127 steps without drafts in 79 - 89 ms, 66 steps of four passes with them in 194 - 197 ms): what the
 example shows is how the calls fit together, and that drafts save steps, not that they pay.
 
@@ -40,6 +42,9 @@ class DecoderConfig:
     max_len: int = 4096
     n_seqs: int = 8
     dtype: torch.dtype = torch.bfloat16
+    window: int = 0                  # tokens that each one sees up to itself, 0: all
+    sinks: int = 4                   # first tokens that all see, where there is a window
+    four_bit: bool = False           # the cache in 4 bits
 
     @property
     def width(self) -> int:
@@ -82,7 +87,10 @@ class Decoder:
         self.max_pages = -(-cfg.max_len // cfg.page)
         self.place = (0.5 * torch.randn(self.max_pages * cfg.page, w, generator=gen)).to(device, cfg.dtype)
         n_pages = cfg.n_seqs * self.max_pages
-        self.pools = [kv.kv_pool(n_pages, cfg.kv_heads, cfg.dim, cfg.page, cfg.dtype, summary=True, device=device) for _ in range(cfg.layers)]
+        self.pools = [kv.kv4_pool(n_pages, cfg.kv_heads, cfg.dim, cfg.page, device=device) if cfg.four_bit else
+                      kv.kv_pool(n_pages, cfg.kv_heads, cfg.dim, cfg.page, cfg.dtype, summary=True, device=device) for _ in range(cfg.layers)]
+        self.append, self.keep, self.copy_pages = ((kv.tbn_kv4_append, kv.tbn_kv4_keep, kv.tbn_kv4_copy_pages) if cfg.four_bit else
+                                                   (kv.tbn_kv_append, kv.tbn_kv_keep, kv.tbn_kv_copy_pages))
         self.index = kv.kv_index(cfg.n_seqs, self.max_pages, n_pages, cfg.page, device=device)
         self.steps = 0   # of generate()
 
@@ -95,24 +103,33 @@ class Decoder:
         f = x.float()
         return (f * torch.rsqrt(f.square().mean(-1, keepdim=True) + 1e-6)).to(x.dtype)
 
+    def _attention(self, q: torch.Tensor, pool, cu: torch.Tensor, max_new: int, mask: Optional[torch.Tensor], n_select: int) -> torch.Tensor:
+        cfg, index = self.cfg, self.index
+        if n_select and not cfg.four_bit and not cfg.window:
+            picks = kv.tbn_block_select(q, pool, index, cu, max_new, n_select)
+            return kv.tbn_block_attention(q, pool, index, cu, max_new, picks)[0]
+        # drafts of a model with a window, or with a cache in 4 bits, see as many keys as the blocks would hold
+        window = min(n_select * cfg.page, cfg.window or n_select * cfg.page) if n_select else cfg.window
+        if cfg.four_bit:
+            return kv.tbn_kv4_attention(q, pool, index, cu, max_new, mask=mask, n_sink=cfg.sinks, window=window)[0]
+        if window:
+            return kv.tbn_window_attention(q, pool, index, cu, max_new, cfg.sinks, window, mask=mask)[0]
+        return kv.tbn_tree_attention(q, pool, index, cu, max_new, mask=mask)[0]
+
     def forward(self, tokens: torch.Tensor, places: torch.Tensor, counts: torch.Tensor, max_new: int, mask: Optional[torch.Tensor] = None,
                 n_select: int = 0) -> torch.Tensor:
         """Logits of `tokens` (all sequences', one after another; counts int32 of each), whose keys join the cache.  n_select: attention
-        over that many picked blocks of each query instead of all."""
+        over that many picked blocks of each query (or a window of as many keys) instead of all."""
         cfg, index = self.cfg, self.index
         cu = torch.nn.functional.pad(counts.cumsum(0, dtype=torch.int32), (1, 0))
         src, dst = kv.tbn_kv_reserve(index, counts)
         x = self.embed[tokens] + self.place[places.clamp(max=self.place.shape[0] - 1)]   # beyond: reserve has said no, check() raises
         q_end, k_end = cfg.heads, cfg.heads + cfg.kv_heads
         for i, pool in enumerate(self.pools):
-            kv.tbn_kv_copy_pages(pool, src, dst)
+            self.copy_pages(pool, src, dst)
             qkv = self._linear(4 * i, self._norm(x)).view(-1, cfg.heads + 2 * cfg.kv_heads, cfg.dim)
-            kv.tbn_kv_append(pool, index, qkv[:, q_end:k_end], qkv[:, k_end:], cu, max_new)
-            if n_select:
-                picks = kv.tbn_block_select(qkv[:, :q_end], pool, index, cu, max_new, n_select)
-                out, _ = kv.tbn_block_attention(qkv[:, :q_end], pool, index, cu, max_new, picks)
-            else:
-                out, _ = kv.tbn_tree_attention(qkv[:, :q_end], pool, index, cu, max_new, mask=mask)
+            self.append(pool, index, qkv[:, q_end:k_end], qkv[:, k_end:], cu, max_new)
+            out = self._attention(qkv[:, :q_end], pool, cu, max_new, mask, n_select)
             x = x + self._linear(4 * i + 1, out.view(-1, cfg.width))
             x = x + self._linear(4 * i + 3, self._linear(4 * i + 2, self._norm(x)))
         return self._linear(4 * cfg.layers, self._norm(x)).float()
@@ -137,19 +154,25 @@ class Decoder:
             kv.tbn_kv_fork(self.index, torch.zeros_like(children), children)
         return logits[-1].topk(copies).indices
 
-    def step(self, last: torch.Tensor, depth: int = 0, n_select: int = 4) -> Tuple[torch.Tensor, torch.Tensor]:
+    def step(self, last: torch.Tensor, depth: int = 0, n_select: int = 4, temperature: float = 0.0,
+             generator: Optional[torch.Generator] = None) -> Tuple[torch.Tensor, torch.Tensor]:
         """One step of the sequences below last.numel(), each of which ends with a token whose key is not in the cache yet.  Drafts `depth`
-        tokens (0: none).  Returns (tokens (sequences, depth + 1), counts): what follows `last`, of which counts are emitted."""
+        tokens (0: none).  Returns (tokens (sequences, depth + 1), counts): what follows `last`, of which counts are emitted.  temperature > 0:
+        tokens are drawn with numbers of `generator` (on the model's device)."""
         cfg, index, dev = self.cfg, self.index, self.device
         n = last.numel()
         live = torch.zeros(cfg.n_seqs, dtype=torch.int32, device=dev)
         live[:n] = 1
         base = index.lens.clone()
         first = base[:n].long()
-        nodes, draft = [last], last
+        nodes, draft, drawn_from = [last], last, []
         for d in range(depth):
             logits = self.forward(draft, first + d, live, 1, n_select=n_select)
-            best = logits.topk(2, 1).indices
+            if temperature > 0:
+                drawn_from.append(torch.softmax(logits / temperature, 1))
+                best = torch.multinomial(drawn_from[-1], 2, replacement=True, generator=generator)
+            else:
+                best = logits.topk(2, 1).indices
             nodes += [best[:, 0], best[:, 1]]
             draft = best[:, 0]
         if depth:
@@ -159,7 +182,10 @@ class Decoder:
         tree = torch.stack(nodes, 1)
         mask = torch.tensor(tree_mask(parents), dtype=torch.int32, device=dev).repeat(n, 1) if depth else None
         places = first[:, None] + torch.tensor(depths, device=dev)
-        choice = self.forward(tree.flatten(), places.flatten(), live * size, size, mask=mask).argmax(1).view(n, size)
+        logits = self.forward(tree.flatten(), places.flatten(), live * size, size, mask=mask)
+        if temperature > 0:
+            return self._sampled(torch.softmax(logits / temperature, 1), tree, parents, drawn_from, base, generator)
+        choice = logits.argmax(1).view(n, size)
         # down the tree, as long as the model's choice is one of the drafts
         at = torch.zeros(n, dtype=torch.int64, device=dev)
         going = torch.ones(n, dtype=torch.bool, device=dev)
@@ -174,14 +200,42 @@ class Decoder:
             emitted.append(choice.gather(1, at[:, None])[:, 0])
             going = main
         if depth:
-            kept = torch.zeros(cfg.n_seqs, depth + 1, dtype=torch.int32, device=dev)
-            kept[:n] = torch.stack(picks, 1)
-            many = torch.zeros(cfg.n_seqs, dtype=torch.int32, device=dev)
-            many[:n] = counts
-            for pool in self.pools:
-                kv.tbn_kv_keep(pool, index, base, kept, many)
-            kv.tbn_kv_release(index, base + many)
+            self._stand(base, torch.stack(picks, 1), counts)
         return torch.stack(emitted, 1), counts
+
+    def _stand(self, base: torch.Tensor, picks: torch.Tensor, counts: torch.Tensor) -> None:
+        """Of the keys from base on those of the picked places stay, the others are given back."""
+        cfg, index, n = self.cfg, self.index, picks.shape[0]
+        kept = torch.zeros(cfg.n_seqs, picks.shape[1], dtype=torch.int32, device=self.device)
+        kept[:n] = picks
+        many = torch.zeros(cfg.n_seqs, dtype=torch.int32, device=self.device)
+        many[:n] = counts
+        for pool in self.pools:
+            self.keep(pool, index, base, kept, many)
+        kv.tbn_kv_release(index, base + many)
+
+    def _sampled(self, target: torch.Tensor, tree: torch.Tensor, parents: List[int], drawn_from: List[torch.Tensor], base: torch.Tensor,
+                 generator: Optional[torch.Generator]) -> Tuple[torch.Tensor, torch.Tensor]:
+        """The end of a step with a temperature: target (all nodes' rows), the probabilities that each depth's tokens were drawn from."""
+        n, size = tree.shape
+        depth = len(drawn_from)
+        draft = None
+        if depth:   # the rows of the nodes that others hang on: the root, and the first token of each depth but the last
+            draft = torch.zeros_like(target).view(n, size, -1)
+            for d, q in enumerate(drawn_from):
+                draft[:, 2 * d - 1 if d else 0] = q
+            draft = draft.flatten(0, 1)
+        tokens = tree.int()
+        u = torch.rand(n * size, generator=generator, device=self.device)
+        cu = torch.arange(0, n * size + 1, size, dtype=torch.int32, device=self.device)
+        picks, counts, follows = kv.tbn_verify(target, tokens.flatten(), u, cu, size, draft=draft,
+                                               parents=torch.tensor(parents, dtype=torch.int32, device=self.device).repeat(n))
+        picks = picks[:, :depth + 1]
+        if depth:
+            self._stand(base, picks, counts)
+        emitted = tree.gather(1, torch.nn.functional.pad(picks[:, 1:], (0, 1)).clamp(min=0).long())   # behind the accepted ones: anything
+        emitted.scatter_(1, counts[:, None].long() - 1, follows[:, None].long())
+        return emitted, counts
 
     def end(self, seq: int) -> None:
         """Frees a sequence's pages and moves the others' to the front of the pool."""
@@ -190,16 +244,19 @@ class Decoder:
         kv.tbn_kv_release(self.index, keep)
         src, dst, count = kv.tbn_kv_compact(self.index)
         for pool in self.pools:
-            kv.tbn_kv_copy_pages(pool, src, dst, count)
+            self.copy_pages(pool, src, dst, count)
 
-    def generate(self, prompt: torch.Tensor, copies: int, n_new: int, depth: int = 0, n_select: int = 4) -> List[List[int]]:
-        """`copies` continuations of at least n_new tokens each (the first of them chosen by prompt(), the others as the model wants)."""
+    def generate(self, prompt: torch.Tensor, copies: int, n_new: int, depth: int = 0, n_select: int = 4, temperature: float = 0.0,
+                 seed: int = 0) -> List[List[int]]:
+        """`copies` continuations of at least n_new tokens each (the first of them chosen by prompt(), the others as the model wants, or,
+        with a temperature, drawn from what it gives)."""
+        generator = torch.Generator(self.device).manual_seed(seed) if temperature > 0 else None
         last = self.prompt(prompt, copies)
         texts = [[t] for t in last.tolist()]
         self.steps = 0
         while min(len(t) for t in texts) < n_new:
             self.steps += 1
-            tokens, counts = self.step(last, depth, n_select)
+            tokens, counts = self.step(last, depth, n_select, temperature, generator) if temperature > 0 else self.step(last, depth, n_select)
             last = tokens.gather(1, counts[:, None].long() - 1)[:, 0]
             for t, row, m in zip(texts, tokens.tolist(), counts.tolist()):
                 t += row[:m]

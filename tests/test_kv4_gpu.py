@@ -289,11 +289,8 @@ def test_infinite_logits_and_queries(kv, dt):
     assert torch.isfinite(out[2, 1].float()).all()
 
 
-@pytest.mark.parametrize("dt", ["f32", "bf16"])
-def test_float32_is_not_lost(kv, dt):
+def test_float32_is_not_lost(kv):
     """Small differences of large logits, long sums: float32 queries are not rounded to bfloat16."""
-    if dt == "bf16":
-        pytest.skip("bfloat16 queries are what they are")
     pool, index, keys, values = make_cache4(kv, 2, 128, 64, [3000, 1], seed=15)
     q, cu, qs = make_queries("f32", [1, 1], 4, 128, scale=6.0)
     out, lse = kv.tbn_kv4_attention(q, pool, index, cu, 1, scale=0.3)
