@@ -1,5 +1,7 @@
 // Layout and numbers of the cache held in 4 bits (tbn_kv4_pages.hip, tbn_kv4_attention.hip); what they mean: include/tbn.h.
 #pragma once
+#include <type_traits>
+
 #include "tbn_kv.h"
 
 namespace tbn {
@@ -7,6 +9,21 @@ namespace tbn {
 constexpr int8_t kNoNumber = -128;   // exponent of a key and value that are not numbers
 
 inline int exponent_bytes(int dim) { return dim <= 128 ? 4 : 8; }   // of a key of one head
+
+// calls f with dim / 32 as a constant
+template <typename F>
+inline void kv4_by_groups(int dim, F f) {
+    switch (dim / 32) {
+        case 1: return f(std::integral_constant<int, 1>());
+        case 2: return f(std::integral_constant<int, 2>());
+        case 3: return f(std::integral_constant<int, 3>());
+        case 4: return f(std::integral_constant<int, 4>());
+        case 5: return f(std::integral_constant<int, 5>());
+        case 6: return f(std::integral_constant<int, 6>());
+        case 7: return f(std::integral_constant<int, 7>());
+        default: return f(std::integral_constant<int, 8>());
+    }
+}
 
 #if defined(__HIPCC__)
 

@@ -3,14 +3,16 @@
 //
 //   S^T = K Q^T,  O^T += V^T P^T  (v_mfma_f32_16x16x32_bf16, keys or channels as rows, query rows as columns)
 //
-// A workgroup takes 16 rows; its waves take steps of 32 keys in turn.  A lane loads a quarter of a key's channels (dim / 8 bytes: 16 bytes of 128
-// channels) of two keys and eight keys of dim / 16 channels (dim / 4 bytes in a row, the order of the cache).  The order in which the first
-// product goes through the channels is free, so a lane's quarter is one run of them and q is loaded to match.
+// A workgroup takes 16 rows, or (FEW) as many as leave each of the 16 columns a row and a group of channels; its waves take steps of 32 keys in turn.
+// A lane loads a quarter of a key's channels (dim / 8 bytes: 16 of 128 channels) of two keys, and eight keys of dim / 16 channels (dim / 4 bytes in a row,
+// the order of the cache).  The order in which the first product goes through the channels is free, so a lane's quarter is one run of them and q
+// is loaded to match.
 //
 // A key's numbers are codes times 2^x, x for 32 channels.  Keys: the conversion to bfloat16 multiplies, which is exact.  Values: eight keys in a
 // lane's word have eight exponents, so they go to the weights instead: p 2^x is rounded to bfloat16 once for each 32 channels, with p's own
-// relative error, and the codes are taken as they are.  Codes are always finite, so a weight of 0 is enough to leave a value out; a key that
-// is no number gives not-a-number logits, and its row is that all over.
+// relative error, and the codes are taken as they are.  FEW, decoding above all: a column of P^T is a row's weights for one group, so that a lane makes them
+// once, not for each group, and of the second product each group's channels are taken from its own columns.  Codes are always finite: a
+// weight of 0 is enough to leave a value out.  A key that is no number gives not-a-number logits, and its row is that all over.
 //
 // float32 queries: q is the sum of three bfloat16 numbers (8 bits each), exactly, and so is each weight to 2^-24: three products of each kind.
 #include "tbn_kv4.h"
@@ -64,24 +66,33 @@ template <> struct Query<float> {
 
 template <int WORDS> struct Words { uint32_t w[WORDS]; };
 
-// NB: groups of 32 channels.  WINDOW: a window; TOKENS: blockIdx.y is a token (sequence_of).
-template <int NB, typename T, Kind KIND, bool TOKENS>
-__global__ __launch_bounds__(kAttnThreads, NB <= 4 ? 2 : 1) void kv4_attention_kernel(AttentionArgs a) {
+// Rows of a workgroup whose lanes share the groups of channels: each of the product's 16 columns is a row and a group.
+constexpr int shared_rows(int nb) { return nb == 1 ? 16 : nb == 2 ? 8 : nb <= 4 ? 4 : 2; }
+
+// Workgroups of a CU, by the registers that one takes.  Three are enough: 64 sequences of 4096 - 16384 keys take as long with four (151 us; a streaming
+// read of their bytes 135) and, where registers would have to be spilled for that, longer.
+constexpr int workgroups_of(int nb, int size) { return size == 2 ? (nb <= 4 ? 3 : nb == 5 ? 2 : 1) : nb <= 2 ? 3 : nb <= 4 ? 2 : 1; }
+
+// NB: groups of 32 channels.  FEW: at most shared_rows(NB) rows; TOKENS: blockIdx.y is a token (sequence_of).
+template <int NB, typename T, Kind KIND, bool FEW, bool TOKENS>
+__global__ __launch_bounds__(kAttnThreads, workgroups_of(NB, sizeof(T))) void kv4_attention_kernel(AttentionArgs a) {
     constexpr bool WINDOW = KIND == kWindow;
     constexpr int D = 32 * NB, NF = 2 * NB, EW = NB <= 4 ? 1 : 2, TERMS = Query<T>::kTerms, KS = 32;
+    constexpr int ROWS = FEW ? shared_rows(NB) : 16, NC = FEW ? 1 : NB;   // NC: groups that a lane's weights are made for
     __shared__ int2 listed[kListed];   // slot and page
-    __shared__ float sums[kAttnWaves][16][D + 4];
-    __shared__ float maxima[kAttnWaves][16], totals[2][kAttnWaves][16];
+    __shared__ float sums[kAttnWaves][ROWS][D + 4];
+    __shared__ float maxima[kAttnWaves][ROWS], totals[2][kAttnWaves][ROWS];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
+    const int col = n & (ROWS - 1), own = FEW ? n / ROWS : 0;   // this lane's row and, FEW, group of channels
     const int s = sequence_of<TOKENS>(a);
     if (TOKENS && s < 0) return;
     const int H = a.q.heads, KV = a.p.kv_heads, G = H / KV, P = a.p.page, shift = __ffs(P) - 1;
     const Span v = span_of(a, s);
     const Block blk = block_of(a);
-    const int head = blk.head, chunk = blk.chunk, base = blk.row_tile * 16, R = v.T * G;
+    const int head = blk.head, chunk = blk.chunk, base = blk.row_tile * ROWS, R = v.T * G;
     if (base >= R) return;
-    const int last = min(base + 16, R) - 1, end = keys_end(a, v, last, G);
+    const int last = min(base + ROWS, R) - 1, end = keys_end(a, v, last, G);
     Within in_reach = {};
     if constexpr (WINDOW) in_reach = within_of(a, v, base, last, G, shift);
     const int first = chunk * a.chunk, stop = WINDOW ? in_reach.end : end;
@@ -93,7 +104,7 @@ __global__ __launch_bounds__(kAttnThreads, NB <= 4 ? 2 : 1) void kv4_attention_k
         listed[i] = make_int2(slot, page_in(table[slot], static_cast<int>(a.p.n_pages)));
     }
 
-    const int row = base + n, place = min(row, R - 1) / G, low = WINDOW ? window_of(a, v, place) : 0;
+    const int row = base + col, place = min(row, R - 1) / G, low = WINDOW ? window_of(a, v, place) : 0;
     u32x4_t q[NB][TERMS];
     {
         const T *src = static_cast<const T *>(a.q.q) + (v.t0 + place) * a.q.q_stride + (head * G + min(row, R - 1) - place * G) * D + g * (8 * NB);
@@ -147,6 +158,8 @@ __global__ __launch_bounds__(kAttnThreads, NB <= 4 ? 2 : 1) void kv4_attention_k
         return i;
     };
 
+    const int all_see = a.mask ? v.prefix : v.prefix + base / G + 1;   // keys from here on are not seen by every row
+    const int all_from = WINDOW ? last_window(a, v, last, G) : 0;      // keys before this one, the first ones aside, neither
     __syncthreads();
     Step x;
     int key = 0, page = 0;
@@ -155,20 +168,16 @@ __global__ __launch_bounds__(kAttnThreads, NB <= 4 ? 2 : 1) void kv4_attention_k
         load_k(x, page, key & (P - 1));
         load_v(x, page, key & (P - 1));
     }
-    const int all_see = a.mask ? v.prefix : v.prefix + base / G + 1;   // keys from here on are not seen by every row
-    const int all_from = WINDOW ? last_window(a, v, last, G) : 0;      // keys before this one, the first ones aside, neither
     while (i < steps) {
-        int next_key = 0, next_page = 0;
-        const int next = next_step(i + kAttnWaves, next_key, next_page);
         float p[8];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int h = 0; h < 2; ++h) {
             f32x4_t s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int f = 0; f < NB; ++f) {
                 const int c = (g * NB + f) >> 2;   // the group that these eight channels lie in
-                const uint32_t e = EW == 1 ? x.ke[t].w[0] : c < 4 ? x.ke[t].w[0] : x.ke[t].w[EW - 1];
-                const u32x4_t k = kv4_values(x.k[t].w[f], kv4_scale(e, c & 3));
+                const uint32_t e = EW == 1 ? x.ke[h].w[0] : c < 4 ? x.ke[h].w[0] : x.ke[h].w[EW - 1];
+                const u32x4_t k = kv4_values(x.k[h].w[f], kv4_scale(e, c & 3));
                 if constexpr (TERMS == 3) {
                     s1 = mma(k, q[f][2], s1);
                     s1 = mma(k, q[f][1], s1);
@@ -177,10 +186,16 @@ __global__ __launch_bounds__(kAttnThreads, NB <= 4 ? 2 : 1) void kv4_attention_k
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e)   // an infinite logit is one already in the first terms, whatever the others' signs
-                p[4 * t + e] = TERMS == 3 && fabsf(s0[e]) < INFINITY ? s0[e] + s1[e] : s0[e];
+                p[4 * h + e] = TERMS == 3 && fabsf(s0[e]) < INFINITY ? s0[e] + s1[e] : s0[e];
         }
-        Step y;
-        if (next < steps) load_k(y, next_page, next_key & (P - 1));
+        // the next step's loads, or the same ones again: never left out, so that the waits before their use are for as many as there are
+        int next_key = 0, next_page = 0;
+        const int next = next_step(i + kAttnWaves, next_key, next_page);
+        if (next >= steps) {
+            next_key = key;
+            next_page = page;
+        }
+        load_k(x, next_page, next_key & (P - 1));
 
         bool edge = key + KS > all_see;   // wave-uniform
         if constexpr (WINDOW) edge |= key < all_from && key + KS > a.n_sink;
@@ -210,27 +225,29 @@ __global__ __launch_bounds__(kAttnThreads, NB <= 4 ? 2 : 1) void kv4_attention_k
         if constexpr (TERMS == 1)
 #pragma unroll
             for (int e = 0; e < 4; ++e) z = add_two_bf16(two_bf16(p[2 * e], p[2 * e + 1]), z);
+        u32x4_t w[NC][TERMS];   // the weights as operand, times the values' powers of two
 #pragma unroll
-        for (int c = 0; c < NB; ++c) {
-            u32x4_t w[TERMS];
+        for (int c = 0; c < NC; ++c)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                float lo = __builtin_ldexpf(p[2 * e], static_cast<int8_t>(x.ve[2 * e].w[c >> 2] >> (8 * (c & 3))));
-                float hi = __builtin_ldexpf(p[2 * e + 1], static_cast<int8_t>(x.ve[2 * e + 1].w[c >> 2] >> (8 * (c & 3))));
-                if constexpr (TERMS == 1) w[0][e] = two_bf16(lo, hi);
+                auto times = [&](int j) {
+                    const int b = FEW ? own : c;
+                    const uint32_t word = EW == 1 || b < 4 ? x.ve[j].w[0] : x.ve[j].w[EW - 1];
+                    return __builtin_ldexpf(p[j], static_cast<int8_t>(word >> (8 * (b & 3))));
+                };
+                float lo = times(2 * e), hi = times(2 * e + 1);
+                if constexpr (TERMS == 1) w[c][0][e] = two_bf16(lo, hi);
                 else
 #pragma unroll
-                    for (int t = 0; t < TERMS; ++t) w[t][e] = split_off(lo, hi);
+                    for (int t = 0; t < TERMS; ++t) w[c][t][e] = split_off(lo, hi);
             }
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const u32x4_t d = kv4_values(x.v.w[2 * c + h], 1.f);
+        for (int f = 0; f < NF; ++f) {
+            const u32x4_t d = kv4_values(x.v.w[f], 1.f);
 #pragma unroll
-                for (int t = TERMS - 1; t >= 0; --t) o[2 * c + h] = mma(d, w[t], o[2 * c + h]);
-            }
+            for (int t = TERMS - 1; t >= 0; --t) o[f] = mma(d, w[FEW ? 0 : f / 2][t], o[f]);
         }
-        if (next < steps) load_v(y, next_page, next_key & (P - 1));
-        x = y;
+        load_v(x, next_page, next_key & (P - 1));
         i = next;
         key = next_key;
         page = next_page;
@@ -242,20 +259,21 @@ __global__ __launch_bounds__(kAttnThreads, NB <= 4 ? 2 : 1) void kv4_attention_k
     ls += __shfl_xor(ls, 32);
     zs += __shfl_xor(zs, 16);
     zs += __shfl_xor(zs, 32);
-    if (g == 0) {
-        maxima[wave][n] = m;
-        totals[0][wave][n] = ls;
-        totals[1][wave][n] = zs;
+    if (lane < ROWS) {
+        maxima[wave][lane] = m;
+        totals[0][wave][lane] = ls;
+        totals[1][wave][lane] = zs;
     }
     __syncthreads();
-    float top = maxima[0][n];
+    float top = maxima[0][col];
 #pragma unroll
-    for (int u = 1; u < kAttnWaves; ++u) top = fmaxf(top, maxima[u][n]);
+    for (int u = 1; u < kAttnWaves; ++u) top = fmaxf(top, maxima[u][col]);
     const float f0 = m == top ? 1.f : exp2_of(m - top);
 #pragma unroll
-    for (int f = 0; f < NF; ++f) *reinterpret_cast<f32x4_t *>(&sums[wave][n][f * 16 + 4 * g]) = o[f] * f0;
+    for (int f = 0; f < NF; ++f)
+        if (!FEW || own == f / 2) *reinterpret_cast<f32x4_t *>(&sums[wave][col][f * 16 + 4 * g]) = o[f] * f0;
     __syncthreads();
-    for (int j = tid; j < 16 * (D / 4); j += kAttnThreads) {
+    for (int j = tid; j < ROWS * (D / 4); j += kAttnThreads) {
         const int rr = j / (D / 4), d = (j - rr * (D / 4)) * 4, row = base + rr;
         if (row >= R) continue;
         float best = maxima[0][rr];
@@ -280,20 +298,28 @@ tbn_kv_pool view_of(const tbn_kv4_pool &p, tbn_dtype dt) { return tbn_kv_pool{p.
 
 Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t keys) {
     Plan pl;
-    const int64_t places = p.dim <= 128 ? 512 : 256;
-    pl.staged = false;
-    pl.rows = 16;
+    const int few = shared_rows(p.dim / 32);
+    // The kernel that stages keys takes as long for 64 (128) rows as this file's for about 4 (7) tiles of 16, whose last ones ragged drafts often do not
+    // need.  16 trees of up to 16 / 24 / 26 / 32 tokens on 4000 keys, 4 heads to a kv head: 40 / 51 / 54 / 55 us, here 44 / 49 / 47 / 65; 12 tokens 38 to 33.  On many
+    // keys it is the faster one with fewer (26 tokens on 60000 keys: 56 us, 77 here; 10 tokens level); 512 tokens on 16000: 173 us to 292.
+    pl.staged = p.dt == TBN_BF16 && rows > 48 && (rows <= 64 || rows > 112 || keys >= 16384);
+    pl.rows = pl.staged ? (rows <= 64 ? 64 : 128) : rows <= few ? few : 16;
     pl.row_tiles = static_cast<int>(ceil_div(rows, pl.rows));
     const int64_t blocks = groups * pl.row_tiles;
-    int64_t chunk = ceil_div(keys, ceil_div(8192, blocks));
-    const double fill = static_cast<double>(keys) * blocks / places;
-    const double want = fill <= 256 ? fill : std::fmax(256, std::fmin(1024, 8 * std::sqrt(fill)));
-    const int64_t least = static_cast<int64_t>(want / 128 + 0.5) * 128;
-    if (chunk < least) chunk = least;
-    if (keys <= 1024 && blocks >= 256) chunk = keys;
+    int64_t chunk;
+    if (pl.staged) {
+        // one round of the places for workgroups (512 tokens on 16000 keys: 173 us, 183 in two, 191 in four)
+        chunk = std::max<int64_t>(256, ceil_div(keys, ceil_div(p.dim <= 128 ? 512 : 256, blocks)));
+    } else {
+        // Stretches of about sqrt(fill) keys, fill: keys of each place, up to 1536 (64 sequences of up to 16384 keys: 151 us; 154 with 1152, 160 with 2304, 180 with
+        // 512, where starting costs a third).  Few keys to a place: one step of each wave at least.
+        const double fill = static_cast<double>(keys) * blocks / (p.dim <= 128 ? 768 : 256);
+        const double want = fill <= 256 ? fill : std::fmax(256, std::fmin(1536, 15 * std::sqrt(fill)));
+        chunk = std::max(ceil_div(keys, ceil_div(8192, blocks)), static_cast<int64_t>(want / 128 + 0.5) * 128);
+        if (keys <= 1024 && blocks >= 256) chunk = keys;   // the join would take longer
+    }
     if (keys <= 256) chunk = keys;
-    chunk = ceil_div(chunk, 128) * 128;
-    if (chunk > int64_t(kListed) * p.page) chunk = int64_t(kListed) * p.page;
+    chunk = std::min(ceil_div(chunk, 128) * 128, int64_t(kListed) * p.page);
     pl.chunk = static_cast<int>(chunk);
     pl.n_chunks = static_cast<int>(ceil_div(keys, chunk));
     return pl;
@@ -304,20 +330,28 @@ Plan plan_of_call(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries 
     return plan_by_sequences(p, ix, q, keys, [&](int64_t rows, int64_t groups, int64_t units) { return plan_of(p, rows, groups, units); });
 }
 
-template <int NB, typename T, Kind KIND>
+template <int NB, typename T, Kind KIND, bool FEW>
 void launch_tokens(const AttentionArgs &a, bool tokens, dim3 grid, hipStream_t stream) {
-    if (tokens) hipLaunchKernelGGL((kv4_attention_kernel<NB, T, KIND, true>), grid, dim3(kAttnThreads), 0, stream, a);
-    else hipLaunchKernelGGL((kv4_attention_kernel<NB, T, KIND, false>), grid, dim3(kAttnThreads), 0, stream, a);
+    if (tokens) hipLaunchKernelGGL((kv4_attention_kernel<NB, T, KIND, FEW, true>), grid, dim3(kAttnThreads), 0, stream, a);
+    else hipLaunchKernelGGL((kv4_attention_kernel<NB, T, KIND, FEW, false>), grid, dim3(kAttnThreads), 0, stream, a);
+}
+
+template <int NB, typename T, Kind KIND>
+void launch_rows(const AttentionArgs &a, int rows, bool tokens, dim3 grid, hipStream_t stream) {
+    if constexpr (NB > 1) {
+        if (rows < 16) return launch_tokens<NB, T, KIND, true>(a, tokens, grid, stream);
+    }
+    launch_tokens<NB, T, KIND, false>(a, tokens, grid, stream);
 }
 
 template <int NB>
-void launch_groups(const AttentionArgs &a, Kind kind, bool tokens, dim3 grid, hipStream_t stream) {
+void launch_groups(const AttentionArgs &a, Kind kind, int rows, bool tokens, dim3 grid, hipStream_t stream) {
     if (a.p.dt == TBN_F32) {
-        if (kind == kWindow) launch_tokens<NB, float, kWindow>(a, tokens, grid, stream);
-        else launch_tokens<NB, float, kAll>(a, tokens, grid, stream);
+        if (kind == kWindow) launch_rows<NB, float, kWindow>(a, rows, tokens, grid, stream);
+        else launch_rows<NB, float, kAll>(a, rows, tokens, grid, stream);
     } else {
-        if (kind == kWindow) launch_tokens<NB, uint16_t, kWindow>(a, tokens, grid, stream);
-        else launch_tokens<NB, uint16_t, kAll>(a, tokens, grid, stream);
+        if (kind == kWindow) launch_rows<NB, uint16_t, kWindow>(a, rows, tokens, grid, stream);
+        else launch_rows<NB, uint16_t, kAll>(a, rows, tokens, grid, stream);
     }
 }
 
@@ -343,16 +377,8 @@ tbn_status launch_kv4_attention(const tbn_kv4_pool &pool, const tbn_kv_index &ix
     bool tokens;
     const tbn_status st = spread(a, pl, ws, kind, what, grid, tokens);
     if (st != TBN_OK) return st;
-    switch (p.dim / 32) {
-        case 1: launch_groups<1>(a, kind, tokens, grid, stream); break;
-        case 2: launch_groups<2>(a, kind, tokens, grid, stream); break;
-        case 3: launch_groups<3>(a, kind, tokens, grid, stream); break;
-        case 4: launch_groups<4>(a, kind, tokens, grid, stream); break;
-        case 5: launch_groups<5>(a, kind, tokens, grid, stream); break;
-        case 6: launch_groups<6>(a, kind, tokens, grid, stream); break;
-        case 7: launch_groups<7>(a, kind, tokens, grid, stream); break;
-        default: launch_groups<8>(a, kind, tokens, grid, stream); break;
-    }
+    if (pl.staged) launch_kv4_rows(a, kind, pl.rows / 32, tokens, grid, stream);
+    else kv4_by_groups(p.dim, [&](auto nb) { launch_groups<nb()>(a, kind, pl.rows, tokens, grid, stream); });
     if (a.n_chunks > 1) launch_kv_join(a, kind, pl.rows, tokens, grid.y, stream);
     return check_launch(what);
 }

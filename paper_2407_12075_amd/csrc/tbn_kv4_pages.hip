@@ -9,8 +9,6 @@
 // so a key that enters a word others have is put between their bits.  One wave takes a block of a head; no two of a launch write to one word.
 //
 // Everything here moves bytes.
-#include <type_traits>
-
 #include "tbn_kv4.h"
 
 namespace tbn {
@@ -96,29 +94,43 @@ __global__ __launch_bounds__(kWave) void kv4_append_kernel(tbn_kv4_pool p, tbn_k
     for (int i = lane; i < 2 * kBlock * EW; i += kWave) exps[i / (kBlock * EW)][i / EW % kBlock][i % EW] = 0;
     __syncthreads();
     int8_t *x8 = reinterpret_cast<int8_t *>(exps);
-    for (int i = lane; i < 2 * rows * 4 * NB; i += kWave) {   // eight channels of a key, then of a value
-        const int r = i / (4 * NB), c = i - r * (4 * NB);
-        const bool value = r >= rows;
-        const int at = value ? r - rows : r;
-        float f[8], a = 0.f;
-        Eight<T>::load(value ? vs + at * v_stride + 8 * c : ks + at * k_stride + 8 * c, f);
-        bool bad = false;
+    // Eight channels of a key, then of a value.  kAhead rounds are loaded before the first is looked at; lanes behind the last one take it again, so
+    // that all go through the exchange between lanes together, and write nothing.
+    constexpr int kAhead = 4;
+    const int units = 2 * rows * 4 * NB;
+    for (int i0 = lane; i0 - lane < units; i0 += kAhead * kWave) {
+        float f[kAhead][8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            a = fmaxf(a, fabsf(f[e]));
-            bad |= !(fabsf(f[e]) < INFINITY);
+        for (int j = 0; j < kAhead; ++j) {
+            const int i = min(i0 + j * kWave, units - 1), r = i / (4 * NB), c = i - r * (4 * NB);
+            Eight<T>::load(r >= rows ? vs + (r - rows) * v_stride + 8 * c : ks + r * k_stride + 8 * c, f[j]);
         }
-        const int x = kv4_exponent(max_of_quad(a));
-        const uint32_t w = kv4_codes(f, pow2_of(x));
-        if (value) {
-            uint8_t *to = codes + 8 * c * PITCH + sh.r0 + at;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) to[e * PITCH] = (w >> (4 * e)) & 15u;
-        } else {
-            kc[at * (D / 8) + c] = w;
+        for (int j = 0; j < kAhead; ++j) {
+            if (i0 - lane + j * kWave >= units) break;
+            const int i = min(i0 + j * kWave, units - 1), r = i / (4 * NB), c = i - r * (4 * NB);
+            const bool value = r >= rows;
+            const int at = value ? r - rows : r;
+            float a = 0.f;
+            bool bad = false;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                a = fmaxf(a, fabsf(f[j][e]));
+                bad |= !(fabsf(f[j][e]) < INFINITY);
+            }
+            const int x = kv4_exponent(max_of_quad(a));
+            if (i0 + j * kWave >= units) continue;
+            const uint32_t w = kv4_codes(f[j], pow2_of(x));
+            if (value) {
+                uint8_t *to = codes + 8 * c * PITCH + sh.r0 + at;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) to[e * PITCH] = (w >> (4 * e)) & 15u;
+            } else {
+                kc[at * (D / 8) + c] = w;
+            }
+            if ((c & 3) == 0) x8[((value ? kBlock : 0) + at) * (4 * EW) + (c >> 2)] = static_cast<int8_t>(x);
+            if (bad) odd[at] = 1;
         }
-        if ((c & 3) == 0) x8[((value ? kBlock : 0) + at) * (4 * EW) + (c >> 2)] = static_cast<int8_t>(x);
-        if (bad) odd[at] = 1;
     }
     __syncthreads();
     for (int i = lane; i < 2 * rows * EW; i += kWave) {
@@ -263,28 +275,13 @@ __global__ __launch_bounds__(kThreads) void kv4_keep_kernel(tbn_kv4_pool p, tbn_
     }
 }
 
-// calls f with dim / 32 as a constant
-template <typename F>
-void by_groups(int dim, F f) {
-    switch (dim / 32) {
-        case 1: return f(std::integral_constant<int, 1>());
-        case 2: return f(std::integral_constant<int, 2>());
-        case 3: return f(std::integral_constant<int, 3>());
-        case 4: return f(std::integral_constant<int, 4>());
-        case 5: return f(std::integral_constant<int, 5>());
-        case 6: return f(std::integral_constant<int, 6>());
-        case 7: return f(std::integral_constant<int, 7>());
-        default: return f(std::integral_constant<int, 8>());
-    }
-}
-
 // blocks that n keys can touch: one more than they fill
 unsigned blocks_of(int32_t n) { return static_cast<unsigned>((int64_t(n) + kBlock - 2) / kBlock + 1); }
 
 template <typename T>
 void launch_append_typed(const tbn_kv4_pool &p, const tbn_kv_index &ix, const void *k, int64_t k_stride, const void *v, int64_t v_stride, const int32_t *cu,
                          int total, int32_t most, hipStream_t stream) {
-    by_groups(p.dim, [&](auto nb) {
+    kv4_by_groups(p.dim, [&](auto nb) {
         hipLaunchKernelGGL((kv4_append_kernel<T, nb()>), dim3(blocks_of(most), p.kv_heads, ix.n_seqs), dim3(kWave), 0, stream, p, ix, static_cast<const T *>(k), k_stride,
                            static_cast<const T *>(v), v_stride, cu, total);
     });
@@ -292,7 +289,7 @@ void launch_append_typed(const tbn_kv4_pool &p, const tbn_kv_index &ix, const vo
 
 template <typename T>
 void launch_read_typed(const tbn_kv4_pool &p, const tbn_kv_index &ix, void *k, void *v, const int32_t *cu, int total, int32_t most, hipStream_t stream) {
-    by_groups(p.dim, [&](auto nb) {
+    kv4_by_groups(p.dim, [&](auto nb) {
         hipLaunchKernelGGL((kv4_read_kernel<T, nb()>), dim3(blocks_of(most), p.kv_heads, ix.n_seqs), dim3(kWave), 0, stream, p, ix, static_cast<T *>(k), static_cast<T *>(v), cu,
                            total);
     });

@@ -361,6 +361,8 @@ constexpr int64_t kMostBlocks = 0x7fffffff;   // workgroups of a sequence
 
 // Fills in how `pl` splits the call and the grid of its launch; an error where one launch cannot hold it.
 tbn_status spread(AttentionArgs &a, const Plan &pl, float *ws, Kind kind, const char *what, dim3 &grid, bool &tokens);
+// the cache in 4 bits, many rows, bfloat16: `tiles` (2 or 4) of 32 rows per workgroup
+void launch_kv4_rows(const AttentionArgs &a, Kind kind, int tiles, bool tokens, dim3 grid, hipStream_t stream);
 // the second kernel of a split call
 void launch_kv_join(const AttentionArgs &a, Kind kind, int tile_rows, bool tokens, unsigned groups, hipStream_t stream);
 

@@ -20,7 +20,8 @@ namespace tbn {
 namespace {
 
 constexpr int kBig = 1024, kSmall = 256;   // threads of a workgroup
-constexpr int kSlice = 4096;               // elements of a row that a workgroup sums
+constexpr int kSlice = 4096;
+constexpr int kDraw = kSlice / 16;         // threads of the last launch's workgroups               // elements of a row that a workgroup sums
 
 struct VerifyArgs {
     const float *target, *draft;
@@ -45,48 +46,62 @@ struct Rest {
     int n;
 };
 
-// r at element v.  Negative numbers and not-a-numbers count as 0.
+__device__ __forceinline__ double count(float p) { return p > 0.f ? static_cast<double>(p) : 0.; }   // negative numbers and not-a-numbers are 0
+
+// r of element v after one refusal.
+template <bool DRAFT>
+__device__ __forceinline__ double refuse(double r, double q, double refused, int v) {
+#pragma clang fp contract(off)
+    if constexpr (DRAFT) {
+        const double part = refused * q, d = r - part;
+        return d > 0. ? d : 0.;
+    } else {
+        return refused == static_cast<double>(v) ? 0. : r;
+    }
+}
+
+// r of one element, whose p and q are at hand
 template <bool DRAFT>
 __device__ __forceinline__ double left_of(const Rest &x, int v, float p, float q) {
-#pragma clang fp contract(off)
-    double r = p > 0.f ? static_cast<double>(p) : 0.;
-    const double qd = q > 0.f ? static_cast<double>(q) : 0.;
-    for (int i = 0; i < x.n; ++i) {
-        if constexpr (DRAFT) {
-            const double part = x.refused[i] * qd, d = r - part;
-            r = d > 0. ? d : 0.;
-        } else {
-            r = x.refused[i] == static_cast<double>(v) ? 0. : r;
-        }
-    }
+    double r = count(p);
+    for (int i = 0; i < x.n; ++i) r = refuse<DRAFT>(r, count(q), x.refused[i], v);
     return r;
 }
 
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
-// four elements from v on, those below hi
-template <bool DRAFT>
-__device__ __forceinline__ void four_of(const Rest &x, int v, int hi, double (&r)[4]) {
-    float p[4] = {0.f, 0.f, 0.f, 0.f}, q[4] = {0.f, 0.f, 0.f, 0.f};
+__device__ __forceinline__ void four_at(const float *row, int v, int hi, float (&f)[4]) {
     if (v + 4 <= hi) {
-        const f32x4_any a = *reinterpret_cast<const f32x4_any *>(x.p + v);
+        const f32x4_any w = *reinterpret_cast<const f32x4_any *>(row + v);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) p[e] = a[e];
-        if (DRAFT && x.n) {
-            const f32x4_any b = *reinterpret_cast<const f32x4_any *>(x.q + v);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) q[e] = b[e];
-        }
+        for (int e = 0; e < 4; ++e) f[e] = w[e];
     } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (v + e < hi) {
-                p[e] = x.p[v + e];
-                if (DRAFT && x.n) q[e] = x.q[v + e];
-            }
+        for (int e = 0; e < 4; ++e) f[e] = v + e < hi ? row[v + e] : 0.f;
+    }
+}
+
+// r of J times four elements, from v + j * step on, those below hi (others 0).
+template <bool DRAFT, int J>
+__device__ __forceinline__ void fours_of(const Rest &x, int v, int step, int hi, double (&r)[J][4]) {
+    float p[J][4], q[J][4];
+#pragma unroll
+    for (int j = 0; j < J; ++j) four_at(x.p, v + j * step, hi, p[j]);
+    if (DRAFT && x.n) {
+#pragma unroll
+        for (int j = 0; j < J; ++j) four_at(x.q, v + j * step, hi, q[j]);
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) r[e] = left_of<DRAFT>(x, v + e, p[e], q[e]);
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[j][e] = count(p[j][e]);
+    for (int i = 0; i < x.n; ++i) {
+        const double refused = x.refused[i];
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[j][e] = refuse<DRAFT>(r[j][e], DRAFT ? count(q[j][e]) : 0., refused, v + j * step + e);
+    }
 }
 
 __device__ __forceinline__ double sum_of_wave(double s) {
@@ -98,20 +113,23 @@ __device__ __forceinline__ double sum_of_wave(double s) {
 // Sum of a wave's elements [lo, hi).
 template <bool DRAFT>
 __device__ __forceinline__ double sum_of(const Rest &x, int lo, int hi) {
+    constexpr int kVectors = 4;
     double s = 0.;
-#pragma unroll 4
-    for (int v = lo + 4 * (threadIdx.x & 63); v < hi; v += 4 * kWave) {
-        double r[4];
-        four_of<DRAFT>(x, v, hi, r);
-        s += (r[0] + r[1]) + (r[2] + r[3]);
+    for (int base = lo; base < hi; base += kVectors * 4 * kWave) {
+        double r[kVectors][4];
+        fours_of<DRAFT, kVectors>(x, base + 4 * (threadIdx.x & 63), 4 * kWave, hi, r);
+#pragma unroll
+        for (int j = 0; j < kVectors; ++j) s += (r[j][0] + r[j][1]) + (r[j][2] + r[j][3]);
     }
     return sum_of_wave(s);
 }
 
 struct DrawLds {
     double sums[kBig / kWave];
-    int token;
+    int token, last;
 };
+
+__device__ __forceinline__ bool drawable(double sum) { return sum > 0. && sum < INFINITY; }
 
 // Every wave of the workgroup takes an equal run of [lo, hi); their sums in order.  Every thread calls it.
 template <bool DRAFT, int THREADS>
@@ -158,53 +176,78 @@ __device__ __forceinline__ void narrow(const double *sums, int run, int &lo, int
     hi = min(lo + run, hi);
 }
 
-// The first element of [lo, hi) whose prefix sum is above `at`, else the last one that is not 0 (-1: none).  One wave.
-template <bool DRAFT>
-__device__ int find_in(const Rest &x, int lo, int hi, double at) {
+__device__ __forceinline__ double prefix_of_wave(double s) {   // inclusive
     const int lane = threadIdx.x & 63;
-    int last = -1;
-    for (int base = lo; base < hi; base += 4 * kWave) {
-        double r[4];
-        four_of<DRAFT>(x, min(base + 4 * lane, hi), hi, r);
-        const double own = (r[0] + r[1]) + (r[2] + r[3]);
-        double sum = own;   // inclusive prefix over the lanes
 #pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) {
-            const double below = __shfl_up(sum, d);
-            if (lane >= d) sum += below;
-        }
-        double s = sum - own;
-        int mine = -1, mine_last = -1;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            s += r[e];
-            if (r[e] > 0.) {
-                mine_last = base + 4 * lane + e;
-                if (mine < 0 && s > at) mine = mine_last;
-            }
-        }
-        const uint64_t hit = __ballot(mine >= 0), any = __ballot(mine_last >= 0);
-        if (hit) return __shfl(mine, __ffsll(static_cast<unsigned long long>(hit)) - 1);
-        if (any) last = __shfl(mine_last, 63 - __clzll(static_cast<long long>(any)));
-        at -= __shfl(sum, 63);
+    for (int d = 1; d < kWave; d <<= 1) {
+        const double below = __shfl_up(s, d);
+        if (lane >= d) s += below;
     }
-    return last;
+    return s;
 }
 
-// The token of a row, given the sum over [lo, hi) and where in it the draw lies.  Every thread calls it; the result is every thread's.
+// The first element of [lo, hi) whose prefix sum is above `at`, else the last one that is not 0 (-1: none).  SHARE: `at` is a share of the sum, and the
+// result -2 where that is no positive finite number.  At most kEach elements of each thread, which are loaded once; every thread calls it.
+constexpr int kEach = 16;
+template <bool DRAFT, bool SHARE, int THREADS>
+__device__ int find_in(const Rest &x, int lo, int hi, double at, DrawLds &l) {
+    constexpr int kWaves = THREADS / kWave;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, from = lo + tid * kEach;
+    double r[kEach / 4][4], own = 0.;
+    fours_of<DRAFT, kEach / 4>(x, from, 4, hi, r);
+#pragma unroll
+    for (int i = 0; i < kEach / 4; ++i) own += (r[i][0] + r[i][1]) + (r[i][2] + r[i][3]);
+    const double incl = prefix_of_wave(own);
+    __syncthreads();   // the sums may still be read from the call before
+    if (lane == 63) l.sums[wave] = incl;
+    if (tid == 0) {
+        l.token = INT32_MAX;
+        l.last = -1;
+    }
+    __syncthreads();
+    double before = 0., sum = 0.;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        before = w == wave ? sum : before;
+        sum += l.sums[w];
+    }
+    if (SHARE) {
+        if (!drawable(sum)) return -2;   // the same for all
+        at *= sum;
+    }
+    double s = before + (incl - own);
+    int mine = INT32_MAX, last = -1;
+#pragma unroll
+    for (int i = 0; i < kEach / 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            s += r[i][e];
+            if (r[i][e] > 0.) {
+                last = from + 4 * i + e;
+                if (s > at) mine = min(mine, last);
+            }
+        }
+    const uint64_t hit = __ballot(mine != INT32_MAX), any = __ballot(last >= 0);
+    if (hit && lane == __ffsll(static_cast<unsigned long long>(hit)) - 1) atomicMin(&l.token, mine);
+    if (any && lane == 63 - __clzll(static_cast<long long>(any))) atomicMax(&l.last, last);
+    __syncthreads();
+    return l.token != INT32_MAX ? l.token : l.last;
+}
+
+// The token of [lo, hi) at the share u of its sum; -2 where that is no positive finite number.
 template <bool DRAFT, int THREADS>
-__device__ int find_token(const Rest &x, int lo, int hi, double at, DrawLds &l) {
-    while (hi - lo > 8 * kWave) {
-        int run;
+__device__ int draw_in(const Rest &x, int lo, int hi, double u, DrawLds &l) {
+    if (hi - lo <= THREADS * kEach) return find_in<DRAFT, true, THREADS>(x, lo, hi, u, l);
+    int run;
+    double sum = sums_of_waves<DRAFT, THREADS>(x, lo, hi, l, run);
+    if (!drawable(sum)) return -2;
+    double at = u * sum;
+    narrow<THREADS / kWave>(l.sums, run, lo, hi, at);
+    while (hi - lo > THREADS * kEach) {
         (void)sums_of_waves<DRAFT, THREADS>(x, lo, hi, l, run);
         narrow<THREADS / kWave>(l.sums, run, lo, hi, at);
     }
-    if (threadIdx.x < kWave) {
-        const int token = find_in<DRAFT>(x, lo, hi, at);
-        if (threadIdx.x == 0) l.token = token;
-    }
-    __syncthreads();
-    return l.token;
+    return find_in<DRAFT, false, THREADS>(x, lo, hi, at, l);
 }
 
 // What the walk leaves behind.
@@ -305,30 +348,22 @@ __device__ __forceinline__ void nothing(const VerifyArgs &a, int s) {
     }
 }
 
-__device__ __forceinline__ bool drawable(double sum) { return sum > 0. && sum < INFINITY; }
-
 // A workgroup for each sequence does everything.
-template <bool DRAFT>
-__global__ __launch_bounds__(kBig) void verify_kernel(VerifyArgs a) {
+template <bool DRAFT, int THREADS>
+__global__ __launch_bounds__(THREADS) void verify_kernel(VerifyArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ DrawLds l;
     const int s = blockIdx.x;
     int t0, T;
     if (!sequence_at(a, s, t0, T)) return nothing(a, s);
     const Nodes nodes = nodes_at(lds, a.max_q);
-    const End end = walk<DRAFT, DRAFT, kBig>(a, t0, T, nodes, l, a.picks + int64_t(s) * a.max_q);
+    const End end = walk<DRAFT, DRAFT, THREADS>(a, t0, T, nodes, l, a.picks + int64_t(s) * a.max_q);
     Rest x{a.target + (t0 + end.at) * a.target_stride, DRAFT ? a.draft + (t0 + end.at) * a.draft_stride : nullptr, nodes.refused + end.at + 1, end.n};
-    int run, lo = 0, hi = a.vocab;
-    double sum = sums_of_waves<DRAFT, kBig>(x, lo, hi, l, run);
-    if (!drawable(sum) && x.n) {   // nothing is left: the target's row itself
+    const double u = static_cast<double>(nodes.u[0]);
+    int token = draw_in<DRAFT, THREADS>(x, 0, a.vocab, u, l);
+    if (token == -2) {   // nothing is left: the target's row itself
         x.n = 0;
-        sum = sums_of_waves<DRAFT, kBig>(x, lo, hi, l, run);
-    }
-    int token = -1;
-    if (drawable(sum)) {
-        double at = static_cast<double>(nodes.u[0]) * sum;
-        narrow<kBig / kWave>(l.sums, run, lo, hi, at);
-        token = find_token<DRAFT, kBig>(x, lo, hi, at, l);
+        token = max(draw_in<DRAFT, THREADS>(x, 0, a.vocab, u, l), -1);
     }
     if (threadIdx.x == 0) {
         a.counts[s] = end.count;
@@ -395,7 +430,7 @@ __global__ __launch_bounds__(kBig) void verify_walk_kernel(VerifyArgs a) {
 
 // Last launch: the slice and the token in it.
 template <bool DRAFT>
-__global__ __launch_bounds__(kSmall) void verify_draw_kernel(VerifyArgs a) {
+__global__ __launch_bounds__(kDraw) void verify_draw_kernel(VerifyArgs a) {
     __shared__ DrawLds l;
     const int s = blockIdx.x, lane = threadIdx.x & 63;
     const int2 end = a.ends[s];
@@ -431,28 +466,25 @@ __global__ __launch_bounds__(kSmall) void verify_draw_kernel(VerifyArgs a) {
         }
         at -= last_start;
         const int lo = last * kSlice, hi = min(lo + kSlice, a.vocab);
-        token = find_token<DRAFT, kSmall>(x, lo, hi, at, l);
+        static_assert(kSlice <= kDraw * kEach, "a slice fits the registers of a workgroup");
+        token = find_in<DRAFT, false, kDraw>(x, lo, hi, at, l);
     } else if (x.n) {   // nothing is left: the target's row itself
         x.n = 0;
-        int run, lo = 0, hi = a.vocab;
-        sum = sums_of_waves<DRAFT, kSmall>(x, lo, hi, l, run);
-        if (drawable(sum)) {
-            double at = u * sum;
-            narrow<kSmall / kWave>(l.sums, run, lo, hi, at);
-            token = find_token<DRAFT, kSmall>(x, lo, hi, at, l);
-        }
+        token = max(draw_in<DRAFT, kDraw>(x, 0, a.vocab, u, l), -1);
     }
     if (threadIdx.x == 0) a.next[s] = token;
 }
 
 // Rows go in slices where they are long and the sequences are too few to give every CU one.
-int slices_of(int64_t vocab, int64_t sequences) { return vocab > 4 * kSlice && sequences < 256 ? static_cast<int>((vocab + kSlice - 1) / kSlice) : 0; }
+int slices_of(int64_t vocab, int64_t sequences) { return vocab > 16384 && sequences < 256 ? static_cast<int>((vocab + kSlice - 1) / kSlice) : 0; }
 
 template <bool DRAFT>
 void launch(const VerifyArgs &a, hipStream_t stream) {
     const unsigned lds = static_cast<unsigned>(kNodeBytes * a.max_q);
     if (!a.slices) {
-        hipLaunchKernelGGL((verify_kernel<DRAFT>), dim3(a.n_seqs), dim3(kBig), lds, stream, a);
+        // as few threads as hold the row in their registers: waiting for each other costs less (1024 elements: 7.2 us in place of 7.9)
+        if (a.vocab <= kSmall * kEach) hipLaunchKernelGGL((verify_kernel<DRAFT, kSmall>), dim3(a.n_seqs), dim3(kSmall), lds, stream, a);
+        else hipLaunchKernelGGL((verify_kernel<DRAFT, kBig>), dim3(a.n_seqs), dim3(kBig), lds, stream, a);
         return;
     }
     const dim3 grid(a.slices, a.n_seqs);
@@ -462,7 +494,7 @@ void launch(const VerifyArgs &a, hipStream_t stream) {
     } else {
         hipLaunchKernelGGL((verify_slices_kernel<DRAFT, true>), grid, dim3(kSmall), lds, stream, a);
     }
-    hipLaunchKernelGGL((verify_draw_kernel<DRAFT>), dim3(a.n_seqs), dim3(kSmall), 0, stream, a);
+    hipLaunchKernelGGL((verify_draw_kernel<DRAFT>), dim3(a.n_seqs), dim3(kDraw), 0, stream, a);
 }
 
 }  // namespace
