@@ -309,7 +309,7 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t keys) {
     int64_t chunk;
     if (pl.staged) {
         // one round of the places for workgroups (512 tokens on 16000 keys: 173 us, 183 in two, 191 in four)
-        chunk = std::max<int64_t>(256, ceil_div(keys, ceil_div(p.dim <= 128 ? 512 : 256, blocks)));
+        chunk = std::max<int64_t>(std::min<int64_t>(256, keys), ceil_div(keys, ceil_div(p.dim <= 128 ? 512 : 256, blocks)));
     } else {
         // Stretches of about sqrt(fill) keys, fill: keys of each place, up to 1536 (64 sequences of up to 16384 keys: 151 us; 154 with 1152, 160 with 2304, 180 with
         // 512, where starting costs a third).  Few keys to a place: one step of each wave at least.
@@ -318,7 +318,9 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t keys) {
         chunk = std::max(ceil_div(keys, ceil_div(8192, blocks)), static_cast<int64_t>(want / 128 + 0.5) * 128);
         if (keys <= 1024 && blocks >= 256) chunk = keys;   // the join would take longer
     }
-    if (keys <= 256) chunk = keys;
+    // nor are few keys split, where the join's launch takes longer than the steps it saves (one token, 8 kv heads of 128 channels: 513 keys 7.3 us, 10.7 in
+    // parts; 1000 keys 9.2 to 9.7, 1500 11.8 to 10.1; float32 513 keys 9.5 to 10.1, 1000 12.2 to 10.1)
+    if (!pl.staged && keys <= (p.dt == TBN_BF16 ? 1024 : 640)) chunk = keys;
     chunk = std::min(ceil_div(chunk, 128) * 128, int64_t(kListed) * p.page);
     pl.chunk = static_cast<int>(chunk);
     pl.n_chunks = static_cast<int>(ceil_div(keys, chunk));

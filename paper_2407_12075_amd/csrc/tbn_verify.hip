@@ -21,7 +21,7 @@ namespace {
 
 constexpr int kBig = 1024, kSmall = 256;   // threads of a workgroup
 constexpr int kSlice = 4096;
-constexpr int kDraw = kSlice / 16;         // threads of the last launch's workgroups               // elements of a row that a workgroup sums
+constexpr int kDraw = kSlice / 16;         // threads of the last launch's workgroups
 
 struct VerifyArgs {
     const float *target, *draft;
