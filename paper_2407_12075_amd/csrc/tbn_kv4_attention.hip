@@ -131,14 +131,14 @@ __global__ __launch_bounds__(kAttnThreads, workgroups_of(NB, sizeof(T))) void kv
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             x.k[t] = *reinterpret_cast<const Words<NB> *>(static_cast<const uint32_t *>(a.p.k) + (key + 4 * t) * (D / 8) + g * NB);
-            x.ke[t] = *reinterpret_cast<const Words<EW> *>(a.k_exp + (key + 4 * t) * (4 * EW));
+            x.ke[t] = *reinterpret_cast<const Words<EW> *>(a.p.summary + (key + 4 * t) * (4 * EW));
         }
     };
     auto load_v = [&](Step &x, int page, int off) {
         const int64_t key = page * page_keys + int64_t(head) * P + off;
         x.v = *reinterpret_cast<const Words<NF> *>(static_cast<const uint32_t *>(a.p.v) + key * (D / 8) + (g * 16 + n) * NF);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x.ve[e] = *reinterpret_cast<const Words<EW> *>(a.v_exp + (key + 8 * g + e) * (4 * EW));
+        for (int e = 0; e < 8; ++e) x.ve[e] = *reinterpret_cast<const Words<EW> *>(reinterpret_cast<const int8_t *>(a.p.step) + (key + 8 * g + e) * (4 * EW));
     };
     const int sub_shift = shift - 5, steps = entries << sub_shift;
     // step i of this stretch: its first key, -1 if there is nothing in it; wave-uniform
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(kAttnThreads, workgroups_of(NB, sizeof(T))) void kv
         const int2 e = listed[i >> sub_shift];
         page = __builtin_amdgcn_readfirstlane(e.y);
         const int key = (__builtin_amdgcn_readfirstlane(e.x) << shift) + (i & ((1 << sub_shift) - 1)) * KS;
-        if (WINDOW && key >= a.n_sink && key + KS <= in_reach.low) return -1;
+        if (WINDOW && key >= a.window.sink && key + KS <= in_reach.low) return -1;
         return key >= end ? -1 : key;
     };
     auto next_step = [&](int i, int &key, int &page) {
@@ -198,7 +198,7 @@ __global__ __launch_bounds__(kAttnThreads, workgroups_of(NB, sizeof(T))) void kv
         load_k(x, next_page, next_key & (P - 1));
 
         bool edge = key + KS > all_see;   // wave-uniform
-        if constexpr (WINDOW) edge |= key < all_from && key + KS > a.n_sink;
+        if constexpr (WINDOW) edge |= key < all_from && key + KS > a.window.sink;
         if (edge) {
             const uint32_t bits = seen_within<KIND>(a, v, key + 8 * g, end, place, low);
 #pragma unroll
@@ -294,7 +294,7 @@ __global__ __launch_bounds__(kAttnThreads, workgroups_of(NB, sizeof(T))) void kv
 }
 
 // The queries' view of the cache: sizes as there, the queries' type.
-tbn_kv_pool view_of(const tbn_kv4_pool &p, tbn_dtype dt) { return tbn_kv_pool{p.k, p.v, nullptr, nullptr, p.n_pages, p.kv_heads, p.dim, p.page, dt}; }
+tbn_kv_pool view_of(const tbn_kv4_pool &p, tbn_dtype dt) { return tbn_kv_pool{p.k, p.v, p.k_exp, reinterpret_cast<float *>(p.v_exp), p.n_pages, p.kv_heads, p.dim, p.page, dt}; }
 
 Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t keys) {
     Plan pl;
@@ -369,11 +369,9 @@ tbn_status launch_kv4_attention(const tbn_kv4_pool &pool, const tbn_kv_index &ix
     const char *what = "tbn_kv4_attention";
     const Kind kind = window ? kWindow : kAll;
     const tbn_kv_pool p = view_of(pool, dt);
-    AttentionArgs a{p, ix, q, out, lse, mask, mask_words, nullptr, 0, factor_of(scale), flip_of(p, scale)};
-    a.n_sink = n_sink;
-    a.window = window;
-    a.k_exp = pool.k_exp;
-    a.v_exp = pool.v_exp;
+    AttentionArgs a{p, ix, q, out, lse, mask, mask_words, {nullptr}, 0, factor_of(scale), flip_of(p, scale)};
+    a.window.sink = n_sink;
+    a.window.size = window;
     const Plan pl = plan_of_call(p, ix, q, n_sink, window, mask != nullptr);
     dim3 grid;
     bool tokens;

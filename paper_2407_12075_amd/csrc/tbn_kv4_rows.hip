@@ -79,10 +79,10 @@ __global__ __launch_bounds__(kAttnThreads, NB <= 4 ? 2 : 1) void kv4_rows_kernel
         const int off = i * KEYS + part * 32, page = __builtin_amdgcn_readfirstlane(listed[min(off >> shift, entries - 1)]);
         const int64_t key = page * page_keys + int64_t(blk.head) * P + (off & (P - 1));
         x.k = *reinterpret_cast<const Words<NB> *>(static_cast<const uint32_t *>(a.p.k) + (key + key_row) * (D / 8) + quarter * NB);
-        x.ke = *reinterpret_cast<const Words<EW> *>(a.k_exp + (key + key_row) * (4 * EW));
+        x.ke = *reinterpret_cast<const Words<EW> *>(a.p.summary + (key + key_row) * (4 * EW));
         x.v = *reinterpret_cast<const Words<NB> *>(static_cast<const uint32_t *>(a.p.v) + key * (D / 8) + (kg * 16 + kn) * NF + kf);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x.ve[e] = *reinterpret_cast<const Words<EW> *>(a.v_exp + (key + 8 * kg + e) * (4 * EW));
+        for (int e = 0; e < 8; ++e) x.ve[e] = *reinterpret_cast<const Words<EW> *>(reinterpret_cast<const int8_t *>(a.p.step) + (key + 8 * kg + e) * (4 * EW));
     };
     auto store = [&](const Step &x, uint16_t *kt, uint16_t *vt) {
         const int r = part * 32 + row_of_key(key_row);
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(kAttnThreads, NB <= 4 ? 2 : 1) void kv4_rows_kernel
 #pragma unroll
             for (int t = 0; t < KEYS; t += 32) {
                 const int k = in_reach.key(key + t);
-                edge |= k + 32 > all_see || (k < all_from && k + 32 > a.n_sink);
+                edge |= k + 32 > all_see || (k < all_from && k + 32 > a.window.sink);
             }
         } else {
             edge |= key + KEYS > all_see;

@@ -20,15 +20,22 @@ constexpr int kListed = 1024;   // pages of a workgroup's stretch of keys, at mo
 constexpr float kSlack = 8.f;   // a row's sums are scaled down when a logit passes their reference by more: weights stay below 2^8
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
-struct AttentionArgs {   // of one launch
-    tbn_kv_pool p;
+struct WindowArgs {
+    int32_t sink, size;   // the first keys, which every token sees, and how many up to its own place
+};
+
+struct AttentionArgs {   // of one launch; not above 248 bytes (256 and 276 cost a call on one token 0.2 - 0.3 us)
+    tbn_kv_pool p;      // a cache in 4 bits: k and v its codes, summary and step its exponents, dt the queries' type
     tbn_kv_index ix;
     KvQueries q;
     void *out;
     float *lse;
     const uint32_t *mask;
     int32_t mask_words;
-    const int32_t *picks;
+    union {
+        const int32_t *picks;   // of a call on picked pages
+        WindowArgs window;      // of a call with a window
+    };
     int32_t n_select;
     float c;            // |scale| log2 e, never 0 (times an infinite logit it would be no number)
     uint32_t flip;      // sign bits of the query's elements, where the scale is negative
@@ -37,8 +44,6 @@ struct AttentionArgs {   // of one launch
     int32_t chunk;      // keys, or picks, of a workgroup
     int32_t n_chunks;
     int32_t row_tiles;  // tiles of a workgroup's rows
-    int32_t n_sink, window;   // of a call with a window: the first keys that every token sees, and how many up to its own place
-    const int8_t *k_exp, *v_exp;   // of a cache in 4 bits (p.k, p.v: its codes, p.dt: the queries' type)
 };
 
 // what the rows of a launch see: every key up to their own, the pages they picked, the first keys and a window
@@ -210,8 +215,8 @@ __device__ __forceinline__ Within within_of(const AttentionArgs &a, const Span &
     const int end = keys_end(a, v, row1, G), pages = (end + a.p.page - 1) >> shift;
     Within w;
     // with a mask a row's place is what it has above it, none at least
-    w.low = max((a.mask ? v.prefix - 1 : v.prefix + row0 / G) - a.window + 1, 0);
-    const int sink = (min(a.n_sink, end) + a.p.page - 1) >> shift, from = w.low >> shift;
+    w.low = max((a.mask ? v.prefix - 1 : v.prefix + row0 / G) - a.window.size + 1, 0);
+    const int sink = (min(a.window.sink, end) + a.p.page - 1) >> shift, from = w.low >> shift;
     w.head = sink << shift;
     w.gap = from > sink && from < pages ? (from - sink) << shift : 0;
     w.end = from >= pages ? min(w.head, end) : end - w.gap;
@@ -227,12 +232,12 @@ __device__ __forceinline__ int window_of(const AttentionArgs &a, const Span &v, 
         at = v.prefix - 1;
         for (int w = 0; w * 32 < v.T; ++w) at += __popc(mask[w] & (v.T - w * 32 >= 32 ? ~0u : (1u << (v.T - w * 32)) - 1u));
     }
-    return at - a.window + 1;
+    return at - a.window.size + 1;
 }
 
 // no row's window begins behind this key
 __device__ __forceinline__ int last_window(const AttentionArgs &a, const Span &v, int row1, int G) {
-    return v.prefix + (a.mask ? v.T - 1 : row1 / G) - a.window + 1;
+    return v.prefix + (a.mask ? v.T - 1 : row1 / G) - a.window.size + 1;
 }
 
 // a word with its first n bits set, as far as it has them
@@ -283,7 +288,7 @@ __device__ __forceinline__ uint32_t seen_bits(const AttentionArgs &a, const Span
 template <Kind KIND>
 __device__ __forceinline__ uint32_t seen_within(const AttentionArgs &a, const Span &v, int k0, int end, int place, int low) {
     uint32_t bits = seen_bits<KIND == kPicked>(a, v, k0, end, place);
-    if constexpr (KIND == kWindow) bits &= first_bits(a.n_sink - k0) | ~first_bits(low - k0);
+    if constexpr (KIND == kWindow) bits &= first_bits(a.window.sink - k0) | ~first_bits(low - k0);
     return bits;
 }
 
@@ -365,6 +370,8 @@ tbn_status spread(AttentionArgs &a, const Plan &pl, float *ws, Kind kind, const 
 void launch_kv4_rows(const AttentionArgs &a, Kind kind, int tiles, bool tokens, dim3 grid, hipStream_t stream);
 // the second kernel of a split call
 void launch_kv_join(const AttentionArgs &a, Kind kind, int tile_rows, bool tokens, unsigned groups, hipStream_t stream);
+
+static_assert(sizeof(AttentionArgs) <= 248, "kernel arguments");
 
 // picked blocks, bfloat16: queries that share a workgroup (0: none), 32 rows at most
 int picked_queries(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, int32_t n_select);

@@ -79,7 +79,8 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
         if (first >= stop && chunk > 0) return;
         entries = (min(stop, first + a.chunk) - first + P - 1) >> shift;
         for (int i = tid; i < entries; i += kAttnThreads) {
-            const int slot = (WINDOW ? in_reach.key(first + (i << shift)) : first + (i << shift)) >> shift;
+            int slot = (first >> shift) + i;
+            if constexpr (WINDOW) slot = in_reach.key(slot << shift) >> shift;
             listed[i] = make_int2(slot, page_in(table[slot], n_pages));
         }
     }
@@ -150,7 +151,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
         page = __builtin_amdgcn_readfirstlane(e.y);
         const int slot = __builtin_amdgcn_readfirstlane(e.x);
         const int key = (slot << shift) + (i & ((1 << sub_shift) - 1)) * KS;
-        if (WINDOW && key >= a.n_sink && key + KS <= in_reach.low) return -1;
+        if (WINDOW && key >= a.window.sink && key + KS <= in_reach.low) return -1;
         return slot < 0 || key >= end ? -1 : key;
     };
     auto next_step = [&](int i, int &key, int &page) {
@@ -215,7 +216,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_attention_
         if (next < steps) load_k(k, next_page, next_key & (P - 1));
 
         bool edge = key + KS > all_see;   // wave-uniform
-        if constexpr (WINDOW) edge |= key < all_from && key + KS > a.n_sink;
+        if constexpr (WINDOW) edge |= key < all_from && key + KS > a.window.sink;
         uint32_t seen[RT];
         bool odd = false;
         if (edge) {
@@ -594,7 +595,7 @@ size_t tree_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, co
 
 tbn_status launch_tree_attention(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, void *out, float *lse, const uint32_t *mask,
                                  int32_t mask_words, float scale, float *ws, hipStream_t stream) {
-    AttentionArgs a{p, ix, q, out, lse, mask, mask_words, nullptr, 0, factor_of(scale), flip_of(p, scale)};
+    AttentionArgs a{p, ix, q, out, lse, mask, mask_words, {nullptr}, 0, factor_of(scale), flip_of(p, scale)};
     return launch<kAll>(a, tree_plan(p, ix, q, q.max_len), ws, "tbn_tree_attention", stream);
 }
 
@@ -604,9 +605,9 @@ size_t window_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, 
 
 tbn_status launch_window_attention(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, void *out, float *lse, int32_t n_sink, int32_t window,
                                    const uint32_t *mask, int32_t mask_words, float scale, float *ws, hipStream_t stream) {
-    AttentionArgs a{p, ix, q, out, lse, mask, mask_words, nullptr, 0, factor_of(scale), flip_of(p, scale)};
-    a.n_sink = n_sink;
-    a.window = window;
+    AttentionArgs a{p, ix, q, out, lse, mask, mask_words, {nullptr}, 0, factor_of(scale), flip_of(p, scale)};
+    a.window.sink = n_sink;
+    a.window.size = window;
     return launch<kWindow>(a, tree_plan(p, ix, q, window_keys(p, q, n_sink, window, mask != nullptr)), ws, "tbn_window_attention", stream);
 }
 
@@ -616,7 +617,7 @@ size_t block_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, c
 
 tbn_status launch_block_attention(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, void *out, float *lse, const int32_t *picks,
                                   int32_t n_select, float scale, float *ws, hipStream_t stream) {
-    AttentionArgs a{p, ix, q, out, lse, nullptr, 0, picks, n_select, factor_of(scale), flip_of(p, scale)};
+    AttentionArgs a{p, ix, q, out, lse, nullptr, 0, {picks}, n_select, factor_of(scale), flip_of(p, scale)};
     const char *what = "tbn_block_attention";
     if (const int queries = picked_queries(p, ix, q, n_select)) {
         a.n_chunks = 1;

@@ -159,7 +159,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
 #pragma unroll
             for (int t = 0; t < KEYS; t += 32) {
                 const int k = in_reach.key(key + t);
-                edge |= k + 32 > all_see || (k < all_from && k + 32 > a.n_sink);
+                edge |= k + 32 > all_see || (k < all_from && k + 32 > a.window.sink);
             }
         } else {
             edge |= key + KEYS > all_see;
