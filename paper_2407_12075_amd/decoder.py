@@ -10,8 +10,10 @@ cache (``kv.py``), and its operators run together as a server would use them:
 What is emitted is what the whole model picks (its highest logit) after each prefix, or, with a temperature, a draw from its probabilities
 (``tbn_verify`` accepts drafts so that they leave that distribution as it is): drafts change the speed only.  A model may look at a window of
 its text and the first tokens only (``window``, ``sinks``), and its cache may be held in 4 bits (``four_bit``; its drafts look at a window, too: picked
-blocks need the other cache).  Weights are synthetic; embeddings, norms, residual sums and the choice of tokens are PyTorch's, everything else is the library's.  At this
-size the host's launches set the pace (127 steps without drafts in 79 - 89 ms, 66 steps of four passes with them in 194 - 197 ms): what the
+blocks need the other cache).
+
+Weights are synthetic; embeddings, norms, residual sums, softmax and the choice of tokens without a temperature are PyTorch's, everything else is the library's.
+At this size the host's launches set the pace (127 steps without drafts in 79 - 89 ms, 66 steps of four passes with them in 194 - 197 ms): what the
 example shows is how the calls fit together, and that drafts save steps, not that they pay.
 
     python -m paper_2407_12075_amd.decoder          # tokens per second with and without drafts on cuda:0
@@ -265,19 +267,20 @@ class Decoder:
 
 
 def main() -> None:
-    cfg = DecoderConfig()
-    prompt = torch.randint(0, cfg.vocab, (2000,), generator=torch.Generator().manual_seed(1)).cuda()
-    copies, n_new, texts = 8, 128, {}
-    for depth in (0, 3):
+    prompt = torch.randint(0, DecoderConfig.vocab, (2000,), generator=torch.Generator().manual_seed(1)).cuda()
+    copies, n_new = 8, 128
+    for name, more, depth, temperature in (("bfloat16 cache", {}, 0, 0.0), ("bfloat16 cache", {}, 3, 0.0), ("window of 512", dict(window=512), 0, 0.0),
+                                           ("cache in 4 bits", dict(four_bit=True), 0, 0.0), ("cache in 4 bits", dict(four_bit=True), 3, 1.0)):
+        cfg = DecoderConfig(**more)
         for timed in (False, True):
             model = Decoder(cfg)
             torch.cuda.synchronize()
             t = time.perf_counter()
-            texts[depth] = model.generate(prompt, copies, n_new, depth)
+            texts = model.generate(prompt, copies, n_new, depth, temperature=temperature)
             torch.cuda.synchronize()
             t = time.perf_counter() - t
-        print(json.dumps({"example": "decoder", "copies": copies, "prompt": prompt.numel(), "drafted_depth": depth, "tokens": sum(map(len, texts[depth])), "steps": model.steps,
-                          "ms": round(1e3 * t, 2), "tokens_per_s": round(sum(map(len, texts[depth])) / t),
+        print(json.dumps({"example": "decoder", "cache": name, "copies": copies, "prompt": prompt.numel(), "drafted_depth": depth, "temperature": temperature,
+                          "tokens": sum(map(len, texts)), "steps": model.steps, "ms": round(1e3 * t, 2), "tokens_per_s": round(sum(map(len, texts)) / t),
                           "pages_in_use": int((model.index.refs > 0).sum()), "data": "synthetic", "dtype": str(cfg.dtype)}), flush=True)
 
 
