@@ -311,16 +311,19 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t keys) {
         // one round of the places for workgroups (512 tokens on 16000 keys: 173 us, 183 in two, 191 in four)
         chunk = std::max<int64_t>(std::min<int64_t>(256, keys), ceil_div(keys, ceil_div(p.dim <= 128 ? 512 : 256, blocks)));
     } else {
-        // Stretches of about sqrt(fill) keys, fill: keys of each place, up to 1536 (64 sequences of up to 16384 keys: 151 us; 154 with 1152, 160 with 2304, 180 with
-        // 512, where starting costs a third).  Few keys to a place: one step of each wave at least.
-        const double fill = static_cast<double>(keys) * blocks / (p.dim <= 128 ? 768 : 256);
-        const double want = fill <= 256 ? fill : std::fmax(256, std::fmin(1536, 15 * std::sqrt(fill)));
-        chunk = std::max(ceil_div(keys, ceil_div(8192, blocks)), static_cast<int64_t>(want / 128 + 0.5) * 128);
+        // fill: keys of each place for a workgroup.  Up to 1024 one round of the places, 256 keys at least (bfloat16, 128 channels, 8 kv heads: 16 sequences of
+        // 3000 keys 15.6 us with 512, 17.6 with 384, 18.5 with 256; one of 8000 keys 10.3 with 256, 12.5 with 128; one of 60000 keys 20 - 21 with 768 - 1024, 23.6 with 384).
+        // Beyond, several stretches a place even out ragged sequences, against what starting each costs: 15 sqrt(fill), up to 1536 (64 sequences of up to
+        // 16384 keys: 151 us; 154 with 1152, 160 with 2304, 180 with 512).
+        const double fill = static_cast<double>(keys) * blocks / (256 * workgroups_of(p.dim / 32, p.dt == TBN_F32 ? 4 : 2));
+        const double want = fill <= 1024 ? std::fmax(256, fill) : std::fmin(1536, 15 * std::sqrt(fill));
+        chunk = std::max(ceil_div(keys, ceil_div(8192, blocks)), fill <= 1024 ? static_cast<int64_t>(std::ceil(want / 128)) * 128 : static_cast<int64_t>(want / 128 + 0.5) * 128);
         if (keys <= 1024 && blocks >= 256) chunk = keys;   // the join would take longer
     }
     // nor are few keys split, where the join's launch takes longer than the steps it saves (one token, 8 kv heads of 128 channels: 513 keys 7.3 us, 10.7 in
     // parts; 1000 keys 9.2 to 9.7, 1500 11.8 to 10.1; float32 513 keys 9.5 to 10.1, 1000 12.2 to 10.1)
     if (!pl.staged && keys <= (p.dt == TBN_BF16 ? 1024 : 640)) chunk = keys;
+    chunk = ceil_div(keys, ceil_div(keys, chunk));   // of one length (64 sequences of 2000 keys, float32: 47 us, 52 with a short last one)
     chunk = std::min(ceil_div(chunk, 128) * 128, int64_t(kListed) * p.page);
     pl.chunk = static_cast<int>(chunk);
     pl.n_chunks = static_cast<int>(ceil_div(keys, chunk));
