@@ -448,7 +448,8 @@ int padded_dim(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 // Rows of a workgroup of this file's kernel: what the registers hold of queries and sums.  (bfloat16: more rows go to the other kernel.)
 int most_rows(const tbn_kv_pool &p) { return p.dt == TBN_BF16 || padded_dim(p.dim) == 256 ? 16 : padded_dim(p.dim) == 128 ? 32 : 64; }
 
-Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, int64_t unit_step, int64_t unit_most, bool picked) {
+Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, int64_t unit_step, int64_t unit_most, Kind kind) {
+    const bool picked = kind == kPicked;
     // units: keys or picks to split, unit_step: the least stretch, a multiple of which a chunk is
     Plan pl;
     const int64_t places = padded_dim(p.dim) == 256 ? 256 : 512;   // for workgroups at a time: the least of both kernels
@@ -467,7 +468,9 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, 
     const bool few = rows <= 16 && padded_dim(p.dim) == 128 && p.dim > 96 && fill > 256 && !whole && (groups >= places || round);
     pl.staged = !picked && p.dt == TBN_BF16 && (rows > 16 || few);
     if (pl.staged) {
-        pl.rows = rows <= 64 ? 64 : 128;
+        // A window's keys are few, so rows are what fills the places: in tiles of 64 while twice as many find one (8 kv heads of 128 channels, window 1024, 1024 tokens:
+        // 38 us, 51 in tiles of 128 with the keys in two parts; 128 tokens 19.9 to 22.6, 200 tokens 25.5 to 24.1), and unsplit once every CU has one (512 tokens: 30 us, 34 in parts).
+        pl.rows = rows <= 64 || (kind == kWindow && groups * ceil_div(rows, 128) <= places / 2) ? 64 : 128;
     } else {
         pl.rows = 16;
         while (pl.rows < rows && pl.rows < most_rows(p)) pl.rows *= 2;
@@ -481,6 +484,7 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, 
     // 16384 level).  Here many short stretches even them out, against the cost of starting, ending and joining each.
     const int64_t parts = (few && round ? fit : ceil_div(places, blocks)) * (few && groups >= places && units > 4096 ? 2 : 1);
     int64_t chunk = ceil_div(units, pl.staged ? parts : ceil_div(8192, blocks));
+    if (kind == kWindow && pl.staged && blocks >= places / 2) chunk = units;
     if (!picked && !pl.staged) {
         // Beyond 256 keys several stretches a place: with a cost of c keys each and about half a stretch idle at the end, the best length grows
         // as sqrt(2 c fill); c of 32 was measured (34 sequences of up to 3698 keys, float32: 72 us with 256 keys, 97 with 1024; 16 of 16000,
@@ -502,12 +506,12 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, 
     return pl;
 }
 
-Plan tree_plan(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, int64_t keys) {
-    return plan_by_sequences(p, ix, q, keys, [&](int64_t rows, int64_t groups, int64_t units) { return plan_of(p, rows, groups, units, 128, int64_t(kListed) * p.page, false); });
+Plan tree_plan(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, int64_t keys, Kind kind) {
+    return plan_by_sequences(p, ix, q, keys, [&](int64_t rows, int64_t groups, int64_t units) { return plan_of(p, rows, groups, units, 128, int64_t(kListed) * p.page, kind); });
 }
 
 Plan picked_plan(const tbn_kv_pool &p, const KvQueries &q, int32_t n_select) {
-    return plan_of(p, q.heads / p.kv_heads, q.total_q * p.kv_heads, n_select, p.page <= 64 ? 128 / p.page : 1, kListed, true);
+    return plan_of(p, q.heads / p.kv_heads, q.total_q * p.kv_heads, n_select, p.page <= 64 ? 128 / p.page : 1, kListed, kPicked);
 }
 
 template <typename T, int DP, int RT, Kind KIND, bool TOKENS>
@@ -591,16 +595,16 @@ void launch_kv_join(const AttentionArgs &a, Kind kind, int tile_rows, bool token
     else launch_join_typed<uint16_t>(a, kind, tile_rows, tokens, groups, stream);
 }
 
-size_t tree_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q) { return workspace_of(p, q, tree_plan(p, ix, q, q.max_len)); }
+size_t tree_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q) { return workspace_of(p, q, tree_plan(p, ix, q, q.max_len, kAll)); }
 
 tbn_status launch_tree_attention(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, void *out, float *lse, const uint32_t *mask,
                                  int32_t mask_words, float scale, float *ws, hipStream_t stream) {
     AttentionArgs a{p, ix, q, out, lse, mask, mask_words, {nullptr}, 0, factor_of(scale), flip_of(p, scale)};
-    return launch<kAll>(a, tree_plan(p, ix, q, q.max_len), ws, "tbn_tree_attention", stream);
+    return launch<kAll>(a, tree_plan(p, ix, q, q.max_len, kAll), ws, "tbn_tree_attention", stream);
 }
 
 size_t window_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, int32_t n_sink, int32_t window, bool masked) {
-    return workspace_of(p, q, tree_plan(p, ix, q, window_keys(p, q, n_sink, window, masked)));
+    return workspace_of(p, q, tree_plan(p, ix, q, window_keys(p, q, n_sink, window, masked), kWindow));
 }
 
 tbn_status launch_window_attention(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, void *out, float *lse, int32_t n_sink, int32_t window,
@@ -608,7 +612,7 @@ tbn_status launch_window_attention(const tbn_kv_pool &p, const tbn_kv_index &ix,
     AttentionArgs a{p, ix, q, out, lse, mask, mask_words, {nullptr}, 0, factor_of(scale), flip_of(p, scale)};
     a.window.sink = n_sink;
     a.window.size = window;
-    return launch<kWindow>(a, tree_plan(p, ix, q, window_keys(p, q, n_sink, window, mask != nullptr)), ws, "tbn_window_attention", stream);
+    return launch<kWindow>(a, tree_plan(p, ix, q, window_keys(p, q, n_sink, window, mask != nullptr), kWindow), ws, "tbn_window_attention", stream);
 }
 
 size_t block_attention_workspace(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, int32_t n_select) {
