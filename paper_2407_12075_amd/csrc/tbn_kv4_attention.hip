@@ -296,20 +296,22 @@ __global__ __launch_bounds__(kAttnThreads, workgroups_of(NB, sizeof(T))) void kv
 // The queries' view of the cache: sizes as there, the queries' type.
 tbn_kv_pool view_of(const tbn_kv4_pool &p, tbn_dtype dt) { return tbn_kv_pool{p.k, p.v, p.k_exp, reinterpret_cast<float *>(p.v_exp), p.n_pages, p.kv_heads, p.dim, p.page, dt}; }
 
-Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t keys) {
+Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t keys, bool window) {
     Plan pl;
     const int few = shared_rows(p.dim / 32);
     // The kernel that stages keys takes as long for 64 (128) rows as this file's for about 4 (7) tiles of 16, whose last ones ragged drafts often do not
     // need.  16 trees of up to 16 / 24 / 26 / 32 tokens on 4000 keys, 4 heads to a kv head: 40 / 51 / 54 / 55 us, here 44 / 49 / 47 / 65; 12 tokens 38 to 33.  On many
     // keys it is the faster one with fewer (26 tokens on 60000 keys: 56 us, 77 here; 10 tokens level); 512 tokens on 16000: 173 us to 292.
     pl.staged = p.dt == TBN_BF16 && rows > 48 && (rows <= 64 || rows > 112 || keys >= 16384);
-    pl.rows = pl.staged ? (rows <= 64 ? 64 : 128) : rows <= few ? few : 16;
+    const int64_t places = p.dim <= 128 ? 512 : 256;   // for workgroups of the kernel that stages keys
+    pl.rows = pl.staged ? (rows <= 64 || (window && rows_of_64(rows, groups, places)) ? 64 : 128) : rows <= few ? few : 16;
     pl.row_tiles = static_cast<int>(ceil_div(rows, pl.rows));
     const int64_t blocks = groups * pl.row_tiles;
     int64_t chunk;
     if (pl.staged) {
         // one round of the places for workgroups (512 tokens on 16000 keys: 173 us, 183 in two, 191 in four)
-        chunk = std::max<int64_t>(std::min<int64_t>(256, keys), ceil_div(keys, ceil_div(p.dim <= 128 ? 512 : 256, blocks)));
+        chunk = std::max<int64_t>(std::min<int64_t>(256, keys), ceil_div(keys, ceil_div(places, blocks)));
+        if (window && blocks >= places / 2) chunk = keys;   // 1024 tokens, window 1024: 43 us, 54 in parts
     } else {
         // fill: keys of each place for a workgroup.  Up to 1024 one round of the places, 256 keys at least (bfloat16, 128 channels, 8 kv heads: 16 sequences of
         // 3000 keys 15.6 us with 512, 17.6 with 384, 18.5 with 256; one of 8000 keys 10.3 with 256, 12.5 with 128; one of 60000 keys 20 - 21 with 768 - 1024, 23.6 with 384).
@@ -332,7 +334,7 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t keys) {
 
 Plan plan_of_call(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQueries &q, int32_t n_sink, int32_t window, bool masked) {
     const int64_t keys = window ? window_keys(p, q, n_sink, window, masked) : q.max_len;
-    return plan_by_sequences(p, ix, q, keys, [&](int64_t rows, int64_t groups, int64_t units) { return plan_of(p, rows, groups, units); });
+    return plan_by_sequences(p, ix, q, keys, [&](int64_t rows, int64_t groups, int64_t units) { return plan_of(p, rows, groups, units, window != 0); });
 }
 
 template <int NB, typename T, Kind KIND, bool FEW>

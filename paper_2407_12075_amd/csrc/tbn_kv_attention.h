@@ -344,6 +344,13 @@ Plan plan_by_sequences(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQue
     }
 }
 
+// Whether the rows of a call with a window are taken in tiles of 64 although they are more.  Its keys are few, so rows are what fills the places: where tiles of
+// 128 would leave half of them empty, and those of 64 give every CU one (8 kv heads of 128 channels, window 1024, 1024 tokens: 38 us, 51 in tiles of 128 with the
+// keys in two parts; on the cache in 4 bits 43, 54).  With fewer rows the keys are split in any case (300 tokens, window 4096: 54 us, in tiles of 128 52; in 4 bits 63, 54).
+inline bool rows_of_64(int64_t rows, int64_t groups, int64_t places) {
+    return groups * ceil_div(rows, 128) <= places / 2 && groups * ceil_div(rows, 64) >= places / 2;
+}
+
 // Keys that a workgroup of `rows` rows at most goes through in a call with a window, at most: the first pages, the window of its first row and
 // what its other rows add.
 inline int64_t window_keys(const tbn_kv_pool &p, const KvQueries &q, int32_t n_sink, int32_t window, bool masked, int rows = 128) {
