@@ -304,14 +304,14 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t keys, b
     // keys it is the faster one with fewer (26 tokens on 60000 keys: 56 us, 77 here; 10 tokens level); 512 tokens on 16000: 173 us to 292.
     pl.staged = p.dt == TBN_BF16 && rows > 48 && (rows <= 64 || rows > 112 || keys >= 16384);
     const int64_t places = p.dim <= 128 ? 512 : 256;   // for workgroups of the kernel that stages keys
-    pl.rows = pl.staged ? (rows <= 64 || (window && rows_of_64(rows, groups, places)) ? 64 : 128) : rows <= few ? few : 16;
+    pl.rows = pl.staged ? (rows <= 64 || (window && rows_of_64(rows, groups, keys, places)) ? 64 : 128) : rows <= few ? few : 16;
     pl.row_tiles = static_cast<int>(ceil_div(rows, pl.rows));
     const int64_t blocks = groups * pl.row_tiles;
     int64_t chunk;
     if (pl.staged) {
         // one round of the places for workgroups (512 tokens on 16000 keys: 173 us, 183 in two, 191 in four)
         chunk = std::max<int64_t>(std::min<int64_t>(256, keys), ceil_div(keys, ceil_div(places, blocks)));
-        if (window && blocks >= places / 2) chunk = keys;   // 1024 tokens, window 1024: 43 us, 54 in parts
+        if (window && keys <= kFewKeys && blocks >= places / 2) chunk = keys;   // 1024 tokens, window 1024: 43 us, 54 in parts
     } else {
         // fill: keys of each place for a workgroup.  Up to 1024 one round of the places, 256 keys at least (bfloat16, 128 channels, 8 kv heads: 16 sequences of
         // 3000 keys 15.6 us with 512, 17.6 with 384, 18.5 with 256; one of 8000 keys 10.3 with 256, 12.5 with 128; one of 60000 keys 20 - 21 with 768 - 1024, 23.6 with 384).

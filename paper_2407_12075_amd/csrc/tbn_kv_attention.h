@@ -344,11 +344,15 @@ Plan plan_by_sequences(const tbn_kv_pool &p, const tbn_kv_index &ix, const KvQue
     }
 }
 
+// Keys of a window up to which rows alone are spread over the places: 8 kv heads of 128 channels, 1024 tokens, in tiles of 64 and unsplit against 128 and in parts: window
+// 4000 94 us, 98; 8000 167, 162 (700 tokens: 146, 164); 16000 315, 289.
+constexpr int64_t kFewKeys = 10240;
+
 // Whether the rows of a call with a window are taken in tiles of 64 although they are more.  Its keys are few, so rows are what fills the places: where tiles of
 // 128 would leave half of them empty, and those of 64 give every CU one (8 kv heads of 128 channels, window 1024, 1024 tokens: 38 us, 51 in tiles of 128 with the
 // keys in two parts; on the cache in 4 bits 43, 54).  With fewer rows the keys are split in any case (300 tokens, window 4096: 54 us, in tiles of 128 52; in 4 bits 63, 54).
-inline bool rows_of_64(int64_t rows, int64_t groups, int64_t places) {
-    return groups * ceil_div(rows, 128) <= places / 2 && groups * ceil_div(rows, 64) >= places / 2;
+inline bool rows_of_64(int64_t rows, int64_t groups, int64_t keys, int64_t places) {
+    return keys <= kFewKeys && groups * ceil_div(rows, 128) <= places / 2 && groups * ceil_div(rows, 64) >= places / 2;
 }
 
 // Keys that a workgroup of `rows` rows at most goes through in a call with a window, at most: the first pages, the window of its first row and

@@ -468,7 +468,7 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, 
     const bool few = rows <= 16 && padded_dim(p.dim) == 128 && p.dim > 96 && fill > 256 && !whole && (groups >= places || round);
     pl.staged = !picked && p.dt == TBN_BF16 && (rows > 16 || few);
     if (pl.staged) {
-        pl.rows = rows <= 64 || (kind == kWindow && rows_of_64(rows, groups, places)) ? 64 : 128;
+        pl.rows = rows <= 64 || (kind == kWindow && rows_of_64(rows, groups, units, places)) ? 64 : 128;
     } else {
         pl.rows = 16;
         while (pl.rows < rows && pl.rows < most_rows(p)) pl.rows *= 2;
@@ -482,7 +482,9 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, 
     // 16384 level).  Here many short stretches even them out, against the cost of starting, ending and joining each.
     const int64_t parts = (few && round ? fit : ceil_div(places, blocks)) * (few && groups >= places && units > 4096 ? 2 : 1);
     int64_t chunk = ceil_div(units, pl.staged ? parts : ceil_div(8192, blocks));
-    if (kind == kWindow && pl.staged && blocks >= places / 2) chunk = units;   // 512 tokens, window 1024: 30 us, 34 in parts
+    // Windows are of one length: 512 tokens, window 1024: 30 us, 34 in parts; one token each of 64 sequences, window 4096, which fill a round: 190 us, 195 in two (of 80
+    // sequences: 276, 248).
+    if (kind == kWindow && pl.staged && units <= kFewKeys && (few ? round && fit == 1 : blocks >= places / 2)) chunk = units;
     if (!picked && !pl.staged) {
         // Beyond 256 keys several stretches a place: with a cost of c keys each and about half a stretch idle at the end, the best length grows
         // as sqrt(2 c fill); c of 32 was measured (34 sequences of up to 3698 keys, float32: 72 us with 256 keys, 97 with 1024; 16 of 16000,
