@@ -143,3 +143,32 @@ def test_binding_refuses_host_tensors():
     i = z(3, dtype=torch.int32)
     with pytest.raises(ValueError):
         kv.tbn_verify(z(2, 5), i, z(2), i, 2)
+
+
+def rows_and_parts(lib, kind, T, window, n_seqs=1, heads=32, dim=128):  # noqa: F811
+    """Stretches that a call's keys are split into, from the bytes of the workspace (0: not split)."""
+    big = dict(n_pages=1 << 20, kv_heads=8, dim=dim, page=64)
+    pool, index = structs(**{f"pool_{k}": v for k, v in big.items()}, pool_dt=1, index_page=64, index_n_pages=1 << 20, index_n_seqs=n_seqs, index_max_pages=2048)
+    total = T * n_seqs
+    if kind == "window":
+        need = lib.tbn_window_attention_workspace_bytes(at(pool), at(index), total, T, heads, 4, window, 0, 20000)
+    else:
+        need = lib.tbn_kv4_attention_workspace_bytes(at(pool4(**big)), at(index), 1, total, T, heads, 4, window, 0, 20000)
+    assert need % (total * heads * (dim + 4) * 4) == 0
+    return need // (total * heads * (dim + 4) * 4)
+
+
+def test_prompts_with_a_window_are_not_split(lib):  # noqa: F811
+    """Rows fill the places: few keys stay whole once every CU has a tile of rows, many are split all the same."""
+    for kind in ("window", "four"):
+        assert [rows_and_parts(lib, kind, T, 1024) for T in (512, 700, 1024, 2048)] == [0] * 4
+        assert rows_and_parts(lib, kind, 128, 4000) > 1 and rows_and_parts(lib, kind, 700, 16000) > 1
+    # single tokens: one round of whole windows, two stretches beyond
+    assert rows_and_parts(lib, "window", 1, 4096, n_seqs=64) == 0 and rows_and_parts(lib, "window", 1, 8000, n_seqs=80) == 2
+
+
+def test_stretches_of_the_cache_in_4_bits(lib):  # noqa: F811
+    """Short histories whole; one round of the places up to 1024 keys each; many sequences in stretches of about 1500 keys."""
+    assert rows_and_parts(lib, "four", 1, 700) == 0
+    assert 20 <= rows_and_parts(lib, "four", 1, 0) <= 96
+    assert 11 <= rows_and_parts(lib, "four", 1, 0, n_seqs=64) <= 15
