@@ -52,14 +52,16 @@ template <> struct Query<float> {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             float lo = __uint_as_float(there ? w[e / 2][2 * (e & 1)] ^ flip : 0u), hi = __uint_as_float(there ? w[e / 2][2 * (e & 1) + 1] ^ flip : 0u);
-            // a number that is not finite stays what it is in the first term (less itself it would be none in the others)
+            // The first terms are cut, not rounded: the nearest bfloat16 to the largest numbers is infinite, and the 16 bits left fill two more.  A number that
+            // is not finite stays what it is in the first term (less itself it would be none in the others).
             const bool fl = fabsf(lo) < INFINITY, fh = fabsf(hi) < INFINITY;
-#pragma unroll
-            for (int t = 0; t < 3; ++t) {
-                q[t][e] = split_off(lo, hi);
-                lo = fl ? lo : 0.f;
-                hi = fh ? hi : 0.f;
-            }
+            const uint32_t first = two_bf16(lo, hi);
+            const uint32_t l = fl ? __float_as_uint(lo) >> 16 : first & 0xffffu, h = fh ? __float_as_uint(hi) & 0xffff0000u : first & 0xffff0000u;
+            q[0][e] = l | h;
+            lo = fl ? lo - __uint_as_float(l << 16) : 0.f;
+            hi = fh ? hi - __uint_as_float(h) : 0.f;
+            q[1][e] = split_off(lo, hi);
+            q[2][e] = split_off(lo, hi);
         }
     }
 };

@@ -91,3 +91,20 @@ def some(qs, keys, values, counts, sink, window, scale, take):
         o, l = reference(qs[t:t + 1], [keys[s][:n]], [values[s][:n]], [1], sink, window, None, scale)
         out[i], lse[i] = o[0], l[0]
     return out, lse
+
+
+@pytest.mark.parametrize("rows", [1, 12])
+def test_largest_float32_queries(kv, rows):
+    """Queries whose nearest bfloat16 number is infinite, on keys so small that the logits are of ordinary size."""
+    H, KV, D, lens = 2, 1, 128, [200, 65]
+    pool, index, keys, values = make_cache4(kv, KV, D, 32, lens, seed=4)
+    pool.k_exp -= 98
+    keys = [k * 2.0 ** -98 for k in keys]
+    rng = np.random.RandomState(5)
+    q = torch.from_numpy((rng.uniform(3.3962e38, 3.4028e38, (2 * rows, H, D)) * rng.choice([-1, 1], (2 * rows, H, D))).astype(np.float32))
+    q[0] = torch.finfo(torch.float32).max
+    assert q.isfinite().all() and q.to(torch.bfloat16).isinf().all()
+    cu = torch.tensor([0, rows, 2 * rows], dtype=torch.int32, device="cuda")
+    scale = 2.0 ** -30 / math.sqrt(D)
+    out, lse = kv.tbn_kv4_attention(q.cuda(), pool, index, cu, rows, scale=scale)
+    compare(out, lse, *reference(q.double().numpy(), keys, values, [rows] * 2, 0, 1 << 30, None, scale), tolerance("f32", values))
