@@ -31,6 +31,9 @@ __device__ __forceinline__ f32x16_t mma(u32x4_t a, u32x4_t b, f32x16_t c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
 
+// Every wave has done its accesses to LDS.  Loads into it may still be on their way, which __syncthreads would wait for.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 // key of row r of a tile of 32: the instruction's output register 4 i + j of a lane of half h is row 8 i + 4 h + j
 __device__ __forceinline__ int key_of_row(int r) { return 16 * (r >> 4) + 8 * ((r >> 2) & 1) + 4 * ((r >> 3) & 1) + (r & 3); }
 
@@ -48,6 +51,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
     __shared__ __attribute__((aligned(16))) uint16_t k0[KEYS * PITCH], k1[KEYS * PITCH], v0[DP * KEYS], v1[DP * KEYS];
     __shared__ int listed[kListed];
     __shared__ float4 halves[RW][32];
+    __shared__ int odd_seen;   // with a window: whether a step that not every row sees all of has a value that is not finite
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
     const int s = sequence_of<TOKENS>(a);
@@ -198,15 +202,29 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
             }
         if (edge) {   // values behind the last key become 0; are the others finite?
             bool odd = false;
-#pragma unroll 1
-            for (int L = tid; L < DP * VP; L += kAttnThreads) {
-                const int d = L / VP, there = stop - (key + ((L % VP) ^ v_swap(d)) * 8);
-                u32x4_t *at_piece = reinterpret_cast<u32x4_t *>(vt + L * 8);
-                const u32x4_t w = Elem<uint16_t>::first_of(*at_piece, there);
+            auto check = [&](int L, u32x4_t w) {
+                const int there = stop - (key + ((L % VP) ^ v_swap(L / VP)) * 8);
+                w = Elem<uint16_t>::first_of(w, there);
                 odd |= Elem<uint16_t>::not_finite(w);
-                if (there < 8) *at_piece = w;
+                if (there < 8) *reinterpret_cast<u32x4_t *>(vt + L * 8) = w;
+            };
+            // With a window five steps of a tile's 19 come here (1024 keys, tiles of 32 tokens), so all pieces are asked for at once, and the next step's loads are not
+            // waited for (two chunks of up to 2048 tokens: 114 us, 118 as below).  Elsewhere one or two do (16 trees of up to 26 tokens: 55.5 us, 54.3 - 55.3).
+            if constexpr (WINDOW) {
+                u32x4_t w[NV];
+#pragma unroll
+                for (int j = 0; j < NV; ++j) w[j] = *reinterpret_cast<const u32x4_t *>(vt + (tid + j * kAttnThreads) * 8);
+#pragma unroll
+                for (int j = 0; j < NV; ++j) check(tid + j * kAttnThreads, w[j]);
+                if (odd) odd_seen = 1;
+                lds_barrier();
+                odd = __builtin_amdgcn_readfirstlane(odd_seen);
+            } else {
+#pragma unroll 1
+                for (int L = tid; L < DP * VP; L += kAttnThreads) check(L, *reinterpret_cast<const u32x4_t *>(vt + L * 8));
+                odd = __syncthreads_or(odd);
             }
-            if (__syncthreads_or(odd)) {   // rare: what they add to the rows that see them, then 0 in their place
+            if (odd) {   // rare: what they add to the rows that see them, then 0 in their place
 #pragma unroll 1
                 for (int u = 0; u < 2 * TILES; ++u) {
                     const int c = (KW > 1 ? half * 4 : 0) + 2 * u + h;
@@ -226,6 +244,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
                     }
                 }
                 __syncthreads();
+                if (WINDOW && tid == 0) odd_seen = 0;   // read by all
 #pragma unroll 1
                 for (int L = tid; L < DP * VP; L += kAttnThreads) {
                     u32x4_t *at_piece = reinterpret_cast<u32x4_t *>(vt + L * 8);
@@ -256,6 +275,7 @@ __global__ __launch_bounds__(kAttnThreads, DP == 256 ? 1 : 2) void kv_rows_kerne
         __builtin_amdgcn_s_setprio(0);
     };
 
+    if (WINDOW && tid == 0) odd_seen = 0;
     __syncthreads();
     const int steps = (stop - first + KEYS - 1) / KEYS;
     if (steps > 0) {
