@@ -482,7 +482,7 @@ Plan plan_of(const tbn_kv_pool &p, int64_t rows, int64_t groups, int64_t units, 
     // 16384 level).  Here many short stretches even them out, against the cost of starting, ending and joining each.
     const int64_t parts = (few && round ? fit : ceil_div(places, blocks)) * (few && groups >= places && units > 4096 ? 2 : 1);
     int64_t chunk = ceil_div(units, pl.staged ? parts : ceil_div(8192, blocks));
-    // Windows are of one length: 512 tokens, window 1024: 30 us, 34 in parts; one token each of 64 sequences, window 4096, which fill a round: 190 us, 195 in two (of 80
+    // Windows are of one length: 512 tokens, window 1024: 29 us, 34 in parts; one token each of 64 sequences, window 4096, which fill a round: 190 us, 195 in two (of 80
     // sequences: 276, 248).
     if (kind == kWindow && pl.staged && units <= kFewKeys && (few ? round && fit == 1 : blocks >= places / 2)) chunk = units;
     if (!picked && !pl.staged) {
