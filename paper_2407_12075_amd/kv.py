@@ -156,6 +156,13 @@ def _rows(t: torch.Tensor, name: str, heads: int, dim: int, like) -> Tuple[int, 
     return t.data_ptr(), st[0] if n > 1 else heads * dim
 
 
+def _of(kind: type, x, name: str) -> None:
+    """Refuses what is not of the class that a call is for: the structs have one size, and the library would take a byte of one pool for an element of the
+    other.  (A call comes here where the type is not the very one.)"""
+    if not isinstance(x, kind):
+        raise ValueError(f"{name} must be a {kind.__name__}, got {type(x).__name__}")
+
+
 def _agree(pool, index: KVIndex):
     if pool.device != index.device:
         raise ValueError(f"pool and index must live on one device, got {pool.device} and {index.device}")
@@ -183,6 +190,8 @@ def _done(st: int):
 
 def tbn_kv_reserve(index: KVIndex, n_new: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Room for n_new[s] more keys of each sequence; returns the pairs of pages (-1: none) for tbn_kv_copy_pages."""
+    if type(index) is not KVIndex:
+        _of(KVIndex, index, "index")
     if _plain(workspace, stream):
         r = tbn._host.kv_reserve(index._at, index._gpu, n_new)
         if r is not None:
@@ -196,6 +205,8 @@ def tbn_kv_reserve(index: KVIndex, n_new: torch.Tensor, workspace: Optional[torc
 
 def tbn_kv_fork(index: KVIndex, parents: torch.Tensor, children: torch.Tensor, stream=None) -> None:
     """Sequence children[i], which is empty, shares the pages of parents[i]."""
+    if type(index) is not KVIndex:
+        _of(KVIndex, index, "index")
     if _plain(stream) and tbn._host.kv_fork(index._at, index._gpu, parents, children):
         return
     n = parents.numel()
@@ -206,6 +217,8 @@ def tbn_kv_fork(index: KVIndex, parents: torch.Tensor, children: torch.Tensor, s
 
 def tbn_kv_release(index: KVIndex, keep: torch.Tensor, stream=None) -> None:
     """Sequence s keeps its first keep[s] keys at most and gives back the pages behind them."""
+    if type(index) is not KVIndex:
+        _of(KVIndex, index, "index")
     if _plain(stream) and tbn._host.kv_release(index._at, index._gpu, keep):
         return
     _done(_call("tbn_kv_release", index._at, _ints(keep, "keep", index.n_seqs, index.device), _stream(stream)))
@@ -213,6 +226,8 @@ def tbn_kv_release(index: KVIndex, keep: torch.Tensor, stream=None) -> None:
 
 def tbn_kv_compact(index: KVIndex, workspace: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """Used pages go to the lowest numbers; returns (src, dst, count) for tbn_kv_copy_pages."""
+    if type(index) is not KVIndex:
+        _of(KVIndex, index, "index")
     half = max(index.n_pages // 2, 1)
     moves = _empty(2 * half + 1, torch.int32, index.device, stream)
     ws, size = _workspace(index._ws, workspace, index.device, stream)
@@ -223,6 +238,8 @@ def tbn_kv_compact(index: KVIndex, workspace: Optional[torch.Tensor] = None, str
 
 def tbn_kv_copy_pages(pool: KVPool, src: torch.Tensor, dst: torch.Tensor, count: Optional[torch.Tensor] = None, stream=None) -> None:
     """Copies page src[i] to page dst[i], of the first count pairs if count is given; pairs with -1 are left out."""
+    if type(pool) is not KVPool:
+        _of(KVPool, pool, "pool")
     if _plain(stream) and tbn._host.kv_copy_pages(pool._at, pool._gpu, src, dst, count):
         return
     n = src.numel()
@@ -234,6 +251,8 @@ def tbn_kv_copy_pages(pool: KVPool, src: torch.Tensor, dst: torch.Tensor, count:
 
 def tbn_kv_append(pool: KVPool, index: KVIndex, k_new: torch.Tensor, v_new: torch.Tensor, cu_new: torch.Tensor, max_new: int, stream=None) -> None:
     """Keys and values (tokens, kv_heads, dim) become the last cu_new[s + 1] - cu_new[s] <= max_new of each sequence."""
+    if type(pool) is not KVPool or type(index) is not KVIndex:
+        _of(KVPool, pool, "pool"), _of(KVIndex, index, "index")
     if _plain(stream) and tbn._host.kv_append(pool._at, pool._gpu, index._at, index._gpu, k_new, v_new, cu_new, max_new):
         return
     _agree(pool, index)
@@ -246,6 +265,8 @@ def tbn_kv_append(pool: KVPool, index: KVIndex, k_new: torch.Tensor, v_new: torc
 
 def tbn_kv_keep(pool: KVPool, index: KVIndex, base: torch.Tensor, picks: torch.Tensor, counts: torch.Tensor, stream=None) -> None:
     """Key base[s] + picks[s, j] moves to base[s] + j for j < counts[s] (picks ascend)."""
+    if type(pool) is not KVPool or type(index) is not KVIndex:
+        _of(KVPool, pool, "pool"), _of(KVIndex, index, "index")
     if _plain(stream) and tbn._host.kv_keep(pool._at, pool._gpu, index._at, index._gpu, base, picks, counts):
         return
     _agree(pool, index)
@@ -276,6 +297,8 @@ def _outputs(q: torch.Tensor, out: Optional[torch.Tensor], lse: Optional[torch.T
 
 
 def tbn_tree_attention_workspace_bytes(q: torch.Tensor, pool: KVPool, index: KVIndex, max_q: int, max_len: int = 0) -> int:
+    if type(pool) is not KVPool or type(index) is not KVIndex:
+        _of(KVPool, pool, "pool"), _of(KVIndex, index, "index")
     return int(lib().tbn_tree_attention_workspace_bytes(pool._at, index._at, q.shape[0], max_q, q.shape[1], max_len))
 
 
@@ -284,6 +307,8 @@ def tbn_tree_attention(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: torc
                        lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Queries q (tokens, heads, dim) of each sequence's last keys against its cache; mask int32 (tokens, words): bit j of a row
     is set where the token sees the sequence's j-th query token (None: its own and the earlier ones).  Returns (out, lse)."""
+    if type(pool) is not KVPool or type(index) is not KVIndex:
+        _of(KVPool, pool, "pool"), _of(KVIndex, index, "index")
     if _plain(out, lse, workspace, stream):
         r = tbn._host.tree_attention(q, pool._at, pool._gpu, index._at, index._gpu, cu_q, max_q, max_len, mask, scale)
         if r is not None:
@@ -316,6 +341,8 @@ def _mask(mask: Optional[torch.Tensor], q: torch.Tensor):
 
 def tbn_window_attention_workspace_bytes(q: torch.Tensor, pool: KVPool, index: KVIndex, max_q: int, n_sink: int, window: int, masked: bool = False,
                                          max_len: int = 0) -> int:
+    if type(pool) is not KVPool or type(index) is not KVIndex:
+        _of(KVPool, pool, "pool"), _of(KVIndex, index, "index")
     return int(lib().tbn_window_attention_workspace_bytes(pool._at, index._at, q.shape[0], max_q, q.shape[1], n_sink, window, int(masked), max_len))
 
 
@@ -325,6 +352,8 @@ def tbn_window_attention(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: to
                          stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """tbn_tree_attention over the sequence's first n_sink keys and the last `window` keys up to the token's own (with a mask: up to its place
     in the tree; then max_q <= window).  Returns (out, lse)."""
+    if type(pool) is not KVPool or type(index) is not KVIndex:
+        _of(KVPool, pool, "pool"), _of(KVIndex, index, "index")
     if _plain(out, lse, workspace, stream):
         r = tbn._host.window_attention(q, pool._at, pool._gpu, index._at, index._gpu, cu_q, max_q, max_len, mask, scale, n_sink, window)
         if r is not None:
@@ -340,6 +369,8 @@ def tbn_window_attention(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: to
 
 
 def tbn_block_select_workspace_bytes(q: torch.Tensor, pool: KVPool, index: KVIndex, max_q: int, max_len: int = 0) -> int:
+    if type(pool) is not KVPool or type(index) is not KVIndex:
+        _of(KVPool, pool, "pool"), _of(KVIndex, index, "index")
     return int(lib().tbn_block_select_workspace_bytes(pool._at, index._at, q.shape[0], max_q, q.shape[1], max_len))
 
 
@@ -347,6 +378,8 @@ def tbn_block_select(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: torch.
                      max_len: Optional[int] = None, picks: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                      stream=None) -> torch.Tensor:
     """Per query and kv head n_select of its sequence's pages: int32 (tokens, kv_heads, n_select), ascending, -1 behind the last."""
+    if type(pool) is not KVPool or type(index) is not KVIndex:
+        _of(KVPool, pool, "pool"), _of(KVIndex, index, "index")
     if _plain(picks, workspace, stream):
         r = tbn._host.block_select(q, pool._at, pool._gpu, index._at, index._gpu, cu_q, max_q, max_len, n_select, n_sink, n_recent)
         if r is not None:
@@ -365,6 +398,8 @@ def tbn_block_select(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: torch.
 
 
 def tbn_block_attention_workspace_bytes(q: torch.Tensor, pool: KVPool, index: KVIndex, max_q: int, n_select: int) -> int:
+    if type(pool) is not KVPool or type(index) is not KVIndex:
+        _of(KVPool, pool, "pool"), _of(KVIndex, index, "index")
     return int(lib().tbn_block_attention_workspace_bytes(pool._at, index._at, q.shape[0], max_q, q.shape[1], n_select))
 
 
@@ -372,6 +407,8 @@ def tbn_block_attention(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: tor
                         out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                         stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """tbn_tree_attention without a mask over the keys of the picked pages only.  Returns (out, lse)."""
+    if type(pool) is not KVPool or type(index) is not KVIndex:
+        _of(KVPool, pool, "pool"), _of(KVIndex, index, "index")
     if _plain(out, lse, workspace, stream):
         r = tbn._host.block_attention(q, pool._at, pool._gpu, index._at, index._gpu, cu_q, max_q, None, picks, scale)
         if r is not None:
@@ -391,6 +428,8 @@ def tbn_block_attention(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: tor
 
 def tbn_kv4_append(pool: KV4Pool, index: KVIndex, k_new: torch.Tensor, v_new: torch.Tensor, cu_new: torch.Tensor, max_new: int, stream=None) -> None:
     """tbn_kv_append into a pool in 4 bits; k_new and v_new float32 or bfloat16."""
+    if type(pool) is not KV4Pool or type(index) is not KVIndex:
+        _of(KV4Pool, pool, "pool"), _of(KVIndex, index, "index")
     if _plain(stream) and tbn._host.kv4_append(pool._at, pool._gpu, index._at, index._gpu, k_new, v_new, cu_new, max_new):
         return
     _agree(pool, index)
@@ -406,6 +445,8 @@ def tbn_kv4_read(pool: KV4Pool, index: KVIndex, cu: torch.Tensor, max_n: int, to
                  stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """The last cu[s + 1] - cu[s] <= max_n keys and values of each sequence, (total, kv_heads, dim) each, as the numbers they stand for (rows of
     a sequence that has fewer keys are undefined)."""
+    if type(pool) is not KV4Pool or type(index) is not KVIndex:
+        _of(KV4Pool, pool, "pool"), _of(KVIndex, index, "index")
     if dtype not in (torch.float32, torch.bfloat16):
         raise ValueError("dtype must be float32 or bfloat16")
     if _plain(stream):
@@ -420,6 +461,8 @@ def tbn_kv4_read(pool: KV4Pool, index: KVIndex, cu: torch.Tensor, max_n: int, to
 
 def tbn_kv4_copy_pages(pool: KV4Pool, src: torch.Tensor, dst: torch.Tensor, count: Optional[torch.Tensor] = None, stream=None) -> None:
     """tbn_kv_copy_pages of a pool in 4 bits."""
+    if type(pool) is not KV4Pool:
+        _of(KV4Pool, pool, "pool")
     if _plain(stream) and tbn._host.kv4_copy_pages(pool._at, pool._gpu, src, dst, count):
         return
     n = src.numel()
@@ -431,6 +474,8 @@ def tbn_kv4_copy_pages(pool: KV4Pool, src: torch.Tensor, dst: torch.Tensor, coun
 
 def tbn_kv4_keep(pool: KV4Pool, index: KVIndex, base: torch.Tensor, picks: torch.Tensor, counts: torch.Tensor, stream=None) -> None:
     """tbn_kv_keep of a pool in 4 bits."""
+    if type(pool) is not KV4Pool or type(index) is not KVIndex:
+        _of(KV4Pool, pool, "pool"), _of(KVIndex, index, "index")
     if _plain(stream) and tbn._host.kv4_keep(pool._at, pool._gpu, index._at, index._gpu, base, picks, counts):
         return
     _agree(pool, index)
@@ -442,6 +487,8 @@ def tbn_kv4_keep(pool: KV4Pool, index: KVIndex, base: torch.Tensor, picks: torch
 
 def tbn_kv4_attention_workspace_bytes(q: torch.Tensor, pool: KV4Pool, index: KVIndex, max_q: int, n_sink: int = 0, window: int = 0, masked: bool = False,
                                       max_len: int = 0) -> int:
+    if type(pool) is not KV4Pool or type(index) is not KVIndex:
+        _of(KV4Pool, pool, "pool"), _of(KVIndex, index, "index")
     return int(lib().tbn_kv4_attention_workspace_bytes(pool._at, index._at, _dt(q), q.shape[0], max_q, q.shape[1], n_sink, window, int(masked), max_len))
 
 
@@ -450,6 +497,8 @@ def tbn_kv4_attention(q: torch.Tensor, pool: KV4Pool, index: KVIndex, cu_q: torc
                       out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                       stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """tbn_tree_attention over a pool in 4 bits, with window > 0 tbn_window_attention; q float32 or bfloat16.  Returns (out, lse)."""
+    if type(pool) is not KV4Pool or type(index) is not KVIndex:
+        _of(KV4Pool, pool, "pool"), _of(KVIndex, index, "index")
     if _plain(out, lse, workspace, stream):
         r = tbn._host.kv4_attention(q, pool._at, pool._gpu, index._at, index._gpu, cu_q, max_q, max_len, mask, scale, n_sink, window)
         if r is not None:
