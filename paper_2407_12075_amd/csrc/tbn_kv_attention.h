@@ -205,14 +205,15 @@ __device__ __forceinline__ int keys_end(const AttentionArgs &a, const Span &v, i
 }
 
 // The keys that the rows [row0, row1] of a call with a window can see, as pages without a gap: the pages of the first keys, then those
-// from the first row's window on.  "Within" counts keys along them; `gap` keys are left out behind the first `head` of them.
+// from the first row's window on.  "Within" counts keys along them; `gap` keys are left out behind the first `head` of them.  No more than a plan has
+// stretches for (window_keys): with a mask keys of tokens beyond max_q, which the caller says there are none of, are left out.
 struct Within {
     int head, gap, end, low;   // keys of the first pages, keys left out, keys in all, the least key of the first row's window
     __device__ __forceinline__ int key(int x) const { return x < head ? x : x + gap; }
 };
 
 __device__ __forceinline__ Within within_of(const AttentionArgs &a, const Span &v, int row0, int row1, int G, int shift) {
-    const int end = keys_end(a, v, row1, G), pages = (end + a.p.page - 1) >> shift;
+    const int end = min(keys_end(a, v, row1, G), v.prefix + v.T), pages = (end + a.p.page - 1) >> shift;
     Within w;
     // with a mask a row's place is what it has above it, none at least
     w.low = max((a.mask ? v.prefix - 1 : v.prefix + row0 / G) - a.window.size + 1, 0);

@@ -369,7 +369,7 @@ __global__ __launch_bounds__(kAttnThreads) void kv_join_kernel(AttentionArgs a, 
     if (KIND != kPicked) {
         const int r = t * G + h % G, base = r / tile_rows * tile_rows, last = min(base + tile_rows, v.T * G) - 1;
         const int end = KIND == kWindow ? within_of(a, v, base, last, G, __ffs(a.p.page) - 1).end : keys_end(a, v, last, G);
-        parts = max(1, (end + a.chunk - 1) / a.chunk);
+        parts = min(max(1, (end + a.chunk - 1) / a.chunk), a.n_chunks);
     }
     const int64_t at = int64_t(v.t0 + t) * H + h, stride = a.q.total_q * H;
     const int shift = D <= 64 ? 4 : D <= 128 ? 5 : 6, group = tid >> shift, groups = kTeam >> shift, d = (tid & ((1 << shift) - 1)) * 4;
