@@ -610,6 +610,8 @@ tbn_status tbn_block_attention(const void *q, int64_t q_stride, void *out, float
  *   picks         : DEVICE, n_seqs x max_q: the accepted places, 0 first, ascending, -1 behind the last (what tbn_kv_keep takes)
  *   counts, next  : DEVICE, n_seqs: accepted places (1 at least; 0 for a sequence without tokens), the token that follows (there -1)
  *   workspace     : DEVICE, 16-byte aligned, the bytes of the query (may be 0)
+ * With a draft each refused token that another one hangs beside costs a pass of one workgroup over a row, however many were refused before it (2047 of them on a
+ * vocabulary of 131072: 0.23 s).
  * Errors: TBN_ERR_NULL, TBN_ERR_SHAPE, TBN_ERR_UNSUPPORTED, TBN_ERR_WORKSPACE, TBN_ERR_DEVICE.
  */
 size_t tbn_verify_workspace_bytes(int64_t total_q, int32_t max_q, int32_t n_seqs, int64_t vocab);

@@ -11,6 +11,10 @@
 // token was refused and another one hangs on the same (with a draft), and at the end.  What bounds it is the latency of a handful of dependent
 // loads and, for many sequences with large vocabularies, the bytes of the last rows: there slices of a row are summed by many workgroups, each of which
 // walks the path for itself, and a second launch finds the slice and the token in it.
+//
+// What is left of a row is made from the target's again wherever it is needed, by the refusals in their order.  Those of many siblings would be applied again for
+// each of them, so every kKept refusals the sum of the row leaves it in the workspace, in binary64 (the same numbers, therefore), and the next ones go on from there:
+// a refusal costs one pass over the row, however many there were before.
 #include <algorithm>
 
 #include "tbn_kv.h"
@@ -18,6 +22,10 @@
 namespace tbn {
 
 namespace {
+
+// Without the draft's probabilities; with them; with them where sequences have tokens enough for rows to be kept.  (Instances of their own: where no row can be kept
+// the branches would cost 16 trees of 10 tokens on 50000 elements 3 us of 29.)
+enum Draft { kNoDraft, kDraft, kKeeping };
 
 constexpr int kBig = 1024, kSmall = 256;   // threads of a workgroup
 constexpr int kSlice = 4096;
@@ -37,22 +45,32 @@ struct VerifyArgs {
     int2 *ends;       // row of the target (-1: no tokens), refused ones
     double *refused;  // (sequence, max_q): m with a draft, else the token
     int32_t slices;
+    double *left;     // rows that kKept refusals and more have left (left_row)
 };
 
-// What is left of a row of the target.
+// Refusals at one token after which what is left is kept: 2047 siblings on 131072 elements take 226 ms (130 with 32), but trees of up to 65 tokens keep the faster
+// instances (4 trees of 48 tokens on 32000 elements: 28.4 us, 30.4 with 32).  A row that is kept belongs to a sequence of kKept + 2 tokens at least, so the rows are
+// few: an eight-byte number for 66 of the target's at most.
+constexpr int kKept = 64, kKeepers = kKept + 2;
+
+// The row of a sequence that begins at token t0 and has kKeepers tokens or more: no two of them have the same.
+__device__ __forceinline__ double *left_row(const VerifyArgs &a, int t0) { return a.left + int64_t(t0 / kKeepers) * a.vocab; }
+
+// What is left of a row of the target: of p, or of `left`, which is what earlier refusals have made of it, after n more.
 struct Rest {
     const float *p, *q;
     const double *refused;
     int n;
+    const double *left;
 };
 
 __device__ __forceinline__ double count(float p) { return p > 0.f ? static_cast<double>(p) : 0.; }   // negative numbers and not-a-numbers are 0
 
 // r of element v after one refusal.
-template <bool DRAFT>
+template <Draft DRAFT>
 __device__ __forceinline__ double refuse(double r, double q, double refused, int v) {
 #pragma clang fp contract(off)
-    if constexpr (DRAFT) {
+    if constexpr (DRAFT != kNoDraft) {
         const double part = refused * q, d = r - part;
         return d > 0. ? d : 0.;
     } else {
@@ -61,9 +79,9 @@ __device__ __forceinline__ double refuse(double r, double q, double refused, int
 }
 
 // r of one element, whose p and q are at hand
-template <bool DRAFT>
+template <Draft DRAFT>
 __device__ __forceinline__ double left_of(const Rest &x, int v, float p, float q) {
-    double r = count(p);
+    double r = DRAFT == kKeeping && x.left ? x.left[v] : count(p);
     for (int i = 0; i < x.n; ++i) r = refuse<DRAFT>(r, count(q), x.refused[i], v);
     return r;
 }
@@ -82,9 +100,27 @@ __device__ __forceinline__ void four_at(const float *row, int v, int hi, float (
 }
 
 // r of J times four elements, from v + j * step on, those below hi (others 0).
-template <bool DRAFT, int J>
+template <Draft DRAFT, int J>
 __device__ __forceinline__ void fours_of(const Rest &x, int v, int step, int hi, double (&r)[J][4]) {
     float p[J][4], q[J][4];
+    auto take_off = [&] {
+        for (int i = 0; i < x.n; ++i) {
+            const double refused = x.refused[i];
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) r[j][e] = refuse<DRAFT>(r[j][e], DRAFT ? count(q[j][e]) : 0., refused, v + j * step + e);
+        }
+    };
+    if (DRAFT == kKeeping && x.left) {
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            four_at(x.q, v + j * step, hi, q[j]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[j][e] = v + j * step + e < hi ? x.left[v + j * step + e] : 0.;
+        }
+        return take_off();
+    }
 #pragma unroll
     for (int j = 0; j < J; ++j) four_at(x.p, v + j * step, hi, p[j]);
     if (DRAFT && x.n) {
@@ -95,13 +131,7 @@ __device__ __forceinline__ void fours_of(const Rest &x, int v, int step, int hi,
     for (int j = 0; j < J; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) r[j][e] = count(p[j][e]);
-    for (int i = 0; i < x.n; ++i) {
-        const double refused = x.refused[i];
-#pragma unroll
-        for (int j = 0; j < J; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) r[j][e] = refuse<DRAFT>(r[j][e], DRAFT ? count(q[j][e]) : 0., refused, v + j * step + e);
-    }
+    take_off();
 }
 
 __device__ __forceinline__ double sum_of_wave(double s) {
@@ -110,14 +140,24 @@ __device__ __forceinline__ double sum_of_wave(double s) {
     return s;
 }
 
-// Sum of a wave's elements [lo, hi).
-template <bool DRAFT>
-__device__ __forceinline__ double sum_of(const Rest &x, int lo, int hi) {
+// Sum of a wave's elements [lo, hi).  KEEP: they go to `keep` where that is not null (it may be x.left: a thread writes what it has read).
+template <Draft DRAFT, bool KEEP>
+__device__ __forceinline__ double sum_of(const Rest &x, int lo, int hi, double *keep) {
     constexpr int kVectors = 4;
     double s = 0.;
     for (int base = lo; base < hi; base += kVectors * 4 * kWave) {
+        const int own = base + 4 * (threadIdx.x & 63);
         double r[kVectors][4];
-        fours_of<DRAFT, kVectors>(x, base + 4 * (threadIdx.x & 63), 4 * kWave, hi, r);
+        fours_of<DRAFT, kVectors>(x, own, 4 * kWave, hi, r);
+        if (KEEP && keep) {
+#pragma unroll
+            for (int j = 0; j < kVectors; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int at = own + j * 4 * kWave + e;
+                    if (at < hi) keep[at] = r[j][e];
+                }
+        }
 #pragma unroll
         for (int j = 0; j < kVectors; ++j) s += (r[j][0] + r[j][1]) + (r[j][2] + r[j][3]);
     }
@@ -132,14 +172,14 @@ struct DrawLds {
 __device__ __forceinline__ bool drawable(double sum) { return sum > 0. && sum < INFINITY; }
 
 // Every wave of the workgroup takes an equal run of [lo, hi); their sums in order.  Every thread calls it.
-template <bool DRAFT, int THREADS>
-__device__ __forceinline__ double sums_of_waves(const Rest &x, int lo, int hi, DrawLds &l, int &run) {
+template <Draft DRAFT, int THREADS, bool KEEP = false>
+__device__ __forceinline__ double sums_of_waves(const Rest &x, int lo, int hi, DrawLds &l, int &run, double *keep = nullptr) {
     constexpr int kWaves = THREADS / kWave;
     const int wave = threadIdx.x >> 6;
     run = ((hi - lo + kWaves - 1) / kWaves + 3) & ~3;
     const int from = min(lo + wave * run, hi), to = min(from + run, hi);
     __syncthreads();   // the sums may still be read from the call before
-    const double s = sum_of<DRAFT>(x, from, to);
+    const double s = sum_of<DRAFT, KEEP>(x, from, to, keep);
     if ((threadIdx.x & 63) == 0) l.sums[wave] = s;
     __syncthreads();
     double all = 0.;
@@ -189,7 +229,7 @@ __device__ __forceinline__ double prefix_of_wave(double s) {   // inclusive
 // The first element of [lo, hi) whose prefix sum is above `at`, else the last one that is not 0 (-1: none).  SHARE: `at` is a share of the sum, and the
 // result -2 where that is no positive finite number.  At most kEach elements of each thread, which are loaded once; every thread calls it.
 constexpr int kEach = 16;
-template <bool DRAFT, bool SHARE, int THREADS>
+template <Draft DRAFT, bool SHARE, int THREADS>
 __device__ int find_in(const Rest &x, int lo, int hi, double at, DrawLds &l) {
     constexpr int kWaves = THREADS / kWave;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, from = lo + tid * kEach;
@@ -235,7 +275,7 @@ __device__ int find_in(const Rest &x, int lo, int hi, double at, DrawLds &l) {
 }
 
 // The token of [lo, hi) at the share u of its sum; -2 where that is no positive finite number.
-template <bool DRAFT, int THREADS>
+template <Draft DRAFT, int THREADS>
 __device__ int draw_in(const Rest &x, int lo, int hi, double u, DrawLds &l) {
     if (hi - lo <= THREADS * kEach) return find_in<DRAFT, true, THREADS>(x, lo, hi, u, l);
     int run;
@@ -278,7 +318,7 @@ constexpr int kNodeBytes = 28;
 constexpr int kMaxNodes = 2048;
 
 // Every wave walks alike.  PASSES: a row is summed where a token was refused and another one hangs on the same.
-template <bool DRAFT, bool PASSES, int THREADS>
+template <Draft DRAFT, bool PASSES, int THREADS>
 __device__ End walk(const VerifyArgs &a, int t0, int T, const Nodes &nodes, DrawLds &l, int32_t *picks) {
     const int tid = threadIdx.x, lane = tid & 63;
     for (int j = tid; j < T; j += THREADS) {
@@ -296,6 +336,10 @@ __device__ End walk(const VerifyArgs &a, int t0, int T, const Nodes &nodes, Draw
     if (picks && tid == 0) picks[0] = 0;
     double m = 1.;
     bool known = true;   // m is the sum of what is left
+    int kept = 0;        // refusals at end.at that the row in the workspace holds
+    auto refusals = [&](const float *p, const float *q) {
+        return Rest{p, q, nodes.refused + end.at + 1 + kept, end.n - kept, kept ? left_row(a, t0) : nullptr};
+    };
     for (int after = 0;;) {
         int c = -1;   // the next one that hangs on it
         for (int j0 = (after + 1) & ~63; j0 < T; j0 += kWave) {
@@ -309,12 +353,15 @@ __device__ End walk(const VerifyArgs &a, int t0, int T, const Nodes &nodes, Draw
         if (c < 0) break;
         after = c;
         if (PASSES && !known) {
-            Rest x{a.target + (t0 + end.at) * a.target_stride, a.draft + (t0 + end.at) * a.draft_stride, nodes.refused + end.at + 1, end.n};
+            const Rest x = refusals(a.target + (t0 + end.at) * a.target_stride, a.draft + (t0 + end.at) * a.draft_stride);
+            const bool keep = DRAFT == kKeeping && end.n % kKept == 0;   // of at least kKeepers tokens: this one, kKept that were refused, and c
             int run;
-            m = sums_of_waves<DRAFT, THREADS>(x, 0, a.vocab, l, run);
+            m = sums_of_waves<DRAFT, THREADS, DRAFT == kKeeping>(x, 0, a.vocab, l, run, keep ? left_row(a, t0) : nullptr);
             known = true;
+            if (keep) kept = end.n;
         }
-        const Rest one{nullptr, nullptr, nodes.refused + end.at + 1, end.n};
+        Rest one = refusals(nullptr, nullptr);
+        if (DRAFT == kKeeping && (nodes.token[c] < 0 || nodes.token[c] >= a.vocab)) one.left = nullptr;   // such tokens have p = q = 0
         const double r = left_of<DRAFT>(one, nodes.token[c], nodes.p[c], nodes.q[c]);
         const double q = nodes.q[c] > 0.f ? static_cast<double>(nodes.q[c]) : 0.;
         const double limit = DRAFT ? m * q : m;
@@ -323,6 +370,7 @@ __device__ End walk(const VerifyArgs &a, int t0, int T, const Nodes &nodes, Draw
             end = End{c, 0, end.count + 1};
             m = 1.;
             known = true;
+            kept = 0;
         } else {
             nodes.refused[end.at + 1 + end.n++] = DRAFT ? m : static_cast<double>(nodes.token[c]);   // every wave writes the same
             if (DRAFT) known = false;
@@ -333,6 +381,15 @@ __device__ End walk(const VerifyArgs &a, int t0, int T, const Nodes &nodes, Draw
         for (int j = end.count + tid; j < a.max_q; j += THREADS) picks[j] = -1;
     return end;
 }
+
+// What is left at the end of a walk, of which `refused` holds all refusals.  The row was summed after each of them but the last.
+template <Draft DRAFT>
+__device__ __forceinline__ Rest rest_of(const VerifyArgs &a, int t0, int row, const double *refused, int n) {
+    const int kept = DRAFT == kKeeping && n > kKept ? (n - 1) / kKept * kKept : 0;
+    return Rest{a.target + row * a.target_stride, DRAFT ? a.draft + row * a.draft_stride : nullptr, refused + kept, n - kept, kept ? left_row(a, t0) : nullptr};
+}
+// the target's row itself
+__device__ __forceinline__ Rest whole_row(const Rest &x) { return Rest{x.p, x.q, nullptr, 0, nullptr}; }
 
 __device__ __forceinline__ bool sequence_at(const VerifyArgs &a, int s, int &t0, int &T) {
     t0 = max(a.cu[s], 0);
@@ -349,7 +406,7 @@ __device__ __forceinline__ void nothing(const VerifyArgs &a, int s) {
 }
 
 // A workgroup for each sequence does everything.
-template <bool DRAFT, int THREADS>
+template <Draft DRAFT, int THREADS>
 __global__ __launch_bounds__(THREADS) void verify_kernel(VerifyArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ DrawLds l;
@@ -357,14 +414,11 @@ __global__ __launch_bounds__(THREADS) void verify_kernel(VerifyArgs a) {
     int t0, T;
     if (!sequence_at(a, s, t0, T)) return nothing(a, s);
     const Nodes nodes = nodes_at(lds, a.max_q);
-    const End end = walk<DRAFT, DRAFT, THREADS>(a, t0, T, nodes, l, a.picks + int64_t(s) * a.max_q);
-    Rest x{a.target + (t0 + end.at) * a.target_stride, DRAFT ? a.draft + (t0 + end.at) * a.draft_stride : nullptr, nodes.refused + end.at + 1, end.n};
+    const End end = walk<DRAFT, DRAFT != kNoDraft, THREADS>(a, t0, T, nodes, l, a.picks + int64_t(s) * a.max_q);
+    const Rest x = rest_of<DRAFT>(a, t0, t0 + end.at, nodes.refused + end.at + 1, end.n);
     const double u = static_cast<double>(nodes.u[0]);
     int token = draw_in<DRAFT, THREADS>(x, 0, a.vocab, u, l);
-    if (token == -2) {   // nothing is left: the target's row itself
-        x.n = 0;
-        token = max(draw_in<DRAFT, THREADS>(x, 0, a.vocab, u, l), -1);
-    }
+    if (token == -2) token = max(draw_in<DRAFT, THREADS>(whole_row(x), 0, a.vocab, u, l), -1);   // nothing is left
     if (threadIdx.x == 0) {
         a.counts[s] = end.count;
         a.next[s] = token;
@@ -372,7 +426,7 @@ __global__ __launch_bounds__(THREADS) void verify_kernel(VerifyArgs a) {
 }
 
 // Rows in slices.  First launch: each workgroup walks the path (WALK; else verify_walk_kernel has) and sums its slice of the last row.
-template <bool DRAFT, bool WALK>
+template <Draft DRAFT, bool WALK>
 __global__ __launch_bounds__(kSmall) void verify_slices_kernel(VerifyArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ DrawLds l;
@@ -396,11 +450,11 @@ __global__ __launch_bounds__(kSmall) void verify_slices_kernel(VerifyArgs a) {
                 a.ends[s] = make_int2(t0 + end.at, end.n);
             }
         }
-        x = Rest{a.target + (t0 + end.at) * a.target_stride, DRAFT ? a.draft + (t0 + end.at) * a.draft_stride : nullptr, nodes.refused + end.at + 1, end.n};
+        x = rest_of<DRAFT>(a, t0, t0 + end.at, nodes.refused + end.at + 1, end.n);
     } else {
         const int2 end = a.ends[s];
         if (end.x < 0) return;
-        x = Rest{a.target + end.x * a.target_stride, DRAFT ? a.draft + end.x * a.draft_stride : nullptr, a.refused + int64_t(s) * a.max_q, end.y};
+        x = rest_of<DRAFT>(a, max(a.cu[s], 0), end.x, a.refused + int64_t(s) * a.max_q, end.y);
     }
     const int lo = slice * kSlice, hi = min(lo + kSlice, a.vocab);
     int run;
@@ -408,7 +462,7 @@ __global__ __launch_bounds__(kSmall) void verify_slices_kernel(VerifyArgs a) {
     if (tid == 0) a.parts[int64_t(s) * a.slices + slice] = sum;
 }
 
-template <bool DRAFT>
+template <Draft DRAFT>
 __global__ __launch_bounds__(kBig) void verify_walk_kernel(VerifyArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ DrawLds l;
@@ -420,7 +474,7 @@ __global__ __launch_bounds__(kBig) void verify_walk_kernel(VerifyArgs a) {
         return;
     }
     const Nodes nodes = nodes_at(lds, a.max_q);
-    const End end = walk<DRAFT, DRAFT, kBig>(a, t0, T, nodes, l, a.picks + int64_t(s) * a.max_q);
+    const End end = walk<DRAFT, DRAFT != kNoDraft, kBig>(a, t0, T, nodes, l, a.picks + int64_t(s) * a.max_q);
     for (int i = threadIdx.x; i < end.n; i += kBig) a.refused[int64_t(s) * a.max_q + i] = nodes.refused[end.at + 1 + i];
     if (threadIdx.x == 0) {
         a.counts[s] = end.count;
@@ -429,18 +483,19 @@ __global__ __launch_bounds__(kBig) void verify_walk_kernel(VerifyArgs a) {
 }
 
 // Last launch: the slice and the token in it.
-template <bool DRAFT>
+template <Draft DRAFT>
 __global__ __launch_bounds__(kDraw) void verify_draw_kernel(VerifyArgs a) {
     __shared__ DrawLds l;
     const int s = blockIdx.x, lane = threadIdx.x & 63;
     const int2 end = a.ends[s];
     if (end.x < 0) return;
-    Rest x{a.target + end.x * a.target_stride, DRAFT ? a.draft + end.x * a.draft_stride : nullptr, a.refused + int64_t(s) * a.max_q, end.y};
+    const int t0 = max(a.cu[s], 0);
+    const Rest x = rest_of<DRAFT>(a, t0, end.x, a.refused + int64_t(s) * a.max_q, end.y);
     const double *parts = a.parts + int64_t(s) * a.slices;
     double sum = 0.;
     for (int i = lane; i < a.slices; i += kWave) sum += parts[i];
     sum = sum_of_wave(sum);
-    const double u = static_cast<double>(a.u[max(a.cu[s], 0)]);
+    const double u = static_cast<double>(a.u[t0]);
     int token = -1;
     if (drawable(sum)) {
         double at = u * sum;
@@ -468,9 +523,8 @@ __global__ __launch_bounds__(kDraw) void verify_draw_kernel(VerifyArgs a) {
         const int lo = last * kSlice, hi = min(lo + kSlice, a.vocab);
         static_assert(kSlice <= kDraw * kEach, "a slice fits the registers of a workgroup");
         token = find_in<DRAFT, false, kDraw>(x, lo, hi, at, l);
-    } else if (x.n) {   // nothing is left: the target's row itself
-        x.n = 0;
-        token = max(draw_in<DRAFT, kDraw>(x, 0, a.vocab, u, l), -1);
+    } else if (end.y) {   // nothing is left
+        token = max(draw_in<DRAFT, kDraw>(whole_row(x), 0, a.vocab, u, l), -1);
     }
     if (threadIdx.x == 0) a.next[s] = token;
 }
@@ -478,7 +532,7 @@ __global__ __launch_bounds__(kDraw) void verify_draw_kernel(VerifyArgs a) {
 // Rows go in slices where they are long and the sequences are too few to give every CU one.
 int slices_of(int64_t vocab, int64_t sequences) { return vocab > 16384 && sequences < 256 ? static_cast<int>((vocab + kSlice - 1) / kSlice) : 0; }
 
-template <bool DRAFT>
+template <Draft DRAFT>
 void launch(const VerifyArgs &a, hipStream_t stream) {
     const unsigned lds = static_cast<unsigned>(kNodeBytes * a.max_q);
     if (!a.slices) {
@@ -491,7 +545,7 @@ void launch(const VerifyArgs &a, hipStream_t stream) {
     if (DRAFT && a.parents) {   // rows may have to be summed on the way
         hipLaunchKernelGGL((verify_walk_kernel<DRAFT>), dim3(a.n_seqs), dim3(kBig), lds, stream, a);
         hipLaunchKernelGGL((verify_slices_kernel<DRAFT, false>), grid, dim3(kSmall), 0, stream, a);
-    } else {
+    } else if constexpr (DRAFT != kKeeping) {
         hipLaunchKernelGGL((verify_slices_kernel<DRAFT, true>), grid, dim3(kSmall), lds, stream, a);
     }
     hipLaunchKernelGGL((verify_draw_kernel<DRAFT>), dim3(a.n_seqs), dim3(kDraw), 0, stream, a);
@@ -501,21 +555,26 @@ void launch(const VerifyArgs &a, hipStream_t stream) {
 
 int verify_most_tokens() { return kMaxNodes; }
 
+// of the slices; of the rows that are kept behind them
+static size_t slices_bytes(int64_t n_seqs, int64_t slices, int64_t max_q) { return slices ? 8 * static_cast<size_t>(n_seqs * (slices + 1 + max_q)) : 0; }
+static size_t left_bytes(int64_t total, int64_t max_q, int64_t vocab) { return max_q >= kKeepers ? 8 * static_cast<size_t>(total / kKeepers * vocab) : 0; }
+
 size_t verify_workspace(int64_t total, int32_t max_q, int32_t n_seqs, int64_t vocab) {
-    const int slices = slices_of(vocab, std::min<int64_t>(n_seqs, total));
-    return slices ? 8 * static_cast<size_t>(n_seqs) * (static_cast<size_t>(slices) + 1 + max_q) : 0;
+    return slices_bytes(n_seqs, slices_of(vocab, std::min<int64_t>(n_seqs, total)), max_q) + left_bytes(total, max_q, vocab);
 }
 
 tbn_status launch_verify(const VerifyCall &c, void *ws, hipStream_t stream) {
     VerifyArgs a{c.target, c.draft, c.target_stride, c.draft_stride, c.tokens, c.parents, c.u, c.cu_q, c.picks, c.counts, c.next, c.total, c.max_q, c.n_seqs,
-                 static_cast<int32_t>(c.vocab), nullptr, nullptr, nullptr, slices_of(c.vocab, std::min<int64_t>(c.n_seqs, c.total))};
+                 static_cast<int32_t>(c.vocab), nullptr, nullptr, nullptr, slices_of(c.vocab, std::min<int64_t>(c.n_seqs, c.total)), nullptr};
+    a.left = reinterpret_cast<double *>(static_cast<char *>(ws) + slices_bytes(a.n_seqs, a.slices, a.max_q));   // not looked at where there are none
     if (a.slices) {
         a.parts = static_cast<double *>(ws);
         a.refused = a.parts + int64_t(a.n_seqs) * a.slices;
         a.ends = reinterpret_cast<int2 *>(a.refused + int64_t(a.n_seqs) * a.max_q);
     }
-    if (a.draft) launch<true>(a, stream);
-    else launch<false>(a, stream);
+    if (!a.draft) launch<kNoDraft>(a, stream);
+    else if (!a.parents || !left_bytes(a.total, a.max_q, a.vocab)) launch<kDraft>(a, stream);
+    else launch<kKeeping>(a, stream);
     return check_launch("tbn_verify");
 }
 
