@@ -163,6 +163,16 @@ def _of(kind: type, x, name: str) -> None:
         raise ValueError(f"{name} must be a {kind.__name__}, got {type(x).__name__}")
 
 
+def _fit(*values: int):
+    """Integers as the library's 32 bits hold them, the nearest where they do not: a window beyond them is none, and what has to be at least a number stays it
+    (cut to its low bits, it would be another one).  Others are refused there."""
+    return tuple(v if -1 << 31 <= v < 1 << 31 else (1 << 31) - 1 if v > 0 else -1 << 31 for v in values)
+
+
+def _fit64(v: Optional[int]) -> int:
+    return 0 if v is None else v if -1 << 63 <= v < 1 << 63 else (1 << 63) - 1 if v > 0 else -1 << 63
+
+
 def _agree(pool, index: KVIndex):
     if pool.device != index.device:
         raise ValueError(f"pool and index must live on one device, got {pool.device} and {index.device}")
@@ -255,6 +265,7 @@ def tbn_kv_append(pool: KVPool, index: KVIndex, k_new: torch.Tensor, v_new: torc
         _of(KVPool, pool, "pool"), _of(KVIndex, index, "index")
     if _plain(stream) and tbn._host.kv_append(pool._at, pool._gpu, index._at, index._gpu, k_new, v_new, cu_new, max_new):
         return
+    max_new, = _fit(max_new)
     _agree(pool, index)
     k, ks = _rows(k_new, "k_new", pool.kv_heads, pool.dim, pool)
     v, vs = _rows(v_new, "v_new", pool.kv_heads, pool.dim, pool)
@@ -299,7 +310,8 @@ def _outputs(q: torch.Tensor, out: Optional[torch.Tensor], lse: Optional[torch.T
 def tbn_tree_attention_workspace_bytes(q: torch.Tensor, pool: KVPool, index: KVIndex, max_q: int, max_len: int = 0) -> int:
     if type(pool) is not KVPool or type(index) is not KVIndex:
         _of(KVPool, pool, "pool"), _of(KVIndex, index, "index")
-    return int(lib().tbn_tree_attention_workspace_bytes(pool._at, index._at, q.shape[0], max_q, q.shape[1], max_len))
+    max_q, = _fit(max_q)
+    return int(lib().tbn_tree_attention_workspace_bytes(pool._at, index._at, q.shape[0], max_q, q.shape[1], _fit64(max_len)))
 
 
 def tbn_tree_attention(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: torch.Tensor, max_q: int, mask: Optional[torch.Tensor] = None,
@@ -313,6 +325,7 @@ def tbn_tree_attention(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: torc
         r = tbn._host.tree_attention(q, pool._at, pool._gpu, index._at, index._gpu, cu_q, max_q, max_len, mask, scale)
         if r is not None:
             return r
+    max_q, = _fit(max_q)
     at, stride, cu = _queries(q, pool, index, cu_q)
     out, lse = _outputs(q, out, lse, stream)
     words = 0
@@ -321,10 +334,10 @@ def tbn_tree_attention(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: torc
             raise ValueError("mask must be (tokens, words)")
         words = mask.shape[1]
         _same_device(q.device, mask)
-    need = int(lib().tbn_tree_attention_workspace_bytes(pool._at, index._at, q.shape[0], max_q, q.shape[1], max_len or 0))
+    need = int(lib().tbn_tree_attention_workspace_bytes(pool._at, index._at, q.shape[0], max_q, q.shape[1], _fit64(max_len)))
     ws, size = _workspace(need, workspace, q.device, stream)
     _done(_call("tbn_tree_attention", at, stride, _dev(out, "out"), _dev(lse, "lse", torch.float32), pool._at, index._at, cu, q.shape[0], max_q, q.shape[1],
-                None if mask is None else _dev(mask, "mask", torch.int32), words, max_len or 0, 1.0 / math.sqrt(pool.dim) if scale is None else scale, ws, size,
+                None if mask is None else _dev(mask, "mask", torch.int32), words, _fit64(max_len), 1.0 / math.sqrt(pool.dim) if scale is None else scale, ws, size,
                 _stream(stream)))
     return out, lse
 
@@ -343,7 +356,8 @@ def tbn_window_attention_workspace_bytes(q: torch.Tensor, pool: KVPool, index: K
                                          max_len: int = 0) -> int:
     if type(pool) is not KVPool or type(index) is not KVIndex:
         _of(KVPool, pool, "pool"), _of(KVIndex, index, "index")
-    return int(lib().tbn_window_attention_workspace_bytes(pool._at, index._at, q.shape[0], max_q, q.shape[1], n_sink, window, int(masked), max_len))
+    max_q, n_sink, window = _fit(max_q, n_sink, window)
+    return int(lib().tbn_window_attention_workspace_bytes(pool._at, index._at, q.shape[0], max_q, q.shape[1], n_sink, window, int(masked), _fit64(max_len)))
 
 
 def tbn_window_attention(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: torch.Tensor, max_q: int, n_sink: int, window: int,
@@ -358,20 +372,22 @@ def tbn_window_attention(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: to
         r = tbn._host.window_attention(q, pool._at, pool._gpu, index._at, index._gpu, cu_q, max_q, max_len, mask, scale, n_sink, window)
         if r is not None:
             return r
+    max_q, n_sink, window = _fit(max_q, n_sink, window)
     at, stride, cu = _queries(q, pool, index, cu_q)
     out, lse = _outputs(q, out, lse, stream)
     mask_at, words = _mask(mask, q)
-    need = int(lib().tbn_window_attention_workspace_bytes(pool._at, index._at, q.shape[0], max_q, q.shape[1], n_sink, window, int(mask is not None), max_len or 0))
+    need = int(lib().tbn_window_attention_workspace_bytes(pool._at, index._at, q.shape[0], max_q, q.shape[1], n_sink, window, int(mask is not None), _fit64(max_len)))
     ws, size = _workspace(need, workspace, q.device, stream)
     _done(_call("tbn_window_attention", at, stride, _dev(out, "out"), _dev(lse, "lse", torch.float32), pool._at, index._at, cu, q.shape[0], max_q, q.shape[1],
-                n_sink, window, mask_at, words, max_len or 0, 1.0 / math.sqrt(pool.dim) if scale is None else scale, ws, size, _stream(stream)))
+                n_sink, window, mask_at, words, _fit64(max_len), 1.0 / math.sqrt(pool.dim) if scale is None else scale, ws, size, _stream(stream)))
     return out, lse
 
 
 def tbn_block_select_workspace_bytes(q: torch.Tensor, pool: KVPool, index: KVIndex, max_q: int, max_len: int = 0) -> int:
     if type(pool) is not KVPool or type(index) is not KVIndex:
         _of(KVPool, pool, "pool"), _of(KVIndex, index, "index")
-    return int(lib().tbn_block_select_workspace_bytes(pool._at, index._at, q.shape[0], max_q, q.shape[1], max_len))
+    max_q, = _fit(max_q)
+    return int(lib().tbn_block_select_workspace_bytes(pool._at, index._at, q.shape[0], max_q, q.shape[1], _fit64(max_len)))
 
 
 def tbn_block_select(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: torch.Tensor, max_q: int, n_select: int, n_sink: int = 1, n_recent: int = 1,
@@ -384,22 +400,24 @@ def tbn_block_select(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: torch.
         r = tbn._host.block_select(q, pool._at, pool._gpu, index._at, index._gpu, cu_q, max_q, max_len, n_select, n_sink, n_recent)
         if r is not None:
             return r
+    max_q, n_select, n_sink, n_recent = _fit(max_q, n_select, n_sink, n_recent)
     at, stride, cu = _queries(q, pool, index, cu_q)
     shape = (q.shape[0], pool.kv_heads, n_select)
     if picks is None:
         picks = _empty(shape, torch.int32, q.device, stream)
     elif tuple(picks.shape) != shape or picks.device != q.device:
         raise ValueError(f"picks must be {shape} on {q.device}")
-    need = int(lib().tbn_block_select_workspace_bytes(pool._at, index._at, q.shape[0], max_q, q.shape[1], max_len or 0))
+    need = int(lib().tbn_block_select_workspace_bytes(pool._at, index._at, q.shape[0], max_q, q.shape[1], _fit64(max_len)))
     ws, size = _workspace(need, workspace, q.device, stream)
     _done(_call("tbn_block_select", at, stride, _dev(picks, "picks", torch.int32), pool._at, index._at, cu, q.shape[0], max_q, q.shape[1], n_select, n_sink,
-                n_recent, max_len or 0, ws, size, _stream(stream)))
+                n_recent, _fit64(max_len), ws, size, _stream(stream)))
     return picks
 
 
 def tbn_block_attention_workspace_bytes(q: torch.Tensor, pool: KVPool, index: KVIndex, max_q: int, n_select: int) -> int:
     if type(pool) is not KVPool or type(index) is not KVIndex:
         _of(KVPool, pool, "pool"), _of(KVIndex, index, "index")
+    max_q, n_select = _fit(max_q, n_select)
     return int(lib().tbn_block_attention_workspace_bytes(pool._at, index._at, q.shape[0], max_q, q.shape[1], n_select))
 
 
@@ -413,6 +431,7 @@ def tbn_block_attention(q: torch.Tensor, pool: KVPool, index: KVIndex, cu_q: tor
         r = tbn._host.block_attention(q, pool._at, pool._gpu, index._at, index._gpu, cu_q, max_q, None, picks, scale)
         if r is not None:
             return r
+    max_q, = _fit(max_q)
     at, stride, cu = _queries(q, pool, index, cu_q)
     out, lse = _outputs(q, out, lse, stream)
     if picks.dim() != 3 or tuple(picks.shape[:2]) != (q.shape[0], pool.kv_heads):
@@ -432,6 +451,7 @@ def tbn_kv4_append(pool: KV4Pool, index: KVIndex, k_new: torch.Tensor, v_new: to
         _of(KV4Pool, pool, "pool"), _of(KVIndex, index, "index")
     if _plain(stream) and tbn._host.kv4_append(pool._at, pool._gpu, index._at, index._gpu, k_new, v_new, cu_new, max_new):
         return
+    max_new, = _fit(max_new)
     _agree(pool, index)
     k, ks = _rows(k_new, "k_new", pool.kv_heads, pool.dim, pool)
     v, vs = _rows(v_new, "v_new", pool.kv_heads, pool.dim, pool)
@@ -453,6 +473,7 @@ def tbn_kv4_read(pool: KV4Pool, index: KVIndex, cu: torch.Tensor, max_n: int, to
         r = tbn._host.kv4_read(pool._at, pool._gpu, index._at, index._gpu, cu, max_n, total, dtype is torch.float32)
         if r is not None:
             return r
+    max_n, = _fit(max_n)
     _agree(pool, index)
     k, v = (_empty((total, pool.kv_heads, pool.dim), dtype, pool.device, stream) for _ in range(2))
     _done(_call("tbn_kv4_read", pool._at, index._at, k.data_ptr(), v.data_ptr(), _dt(k), _ints(cu, "cu", index.n_seqs + 1, index.device), total, max_n, _stream(stream)))
@@ -489,7 +510,8 @@ def tbn_kv4_attention_workspace_bytes(q: torch.Tensor, pool: KV4Pool, index: KVI
                                       max_len: int = 0) -> int:
     if type(pool) is not KV4Pool or type(index) is not KVIndex:
         _of(KV4Pool, pool, "pool"), _of(KVIndex, index, "index")
-    return int(lib().tbn_kv4_attention_workspace_bytes(pool._at, index._at, _dt(q), q.shape[0], max_q, q.shape[1], n_sink, window, int(masked), max_len))
+    max_q, n_sink, window = _fit(max_q, n_sink, window)
+    return int(lib().tbn_kv4_attention_workspace_bytes(pool._at, index._at, _dt(q), q.shape[0], max_q, q.shape[1], n_sink, window, int(masked), _fit64(max_len)))
 
 
 def tbn_kv4_attention(q: torch.Tensor, pool: KV4Pool, index: KVIndex, cu_q: torch.Tensor, max_q: int, mask: Optional[torch.Tensor] = None,
@@ -503,13 +525,14 @@ def tbn_kv4_attention(q: torch.Tensor, pool: KV4Pool, index: KVIndex, cu_q: torc
         r = tbn._host.kv4_attention(q, pool._at, pool._gpu, index._at, index._gpu, cu_q, max_q, max_len, mask, scale, n_sink, window)
         if r is not None:
             return r
+    max_q, n_sink, window = _fit(max_q, n_sink, window)
     at, stride, cu = _queries(q, pool, index, cu_q)
     out, lse = _outputs(q, out, lse, stream)
     mask_at, words = _mask(mask, q)
-    need = int(lib().tbn_kv4_attention_workspace_bytes(pool._at, index._at, _dt(q), q.shape[0], max_q, q.shape[1], n_sink, window, int(mask is not None), max_len or 0))
+    need = int(lib().tbn_kv4_attention_workspace_bytes(pool._at, index._at, _dt(q), q.shape[0], max_q, q.shape[1], n_sink, window, int(mask is not None), _fit64(max_len)))
     ws, size = _workspace(need, workspace, q.device, stream)
     _done(_call("tbn_kv4_attention", at, stride, _dt(q), _dev(out, "out"), _dev(lse, "lse", torch.float32), pool._at, index._at, cu, q.shape[0], max_q, q.shape[1],
-                n_sink, window, mask_at, words, max_len or 0, 1.0 / math.sqrt(pool.dim) if scale is None else scale, ws, size, _stream(stream)))
+                n_sink, window, mask_at, words, _fit64(max_len), 1.0 / math.sqrt(pool.dim) if scale is None else scale, ws, size, _stream(stream)))
     return out, lse
 
 
@@ -535,6 +558,7 @@ def tbn_verify(target: torch.Tensor, tokens: torch.Tensor, u: torch.Tensor, cu_q
         r = tbn._host.verify(target, tokens, u, cu_q, max_q, draft, parents)
         if r is not None:
             return r
+    max_q, = _fit(max_q)
     dev, n_seqs = target.device, cu_q.numel() - 1
     p, ps = _probabilities(target, "target")
     q, qs = (None, 0) if draft is None else _probabilities(draft, "draft", target)
