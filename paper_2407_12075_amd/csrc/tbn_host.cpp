@@ -660,7 +660,7 @@ PyObject *verify(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     int64_t ps, qs = 0, most;
     if (!p_verify_workspace_bytes || !p_verify || n_args != 7 || !ordinary_context()) Py_RETURN_NONE;
     const at::Tensor *p = probabilities(args[0], ps), *q = nullptr;
-    if (!p || !integer(args[4], 0, 1 << 30, most)) Py_RETURN_NONE;
+    if (!p || !integer(args[4], 0, 2048, most)) Py_RETURN_NONE;   // more tokens, or sequences, get no memory: the wrapper raises the library's error
     const int64_t n = p->size(0), vocab = p->size(1), gpu = p->device().index();
     const int32_t *tokens = ints(args[1], n, gpu), *cu = ints(args[3], 2, gpu), *parents = nullptr;
     const at::Tensor *u = plain(args[2], at::kFloat, *p);
@@ -668,7 +668,7 @@ PyObject *verify(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     if (args[5] != Py_None && (!(q = probabilities(args[5], qs)) || q->sizes() != p->sizes() || q->device() != p->device())) Py_RETURN_NONE;
     if (args[6] != Py_None && !(parents = ints(args[6], n, gpu))) Py_RETURN_NONE;
     const int64_t n_seqs = THPVariable_Unpack(args[3]).numel() - 1;
-    if (n_seqs > INT32_MAX) Py_RETURN_NONE;
+    if (n_seqs > 8192) Py_RETURN_NONE;
     const auto options = THPVariable_Unpack(args[3]).options();
     at::Tensor picks = at::empty({n_seqs, most}, options), counts = at::empty({n_seqs}, options), next = at::empty({n_seqs}, options), ws;
     const int32_t max_q = static_cast<int32_t>(most), seqs = static_cast<int32_t>(n_seqs);

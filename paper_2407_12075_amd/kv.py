@@ -33,6 +33,8 @@ from .tbn import _call, _dev, _dt, _empty, _own, _raise, _stream, lib, TBN_OK
 
 TBN_KV_FULL = 1
 TBN_KV_INVALID = 2
+MAX_SEQUENCES = 8192        # of an index, of a verification
+VERIFY_MAX_TOKENS = 2048    # of a sequence
 
 
 class _Pool(ctypes.Structure):
@@ -569,7 +571,9 @@ def tbn_verify(target: torch.Tensor, tokens: torch.Tensor, u: torch.Tensor, cu_q
             raise ValueError(f"{name} has {t.numel()} entries, {n} needed")
     if n_seqs < 1 or max_q < 0:
         raise ValueError("cu_q must have an entry more than there are sequences, max_q must be >= 0")
-    picks, counts, follows = (_empty(shape, torch.int32, dev, stream) for shape in ((n_seqs, max_q), (n_seqs,), (n_seqs,)))
+    # sizes that the library refuses get no memory: the call below raises its error
+    fine = max_q <= VERIFY_MAX_TOKENS and n_seqs <= MAX_SEQUENCES
+    picks, counts, follows = (_empty(shape, torch.int32, dev, stream) for shape in (((n_seqs, max_q), (n_seqs,), (n_seqs,)) if fine else ((0,),) * 3))
     ws, size = _workspace(int(lib().tbn_verify_workspace_bytes(n, max_q, n_seqs, vocab)), workspace, dev, stream)
     _done(_call("tbn_verify", p, ps, q, qs, _dev(tokens, "tokens", torch.int32), None if parents is None else _dev(parents, "parents", torch.int32),
                 _dev(u, "u", torch.float32), _dev(cu_q, "cu_q", torch.int32), n, max_q, n_seqs, vocab, picks.data_ptr(), counts.data_ptr(), follows.data_ptr(),
