@@ -162,6 +162,8 @@ class Decoder:
         tokens (0: none).  Returns (tokens (sequences, depth + 1), counts): what follows `last`, of which counts are emitted.  temperature > 0:
         tokens are drawn with numbers of `generator` (on the model's device)."""
         cfg, index, dev = self.cfg, self.index, self.device
+        if depth and 0 < cfg.window < 2 * depth + 1:   # before anything is drafted, so that the cache stays as it is
+            raise ValueError(f"a window of {cfg.window} tokens does not hold the tree of {2 * depth + 1}")
         n = last.numel()
         live = torch.zeros(cfg.n_seqs, dtype=torch.int32, device=dev)
         live[:n] = 1
