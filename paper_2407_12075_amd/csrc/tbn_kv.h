@@ -73,6 +73,12 @@ tbn_status launch_verify(const VerifyCall &c, void *ws, hipStream_t stream);
 
 // what the GPU's data say is bounded before it becomes an address
 __device__ __forceinline__ int32_t page_in(int32_t page, int32_t n_pages) { return min(max(page, 0), n_pages - 1); }
+// Tokens of a sequence, none where not above 0.  An end below 0, which no call has, is taken as that of the call: less the first token it could leave 32 bits and come out
+// above 0.  (As an unsigned number it costs nothing; an instruction more for another order moved one token on the cache in 4 bits from 6.85 us to 7.0.)
+__device__ __forceinline__ int32_t tokens_in(const int32_t *cu, int s, int64_t total, int32_t &first) {
+    first = max(cu[s], 0);
+    return static_cast<int32_t>(min(static_cast<uint32_t>(cu[s + 1]), static_cast<uint32_t>(total))) - first;
+}
 __device__ __forceinline__ int32_t len_in(int32_t len, int64_t most) { return min(max(len, 0), static_cast<int32_t>(most)); }
 
 // exponent x with 2^(x-1) <= a < 2^x for finite a >= 0, at least -100; the power of two of a whole number -126 .. 127

@@ -63,7 +63,8 @@ struct Share {
 
 __device__ __forceinline__ bool share_of(const tbn_kv4_pool &p, const tbn_kv_index &ix, const int32_t *cu, int total, Share &sh) {
     const int s = blockIdx.z, shift = __ffs(p.page) - 1;
-    const int t0 = max(cu[s], 0), n = min(cu[s + 1], total) - t0, len = len_in(ix.lens[s], int64_t(ix.max_pages) << shift);
+    int t0;
+    const int n = tokens_in(cu, s, total, t0), len = len_in(ix.lens[s], int64_t(ix.max_pages) << shift);
     if (n <= 0 || n > len) return false;
     const int base = ((len - n) & -kBlock) + static_cast<int>(blockIdx.x) * kBlock;
     if (base >= len) return false;

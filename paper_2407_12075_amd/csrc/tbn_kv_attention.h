@@ -153,8 +153,7 @@ struct Span {
 
 __device__ __forceinline__ Span span_of(const AttentionArgs &a, int s) {
     Span v;
-    v.t0 = max(a.q.cu_q[s], 0);
-    const int all = min(a.q.cu_q[s + 1], static_cast<int>(a.q.total_q)) - v.t0;
+    const int all = tokens_in(a.q.cu_q, s, a.q.total_q, v.t0);
     v.T = min(all, a.q.max_q);
     v.len = len_in(a.ix.lens[s], a.q.max_len);
     v.prefix = max(v.len - max(all, 0), 0);

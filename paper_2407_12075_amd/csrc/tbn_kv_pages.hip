@@ -408,7 +408,8 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(tbn_kv_pool p, tbn_
     constexpr int V = Pack<T>::kVec;
     __shared__ union { AppendLds<T> v; SummaryLds s; } lds;
     const int tid = threadIdx.x, s = blockIdx.z, head = blockIdx.y, shift = __ffs(p.page) - 1;
-    const int failed = *ix.status, t0 = max(cu_new[s], 0), n = min(cu_new[s + 1], total) - t0;
+    int t0;
+    const int failed = *ix.status, n = tokens_in(cu_new, s, total, t0);
     const int len = len_in(ix.lens[s], int64_t(ix.max_pages) << shift);
     if (failed || n <= 0 || n > len) return;
     const int slot = ((len - n) >> shift) + blockIdx.x, base = slot << shift;

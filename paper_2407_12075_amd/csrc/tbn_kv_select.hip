@@ -175,7 +175,8 @@ struct Query {
 
 __device__ __forceinline__ Query query_of(const SelectArgs &a, int s, int t) {
     Query r;
-    const int t0 = max(a.q.cu_q[s], 0), T = min(a.q.cu_q[s + 1], static_cast<int>(a.q.total_q)) - t0;
+    int t0;
+    const int T = tokens_in(a.q.cu_q, s, a.q.total_q, t0);
     const int len = len_in(a.ix.lens[s], a.q.max_len), shift = __ffs(a.p.page) - 1;
     r.there = t < min(T, a.q.max_q);
     r.tok = t0 + t;

@@ -392,8 +392,7 @@ __device__ __forceinline__ Rest rest_of(const VerifyArgs &a, int t0, int row, co
 __device__ __forceinline__ Rest whole_row(const Rest &x) { return Rest{x.p, x.q, nullptr, 0, nullptr}; }
 
 __device__ __forceinline__ bool sequence_at(const VerifyArgs &a, int s, int &t0, int &T) {
-    t0 = max(a.cu[s], 0);
-    T = min(min(a.cu[s + 1], static_cast<int>(a.total)) - t0, a.max_q);
+    T = min(tokens_in(a.cu, s, a.total, t0), a.max_q);
     return T > 0;
 }
 
