@@ -118,3 +118,21 @@ def test_a_refusal_costs_one_pass(kv):
     print(f"2047 refusals on 131072 elements: {ms:.1f} ms")
     assert counts.tolist() == [1] and 0 <= int(follows) < V
     assert ms < 2000
+
+
+@pytest.mark.parametrize("V", [16385, 40000])
+@pytest.mark.parametrize("n", [64, 65, 66, 130])
+def test_among_many_sequences(kv, V, n):
+    """A sequence of n refused siblings among 260 others: a workgroup draws from what they left in runs of the row."""
+    rng = np.random.RandomState(n)
+    sizes = [1] * 120 + [n + 1] + [1] * 100 + [n + 1] + [1] * 40
+    N = sum(sizes)
+    p, q = rows(rng, 1, V)
+    low, _ = least(p[0], q[0], V // 4)
+    p, q = np.repeat(p, N, 0), np.repeat(q, N, 0)
+    tokens, parents, u = np.zeros(N, np.int32), np.full(N, -1, np.int32), rng.rand(N).astype(np.float32)
+    for first in (120, 120 + n + 1 + 100):
+        tokens[first + 1:first + n + 1], parents[first + 1:first + n + 1], u[first + 1:first + n + 1] = rng.choice(low, n), 0, 1.0
+    assert kv.lib().tbn_verify_workspace_bytes(N, n + 1, len(sizes), V) == (8 * V * (N // 66) if n >= 65 else 0)
+    got = check(kv, p, q, tokens, parents, u, sizes)
+    assert max(got[1].tolist()) == 1
